@@ -330,6 +330,102 @@ awe_status_t awe_reconstruct(awe_handle_t h, int enc, int modulus, const float* 
                              int64_t ldp, int64_t M, int64_t N, void* C_dev, awe_out_dtype_t out_dt, int64_t ldc,
                              void* stream);
 
+/* ---- Serving operators: a linear layer on 4-bit weights, and a paged cache of 8-bit keys and values with
+ * the attention that reads it.  They keep the integer containers of this library (AWE_I4_PACKED weights,
+ * AWE_I8 cache values) and multiply them with floating-point activations, so they round where the exact
+ * products above do not: every sum, softmax statistic and scale is held in 32 bits, and the result is
+ * rounded once to its output type.  (No counterpart in the paper.)
+ *   - An empty batch (M, T or B equal to 0) is not an error.
+ *   - Lengths, tables and slots are read on the device only.  An entry that points outside what the
+ *     descriptor says exists (a page outside the pool, a slot outside it) is skipped, never followed.
+ *   - Warmed-up calls can be captured in a CUDA graph: sizes that the host passes are upper bounds,
+ *     lengths are read when the graph runs. */
+
+typedef enum {
+    AWE_F16 = 0,
+    AWE_BF16 = 1,
+    AWE_F32 = 2
+} awe_float_t;
+
+/* A linear layer's weight: w(n, k) = scale(n, k / group) * (code(n, k) - zero(n, k / group)). */
+typedef struct {
+    const void* codes_dev;   /* N x K signed 4-bit values, AWE_I4_PACKED, row n at byte n * ld / 2        */
+    const void* scale_dev;   /* N x ceil(K / group), row-major, of type scale_type (AWE_F16, AWE_BF16)   */
+    const int8_t* zero_dev;  /* NULL, or N x ceil(K / group) zero points, AWE_I4_IN_I8                   */
+    int64_t N, K, ld;        /* ld: elements from one row of codes to the next, even, >= K               */
+    int64_t group;           /* values of k that share a scale: a power of two >= 32                     */
+    int32_t scale_type;
+} awe_w4_matrix;
+
+/* y(m, n) = sum_k x(m, k) w(n, k).  x_dev: M x K of type x_type (AWE_F16 or AWE_BF16), row stride ldx;
+ * y_dev: M x N of x's type or AWE_F32, row stride ldy (elements).  Products are exact (a 4-bit code less its zero
+ * point has 5 significant bits), summed in FP32 over a group (part of one where it is longer than 256), scaled in
+ * FP32 and summed in FP32; y is rounded once.  Every alignment of the element size is accepted; codes_dev % 16 == 0 with ld % 32 == 0, and
+ * x_dev % 16 == 0 with ldx % 8 == 0, take 16-byte loads of rows as they lie. */
+awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, const void* x_dev, awe_float_t x_type, int64_t M,
+                           int64_t ldx, void* y_dev, awe_float_t y_type, int64_t ldy, void* stream);
+
+/* A pool of pages of keys and values: token `i` of page p, head g, is the head_dim signed bytes at
+ * ((p * n_heads + g) * page_size + i) * head_dim, and stands for them times the scale of (p, g). */
+typedef struct {
+    int8_t* k_dev;           /* n_pages x n_heads x page_size x head_dim, 16-B aligned                   */
+    int8_t* v_dev;
+    float* k_scale_dev;      /* n_pages x n_heads                                                        */
+    float* v_scale_dev;
+    int64_t n_pages, n_heads;
+    int64_t page_size;       /* tokens of a page: a power of two, 16 .. 256                              */
+    int64_t head_dim;        /* 64, 128 or 256                                                           */
+} awe_kv_cache;
+
+/* What a step over B requests (at most AWE_KV_MAX_REQUESTS) needs to know of its pages.  Request b holds cached_len[b] tokens and adds
+ * new_len[b] (negative lengths count as 0; the sums stay below 2^31).  Its row of block_table_dev (max_pages
+ * entries, rows ld_table apart) names the pages of the tokens it holds; the entries of the pages it needs
+ * besides are written, taken from free_pages_dev in order, request by request (-1 where the list has ended).
+ * Entries before and behind those stay as they are.  Written besides:
+ *   slots_dev[max_tokens] (int64)      page * page_size + place of every new token, request by request; -1
+ *                                      where it has no page, and behind the last token
+ *   positions_dev[max_tokens] (int32)  its position in its request; -1 behind the last token (may be NULL)
+ *   q_start_dev[B + 1], ctx_len_dev[B] first new token of each request, and the tokens it then holds
+ *   counts_dev[4]                      pages taken, new tokens, pages that were wanted and not had (the
+ *                                      list or a table row was too short), longest request
+ * Nothing is removed from the free list: the caller drops its first counts_dev[0] entries.  A call with the
+ * same arguments again writes the same again. */
+#define AWE_KV_MAX_REQUESTS 16384
+awe_status_t awe_kv_plan(awe_handle_t h, const int32_t* cached_len_dev, const int32_t* new_len_dev, int64_t B,
+                         int64_t page_size, const int32_t* free_pages_dev, int64_t n_free, int32_t* block_table_dev,
+                         int64_t max_pages, int64_t ld_table, int64_t* slots_dev, int32_t* positions_dev,
+                         int64_t max_tokens, int32_t* q_start_dev, int32_t* ctx_len_dev, int32_t* counts_dev,
+                         void* stream);
+
+/* Quantise T new tokens' keys and values (type AWE_F16 or AWE_BF16, T x n_heads x head_dim, token strides
+ * ldk and ldv in elements) into their slots.  The tokens of one page stand together in the list and fill it in order
+ * (awe_kv_plan's order).  The scale of a page and head is the largest magnitude in it times 1 / 127 (both FP32); it starts anew with the
+ * token at place 0 and only grows: where a new token needs a larger one, the values already there are rounded
+ * again to it.  A value is stored as round(x * (1 / scale)), ties to even.  NaN is stored as 0 and an infinity
+ * as +-127, and neither counts for the scale; new tokens whose magnitudes all stay below 2^-100 ask for scale 0.  A negative slot, or one outside the
+ * pool, is skipped. */
+awe_status_t awe_kv_write(awe_handle_t h, const awe_kv_cache* cache, const void* k_dev, const void* v_dev,
+                          awe_float_t type, int64_t T, int64_t ldk, int64_t ldv, const int64_t* slots_dev,
+                          void* stream);
+
+/* Scratch awe_kv_attention needs for at most T queries of B requests. */
+size_t awe_kv_attention_workspace_bytes(awe_handle_t h, const awe_kv_cache* cache, int64_t T, int64_t n_q_heads,
+                                        int64_t B);
+
+/* out(t, head) = sum_j p_j v_j, p = softmax over the visible tokens of scale * q . k_j, for the T queries of B
+ * requests: request b has the queries q_start[b] .. q_start[b+1] - 1, which are its last ones of ctx_len[b]
+ * tokens.  Query head i reads cache head i / (n_q_heads / n_heads).  causal: a query sees the tokens up to its own
+ * position, else all ctx_len[b]; window > 0 (causal only): the last `window` of those.  A query that sees nothing gets zeros and
+ * lse = -inf.  A table entry outside the pool hides its tokens.  q_dev: T x n_q_heads x head_dim of type AWE_F16 or AWE_BF16 with token stride
+ * ldq, out_dev alike with ldo; lse_dev (T x n_q_heads floats, natural logarithm of the sum of exponentials) may
+ * be NULL.  q_dev and out_dev 16-B aligned, ldq and ldo multiples of 8.  workspace_dev: 256-B aligned. */
+awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const void* q_dev, awe_float_t type,
+                              int64_t T, int64_t n_q_heads, int64_t ldq, const int32_t* q_start_dev,
+                              const int32_t* ctx_len_dev, int64_t B, const int32_t* block_table_dev,
+                              int64_t max_pages, int64_t ld_table, float scale, int causal, int64_t window,
+                              void* out_dev, int64_t ldo, float* lse_dev, void* workspace_dev,
+                              size_t workspace_bytes, void* stream);
+
 /* Wait for `stream` and read the handle's device status word: AWE_OK, or AWE_ERR_TIMEOUT with
  * *site (may be NULL) naming the wait that gave up.  The word is cleared by the read. */
 awe_status_t awe_last_device_status(awe_handle_t h, void* stream, int* site);

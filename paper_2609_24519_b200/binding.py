@@ -32,12 +32,14 @@ SIDE_A, SIDE_B = 0, 1
 ROWMAJOR_RxK, ROWMAJOR_KxR = 0, 1
 MAX_PRODUCTS, MAX_PLANES = 16, 8
 STATIC_WORKSPACE_BYTES = 24 << 20
+F16, BF16, F32 = 0, 1, 2
+KV_MAX_REQUESTS = 16384
 
 EXPORTS = ["awe_create", "awe_destroy", "awe_encoding_info", "awe_encoding_lut", "awe_planes_bytes",
            "awe_workspace_bytes", "awe_host_staging_bytes", "awe_encode", "awe_gemm_planes", "awe_gemm_exact",
            "awe_gemm_exact_host", "awe_gemm_exact_static", "awe_wide_moduli", "awe_wide_select", "awe_wide_workspace_bytes",
            "awe_wide_residues", "awe_wide_crt", "awe_gemm_exact_wide", "awe_reconstruct", "awe_fp4_product_raw", "awe_fp8_product_raw", "awe_last_device_status", "awe_selftest_bounded_wait", "awe_last_gemm_clock_mhz", "awe_launch_count",
-           "awe_status_string"]
+           "awe_status_string", "awe_linear_w4", "awe_kv_plan", "awe_kv_write", "awe_kv_attention_workspace_bytes", "awe_kv_attention"]
 
 
 class EncodingDesc(ctypes.Structure):
@@ -49,6 +51,20 @@ class EncodingDesc(ctypes.Structure):
                 ("b_hi", ctypes.c_int32), ("plane_bits_a", ctypes.c_int32 * MAX_PLANES),
                 ("plane_bits_b", ctypes.c_int32 * MAX_PLANES), ("fp8", ctypes.c_int32 * MAX_PRODUCTS),
                 ("ia2", ctypes.c_int32 * MAX_PRODUCTS), ("ib2", ctypes.c_int32 * MAX_PRODUCTS)]
+
+
+class W4Matrix(ctypes.Structure):
+    """awe_w4_matrix; keeps the tensors it points into alive."""
+    _fields_ = [("codes_dev", ctypes.c_void_p), ("scale_dev", ctypes.c_void_p), ("zero_dev", ctypes.c_void_p),
+                ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("ld", ctypes.c_int64), ("group", ctypes.c_int64),
+                ("scale_type", ctypes.c_int32)]
+
+
+class KvCache(ctypes.Structure):
+    """awe_kv_cache; keeps the tensors it points into alive."""
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("k_scale_dev", ctypes.c_void_p),
+                ("v_scale_dev", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_heads", ctypes.c_int64),
+                ("page_size", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
 
 
 class AweError(RuntimeError):
@@ -94,6 +110,14 @@ def lib() -> ctypes.CDLL:
     L.awe_reconstruct.argtypes = [vp, i32, i32, vp, i64, i64, i64, i64, vp, i32, i64, vp]
     L.awe_fp4_product_raw.argtypes = [vp, vp, vp, i64, i64, i64, vp, i64, vp]
     L.awe_fp8_product_raw.argtypes = [vp, vp, vp, i64, i64, i64, vp, i64, vp]
+    f32, mat, kv = ctypes.c_float, ctypes.POINTER(W4Matrix), ctypes.POINTER(KvCache)
+    L.awe_linear_w4.argtypes = [vp, mat, vp, i32, i64, i64, vp, i32, i64, vp]
+    L.awe_kv_plan.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, i64, i64, vp, vp, i64, vp, vp, vp, vp]
+    L.awe_kv_write.argtypes = [vp, kv, vp, vp, i32, i64, i64, i64, vp, vp]
+    L.awe_kv_attention_workspace_bytes.argtypes = [vp, kv, i64, i64, i64]
+    L.awe_kv_attention_workspace_bytes.restype = sz
+    L.awe_kv_attention.argtypes = [vp, kv, vp, i32, i64, i64, i64, vp, vp, i64, vp, i64, i64, f32, i32, i64, vp, i64, vp, vp,
+                                   sz, vp]
     L.awe_last_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     L.awe_selftest_bounded_wait.argtypes = [vp, i64, vp]
     L.awe_last_gemm_clock_mhz.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_double)]
@@ -279,6 +303,52 @@ def awe_reconstruct(h: Handle, enc: int, modulus: int, P, plane_stride: int, ldp
                     out_dt: int, ldc: int, stream=None) -> None:
     _check(lib().awe_reconstruct(h.raw, enc, modulus, _ptr(P), plane_stride, ldp, M, N, _ptr(C), out_dt, ldc,
                                  _stream(stream)), "awe_reconstruct")
+
+
+# ------------------------------------------------------------------ serving operators
+def w4_matrix(codes, scale, scale_type: int, zero, N: int, K: int, ld: int, group: int) -> W4Matrix:
+    """Describes a 4-bit weight matrix (awe_w4_matrix); zero may be None."""
+    W = W4Matrix(_ptr(codes), _ptr(scale), _ptr(zero), N, K, ld, group, scale_type)
+    W.tensors = (codes, scale, zero)
+    return W
+
+
+def kv_cache(k, v, k_scale, v_scale, n_pages: int, n_heads: int, page_size: int, head_dim: int) -> KvCache:
+    """Describes a paged 8-bit cache (awe_kv_cache)."""
+    c = KvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, n_heads, page_size, head_dim)
+    c.tensors = (k, v, k_scale, v_scale)
+    return c
+
+
+def awe_linear_w4(h: Handle, W: W4Matrix, x, x_type: int, M: int, ldx: int, y, y_type: int, ldy: int, stream=None) -> None:
+    _check(lib().awe_linear_w4(h.raw, W, _ptr(x), x_type, M, ldx, _ptr(y), y_type, ldy, _stream(stream)), "awe_linear_w4")
+
+
+def awe_kv_plan(h: Handle, cached_len, new_len, B: int, page_size: int, free_pages, n_free: int, block_table,
+                max_pages: int, ld_table: int, slots, positions, max_tokens: int, q_start, ctx_len, counts,
+                stream=None) -> None:
+    _check(lib().awe_kv_plan(h.raw, _ptr(cached_len), _ptr(new_len), B, page_size, _ptr(free_pages), n_free,
+                             _ptr(block_table), max_pages, ld_table, _ptr(slots), _ptr(positions), max_tokens,
+                             _ptr(q_start), _ptr(ctx_len), _ptr(counts), _stream(stream)), "awe_kv_plan")
+
+
+def awe_kv_write(h: Handle, cache: KvCache, k, v, dtype: int, T: int, ldk: int, ldv: int, slots, stream=None) -> None:
+    _check(lib().awe_kv_write(h.raw, cache, _ptr(k), _ptr(v), dtype, T, ldk, ldv, _ptr(slots), _stream(stream)),
+           "awe_kv_write")
+
+
+def awe_kv_attention_workspace_bytes(h: Handle, cache: KvCache, T: int, n_q_heads: int, B: int) -> int:
+    return int(lib().awe_kv_attention_workspace_bytes(h.raw, cache, T, n_q_heads, B))
+
+
+def awe_kv_attention(h: Handle, cache: KvCache, q, dtype: int, T: int, n_q_heads: int, ldq: int, q_start, ctx_len, B: int,
+                     block_table, max_pages: int, ld_table: int, scale: float, causal: bool, window: int, out, ldo: int,
+                     lse, workspace, workspace_bytes: Optional[int] = None, stream=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    _check(lib().awe_kv_attention(h.raw, cache, _ptr(q), dtype, T, n_q_heads, ldq, _ptr(q_start), _ptr(ctx_len), B,
+                                  _ptr(block_table), max_pages, ld_table, scale, causal, window, _ptr(out), ldo, _ptr(lse),
+                                  _ptr(workspace), workspace_bytes, _stream(stream)), "awe_kv_attention")
 
 
 def awe_last_device_status(h: Handle, stream=None):

@@ -1,0 +1,207 @@
+// Quantises new keys and values into the pages of the 8-bit cache (awe_kv_write).
+//
+// For the run of tokens of one page and head: a = max |x| over the run's finite values, s' = max(s, a * (1 / 127)) with the
+// scale s that the page has (0 where the run starts the page), q = round(x / s'); where s' > s the values already in the page
+// become round(q s / s').  Each row is read once (it waits in registers between the maximum and the rounding) and
+// written once: 3 bytes per value, bound by HBM.  The list's tokens of one page stand together, so a block finds its
+// runs by itself: it looks at `window` neighbouring slots and takes the runs that begin there.
+#include <algorithm>
+
+#include "awe_internal.h"
+#include "serve_common.cuh"
+
+namespace awe {
+namespace {
+
+using namespace serve;
+
+constexpr int kThreads = 128;
+constexpr int kHeld = 4;  // 16-byte pieces a thread keeps in registers between the two passes
+
+struct WriteParams {
+    const void *k, *v;
+    int8_t *k_cache, *v_cache;
+    float *k_scale, *v_scale;
+    const int64_t* slots;
+    int64_t ldk, ldv, T, n_slots;
+    int heads, page_log2, dim_log2, window;
+};
+
+template <bool kBf16, bool kVec>
+__device__ __forceinline__ uint4 load8(const typename Half<kBf16>::type* x) {
+    if constexpr (kVec) return __ldg(reinterpret_cast<const uint4*>(x));
+    else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint16_t* u = reinterpret_cast<const uint16_t*>(x) + 2 * i;
+            w[i] = u[0] | ((uint32_t)u[1] << 16);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.0f;  // NaN and infinities do not count
+}
+template <bool kBf16>
+__device__ __forceinline__ float largest8(uint4 w) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = Half<kBf16>::unpack((&w.x)[i]);
+        m = fmaxf(m, fmaxf(finite_abs(f.x), finite_abs(f.y)));
+    }
+    return m;
+}
+// round(x * inverse) for finite x, 0 for NaN, +-127 for the infinities (whatever the scale).
+__device__ __forceinline__ int quantise(float x, float inverse) {
+    const float y = fabsf(x) <= 3.402823466e38f ? rintf(__fmul_rn(x, inverse)) : (x > 0.0f ? 127.0f : (x < 0.0f ? -127.0f : 0.0f));
+    return (int)fminf(fmaxf(y, -127.0f), 127.0f);
+}
+template <bool kBf16>
+__device__ __forceinline__ uint2 quantise8(uint4 w, float inverse) {
+    uint32_t q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float2 a = Half<kBf16>::unpack((&w.x)[2 * i]), b = Half<kBf16>::unpack((&w.x)[2 * i + 1]);
+        q[i] = (uint32_t)(uint8_t)quantise(a.x, inverse) | (uint32_t)(uint8_t)quantise(a.y, inverse) << 8 |
+               (uint32_t)(uint8_t)quantise(b.x, inverse) << 16 | (uint32_t)(uint8_t)quantise(b.y, inverse) << 24;
+    }
+    return make_uint2(q[0], q[1]);
+}
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
+    uint32_t q = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        q |= (uint32_t)(uint8_t)(int)rintf(__fmul_rn((float)(int8_t)(w >> (8 * i)), ratio)) << (8 * i);
+    return q;
+}
+
+// grid: (windows of tokens, heads, keys / values)
+template <bool kBf16, bool kVec>
+__global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
+    using T16 = typename Half<kBf16>::type;
+    __shared__ float warp_max[kThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, head = blockIdx.y;
+    const bool values = blockIdx.z != 0;
+    const T16* x = reinterpret_cast<const T16*>(values ? p.v : p.k);
+    const int64_t ldx = values ? p.ldv : p.ldk;
+    int8_t* cache = values ? p.v_cache : p.k_cache;
+    float* scales = values ? p.v_scale : p.k_scale;
+    const int dim = 1 << p.dim_log2, page_size = 1 << p.page_log2, per_row_log2 = p.dim_log2 - 3;
+    auto page_of = [&](int64_t t) -> int64_t {
+        const int64_t s = p.slots[t];
+        return s < 0 || s >= p.n_slots ? -1 : s >> p.page_log2;
+    };
+    const int64_t t_end = min(p.T, (int64_t)(blockIdx.x + 1) * p.window);
+    for (int64_t t0 = (int64_t)blockIdx.x * p.window; t0 < t_end; ++t0) {
+        const int64_t page = page_of(t0);
+        if (page < 0 || (t0 > 0 && page_of(t0 - 1) == page)) continue;  // not the first token of a run
+        const int place = (int)(p.slots[t0] & (page_size - 1));
+        // the run: the tokens of the same page that follow
+        int n = 1;
+        while (true) {
+            const int64_t t = t0 + n + lane;
+            const unsigned ok = __ballot_sync(~0u, t < p.T && page_of(t) == page);
+            const int more = ok == ~0u ? 32 : __ffs(~ok) - 1;
+            n += more;
+            if (more < 32) break;
+        }
+        const T16* row0 = x + t0 * ldx + (int64_t)head * dim;
+        const int pieces = n << per_row_log2;
+        auto piece = [&](int i) { return row0 + (int64_t)(i >> per_row_log2) * ldx + ((i & ((1 << per_row_log2) - 1)) << 3); };
+        uint4 held[kHeld];
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const int i = tid + j * kThreads;
+            if (i < pieces) held[j] = load8<kBf16, kVec>(piece(i));
+        }
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (tid + j * kThreads < pieces) m = fmaxf(m, largest8<kBf16>(held[j]));
+        for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) m = fmaxf(m, largest8<kBf16>(load8<kBf16, kVec>(piece(i))));
+#pragma unroll
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+        __syncthreads();  // the run before has read warp_max and its scale
+        if (lane == 0) warp_max[tid >> 5] = m;
+        float* scale = scales + page * p.heads + head;
+        const float before = place > 0 ? *scale : 0.0f;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, warp_max[w]);
+        const float wanted = m < 7.888609052e-31f ? 0.0f : __fmul_rn(m, 1.0f / 127.0f);  // 2^-100: its reciprocal stays finite
+        const float after = fmaxf(before, wanted);
+        const float inverse = after > 0.0f ? 1.0f / after : 0.0f;
+        int8_t* block = cache + ((page * p.heads + head) << (p.page_log2 + p.dim_log2));
+        if (after > before && place > 0) {
+            const float ratio = before / after;
+            uint32_t* old = reinterpret_cast<uint32_t*>(block);
+            for (int i = tid; i < place << (p.dim_log2 - 2); i += kThreads) old[i] = rescale4(old[i], ratio);
+        }
+        auto out = [&](int i) {
+            const int at = (int)(p.slots[t0 + (i >> per_row_log2)] & (page_size - 1));
+            return reinterpret_cast<uint2*>(block + (at << p.dim_log2)) + (i & ((1 << per_row_log2) - 1));
+        };
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (tid + j * kThreads < pieces) *out(tid + j * kThreads) = quantise8<kBf16>(held[j], inverse);
+        for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) *out(i) = quantise8<kBf16>(load8<kBf16, kVec>(piece(i)), inverse);
+        __syncthreads();  // every thread has read the old scale
+        if (tid == 0) *scale = after;
+    }
+}
+
+}  // namespace
+
+// Checks shared by the operators that take the cache.
+awe_status_t check_kv_cache(const awe_kv_cache* c) {
+    if (!c || !c->k_dev || !c->v_dev || !c->k_scale_dev || !c->v_scale_dev || c->n_pages <= 0 || c->n_heads <= 0)
+        return AWE_ERR_INVALID_ARG;
+    if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return AWE_ERR_UNSUPPORTED;
+    if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return AWE_ERR_UNSUPPORTED;
+    if (c->n_pages > INT32_MAX || c->n_heads > 65535) return AWE_ERR_UNSUPPORTED;
+    if ((uintptr_t)c->k_dev % 16 || (uintptr_t)c->v_dev % 16 || (uintptr_t)c->k_scale_dev % 4 || (uintptr_t)c->v_scale_dev % 4)
+        return AWE_ERR_ALIGNMENT;
+    return AWE_OK;
+}
+
+}  // namespace awe
+
+using namespace awe;
+
+extern "C" awe_status_t awe_kv_write(awe_handle_t h, const awe_kv_cache* cache, const void* k_dev, const void* v_dev,
+                                     awe_float_t type, int64_t T, int64_t ldk, int64_t ldv, const int64_t* slots_dev,
+                                     void* stream) {
+    if (!h || T < 0) return AWE_ERR_INVALID_ARG;
+    const awe_status_t s = check_kv_cache(cache);
+    if (s != AWE_OK) return s;
+    if ((int)type < AWE_F16 || (int)type > AWE_F32) return AWE_ERR_INVALID_ARG;
+    if (!is_half_type(type)) return AWE_ERR_UNSUPPORTED;
+    if (T == 0) return AWE_OK;
+    const int64_t width = cache->n_heads * cache->head_dim;
+    if (!k_dev || !v_dev || !slots_dev || T > INT32_MAX || (T > 1 && (ldk < width || ldv < width))) return AWE_ERR_INVALID_ARG;
+    if ((uintptr_t)k_dev % 2 || (uintptr_t)v_dev % 2 || (uintptr_t)slots_dev % 8) return AWE_ERR_ALIGNMENT;
+    WriteParams p = {k_dev, v_dev, cache->k_dev, cache->v_dev, cache->k_scale_dev, cache->v_scale_dev, slots_dev, ldk, ldv, T,
+                     cache->n_pages * cache->page_size, (int)cache->n_heads, 4, 6, 1};
+    while ((1 << p.page_log2) < cache->page_size) ++p.page_log2;
+    while ((1 << p.dim_log2) < cache->head_dim) ++p.dim_log2;
+    // A block looks at `window` tokens: one where that leaves few blocks (each token may start a run), up to a
+    // page's where there are many (then nearly every block finds one run).
+    while (p.window < cache->page_size && T / (2 * p.window) * cache->n_heads * 2 >= 16 * h->sm_count) p.window *= 2;
+    const dim3 grid((unsigned)((T + p.window - 1) / p.window), (unsigned)cache->n_heads, 2);
+    const bool vec = (uintptr_t)k_dev % 16 == 0 && (uintptr_t)v_dev % 16 == 0 && ldk % 8 == 0 && ldv % 8 == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (type == AWE_BF16) {
+        if (vec) kv_write_kernel<true, true><<<grid, kThreads, 0, st>>>(p);
+        else kv_write_kernel<true, false><<<grid, kThreads, 0, st>>>(p);
+    } else {
+        if (vec) kv_write_kernel<false, true><<<grid, kThreads, 0, st>>>(p);
+        else kv_write_kernel<false, false><<<grid, kThreads, 0, st>>>(p);
+    }
+    if (cudaGetLastError() != cudaSuccess) return AWE_ERR_CUDA;
+    h->launches += 1;
+    return AWE_OK;
+}
