@@ -66,8 +66,21 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int b) {
     return r;
 }
 
-// Range of global steps of block i.
-__device__ __forceinline__ int64_t block_begin(int64_t total, int i, int blocks) { return total * i / blocks; }
+// The steps are dealt out to the blocks in order, as evenly as whole numbers go: the first `extra` blocks take one more.
+struct Deal {
+    int64_t each;
+    int extra, blocks;
+    __device__ __forceinline__ Deal(int64_t total, int most_blocks) {
+        blocks = (int)min((int64_t)most_blocks, max(total, (int64_t)1));
+        each = total / blocks;
+        extra = (int)(total - each * blocks);
+    }
+    __device__ __forceinline__ int64_t begin(int i) const { return each * i + min(i, extra); }
+    __device__ __forceinline__ int block_of(int64_t step) const {
+        const int64_t cut = (each + 1) * extra;
+        return step < cut ? (int)(step / (each + 1)) : extra + (int)((step - cut) / each);
+    }
+};
 
 template <int kD, int kNT>
 struct Config {
@@ -110,7 +123,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     // ---- which steps are mine: exclusive sum of units x steps over the requests
     int64_t total = 0;
     for (int pass = 0; pass < 2; ++pass) {
-        const int64_t mine = pass ? block_begin(total, blockIdx.x, p.blocks) : 0;
+        const int64_t mine = pass ? Deal(total, p.blocks).begin(blockIdx.x) : 0;
         int64_t sum = 0;
         for (int b0 = 0; b0 < p.B; b0 += kThreads) {
             const int b = b0 + tid;
@@ -147,8 +160,9 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     }
     if (blockIdx.x == 0 && tid == 0) p.unit_steps[p.B] = total;
     __syncthreads();
-    const int64_t begin = block_begin(total, blockIdx.x, p.blocks), end = block_begin(total, blockIdx.x + 1, p.blocks);
-    if (begin >= end) return;
+    const Deal deal(total, p.blocks);
+    if ((int)blockIdx.x >= deal.blocks || total == 0) return;
+    const int64_t begin = deal.begin(blockIdx.x), end = deal.begin(blockIdx.x + 1);
 
     int b = found_b;
     int64_t at = found_at;
@@ -229,6 +243,16 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             }
         }
 
+        // tokens that every row of the unit sees
+        int all_lo = see_lo[0][0], all_hi = see_hi[0][0];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (8 * nt + 2 * t + j < n_rows) all_lo = max(all_lo, see_lo[nt][j]), all_hi = min(all_hi, see_hi[nt][j]);
+        all_lo = __reduce_max_sync(~0u, all_lo);
+        all_hi = __reduce_min_sync(~0u, all_hi);
+
         float o[kSteps16][kNT][4];
         float m_ref[kNT][2], sum[kNT][2], sum_lse[kNT][2];
 #pragma unroll
@@ -289,8 +313,6 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             // scores of 16 tokens (rows g, g + 8) and the query rows (columns 2t, 2t + 1)
             float s[kNT][4];
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
-#pragma unroll
             for (int c = 0; c < kD / 64; ++c) {
                 const int piece = kD == 64 ? t : 8 * (c >> 1) + 2 * t + (c & 1);
                 const uint4 a = lds128(ks_at + piece_at<kD>(g, piece)), b8 = lds128(ks_at + piece_at<kD>(g + 8, piece));
@@ -300,22 +322,33 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                     const uint32_t f[4] = {bytes_to_half2(x, 0x4140), bytes_to_half2(y, 0x4140), bytes_to_half2(x, 0x4342),
                                            bytes_to_half2(y, 0x4342)};
 #pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt) mma_16816<false>(s[nt], f, qf[nt][4 * c + w][0], qf[nt][4 * c + w][1]);
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        if (c == 0 && w == 0) mma_16816_zero<false>(s[nt], f, qf[nt][0][0], qf[nt][0][1]);
+                        else mma_16816<false>(s[nt], f, qf[nt][4 * c + w][0], qf[nt][4 * c + w][1]);
+                    }
                 }
             }
 
-            const int tok = tok0 + i * kStepTokens + g;
+            const int tile = tok0 + i * kStepTokens, tok = tile + g;
             uint32_t pf[kNT][2];
             bool grows = false;
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt)
+            for (int nt = 0; nt < kNT; ++nt) {
+                const float c0 = ks * cq[nt][0], c1 = ks * cq[nt][1];
+                s[nt][0] *= c0, s[nt][1] *= c1, s[nt][2] *= c0, s[nt][3] *= c1;
+            }
+            if (tile < all_lo || tile + 16 > all_hi) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int at_tok = tok + (j >> 1) * 8;
-                    const float x = s[nt][j] * (ks * cq[nt][j & 1]);
-                    s[nt][j] = at_tok >= see_lo[nt][j & 1] && at_tok < see_hi[nt][j & 1] ? x : -INFINITY;
-                    grows |= s[nt][j] > m_ref[nt][j & 1] + 8.0f;
-                }
+                for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at_tok = tok + (j >> 1) * 8;
+                        if (at_tok < see_lo[nt][j & 1] || at_tok >= see_hi[nt][j & 1]) s[nt][j] = -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+                grows |= fmaxf(s[nt][0], s[nt][2]) > m_ref[nt][0] + 8.0f || fmaxf(s[nt][1], s[nt][3]) > m_ref[nt][1] + 8.0f;
             // The reference only has to stay within 2^8 of the maximum for FP16 to hold exp2(s - m_ref); it moves rarely.
             if (__any_sync(~0u, grows)) {
 #pragma unroll
@@ -381,8 +414,8 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                         const int tile = (c * kWords + w) * 2 + pair;
 #pragma unroll
                         for (int nt = 0; nt < kNT; ++nt) {
-                            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                            mma_16816<false>(d, f, pf[nt][0], pf[nt][1]);
+                            float d[4];
+                            mma_16816_zero<false>(d, f, pf[nt][0], pf[nt][1]);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) o[tile][nt][j] = fmaf(d[j], vs, o[tile][nt][j]);
                         }
@@ -477,20 +510,15 @@ __global__ void __launch_bounds__(kThreads) kv_attention_join_kernel(const AttnP
     const int row_all = (token - r.q0) * p.group + qh % p.group, row = row_all % kRows;
     const int unit = row_all / kRows * p.heads + qh / p.group;
     const int64_t w0 = p.unit_steps[b] + (int64_t)unit * r.steps, w1 = w0 + r.steps;
-    // first block that holds a step of the unit
-    int first = (int)(w0 * p.blocks / total);
-    while (first > 0 && block_begin(total, first, p.blocks) > w0) --first;
-    while (block_begin(total, first + 1, p.blocks) <= w0) ++first;
-    if (block_begin(total, first + 1, p.blocks) >= w1) return;  // one block had all of it
+    const Deal deal(total, p.blocks);
+    const int first = deal.block_of(w0), last = deal.block_of(w1 - 1);
+    if (first == last) return;  // one block had all of it
     float m = -INFINITY, sum = 0.0f, sum_lse = 0.0f;
     float4 x[kD / 128 + (kD < 128)];
 #pragma unroll
     for (auto& v : x) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = first; i < p.blocks; ++i) {
-        const int64_t lo = block_begin(total, i, p.blocks);
-        if (lo >= w1) break;
-        if (block_begin(total, i + 1, p.blocks) == lo) continue;  // a block without steps
-        const int64_t part = ((int64_t)2 * i + (lo <= w0)) * kRows + row;
+    for (int i = first; i <= last; ++i) {
+        const int64_t part = ((int64_t)2 * i + (i == first)) * kRows + row;  // the first part is the one that begins the unit
         const float4 st = p.part_stat[part];
         const float m_new = fmaxf(m, st.x);
         const float a = m == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_approx(m - m_new);

@@ -41,17 +41,20 @@ __device__ __forceinline__ uint4 load8(const typename Half<kBf16>::type* x) {
     }
 }
 
-__device__ __forceinline__ float finite_abs(float x) {
-    const float a = fabsf(x);
-    return a <= 3.402823466e38f ? a : 0.0f;  // NaN and infinities do not count
+// Two unsigned maxima of 16-bit magnitudes: the patterns of finite values order like the values, and a maximum of
+// kInfinity or more says that an infinity or a NaN is among them.
+__device__ __forceinline__ uint32_t largest8(uint4 w, uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, (&w.x)[i] & 0x7FFF7FFFu);
+    return m;
 }
 template <bool kBf16>
-__device__ __forceinline__ float largest8(uint4 w) {
-    float m = 0.0f;
+__device__ __forceinline__ uint32_t largest_finite8(uint4 w, uint32_t m) {
+    constexpr uint32_t kInfinity = kBf16 ? 0x7F80u : 0x7C00u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = Half<kBf16>::unpack((&w.x)[i]);
-        m = fmaxf(m, fmaxf(finite_abs(f.x), finite_abs(f.y)));
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t x = ((&w.x)[i >> 1] >> (16 * (i & 1))) & 0x7FFFu;
+        if (x < kInfinity) m = max(m, x);
     }
     return m;
 }
@@ -61,13 +64,26 @@ __device__ __forceinline__ int quantise(float x, float inverse) {
     return (int)fminf(fmaxf(y, -127.0f), 127.0f);
 }
 template <bool kBf16>
-__device__ __forceinline__ uint2 quantise8(uint4 w, float inverse) {
+__device__ __forceinline__ uint2 quantise8_any(uint4 w, float inverse) {
     uint32_t q[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const float2 a = Half<kBf16>::unpack((&w.x)[2 * i]), b = Half<kBf16>::unpack((&w.x)[2 * i + 1]);
         q[i] = (uint32_t)(uint8_t)quantise(a.x, inverse) | (uint32_t)(uint8_t)quantise(a.y, inverse) << 8 |
                (uint32_t)(uint8_t)quantise(b.x, inverse) << 16 | (uint32_t)(uint8_t)quantise(b.y, inverse) << 24;
+    }
+    return make_uint2(q[0], q[1]);
+}
+// The same where every value is finite, so that |x * inverse| < 127.5: adding 1.5 * 2^23 rounds to an integer, ties to
+// even, whose two's complement is the low byte of the sum.
+template <bool kBf16>
+__device__ __forceinline__ uint2 quantise8(uint4 w, float inverse) {
+    uint32_t q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float2 a = Half<kBf16>::unpack((&w.x)[2 * i]), b = Half<kBf16>::unpack((&w.x)[2 * i + 1]);
+        auto round = [&](float x) { return __float_as_uint(__fadd_rn(__fmul_rn(x, inverse), 12582912.0f)); };
+        q[i] = __byte_perm(__byte_perm(round(a.x), round(a.y), 0x0040), __byte_perm(round(b.x), round(b.y), 0x0040), 0x5410);
     }
     return make_uint2(q[0], q[1]);
 }
@@ -83,7 +99,8 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
 template <bool kBf16, bool kVec>
 __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
     using T16 = typename Half<kBf16>::type;
-    __shared__ float warp_max[kThreads / 32];
+    __shared__ uint32_t warp_max[kThreads / 32];
+    constexpr uint32_t kInfinity = kBf16 ? 0x7F80u : 0x7C00u;
     const int tid = threadIdx.x, lane = tid & 31, head = blockIdx.y;
     const bool values = blockIdx.z != 0;
     const T16* x = reinterpret_cast<const T16*>(values ? p.v : p.k);
@@ -95,10 +112,17 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
         const int64_t s = p.slots[t];
         return s < 0 || s >= p.n_slots ? -1 : s >> p.page_log2;
     };
-    const int64_t t_end = min(p.T, (int64_t)(blockIdx.x + 1) * p.window);
-    for (int64_t t0 = (int64_t)blockIdx.x * p.window; t0 < t_end; ++t0) {
+    const int64_t t_begin = (int64_t)blockIdx.x * p.window, t_end = min(p.T, t_begin + p.window);
+    unsigned begins = 0;  // of the 32 tokens from t32, those that begin a run (every warp finds out for itself)
+    for (int64_t t32 = t_begin, t0 = 0; t32 < t_end || begins; begins &= begins - 1) {
+        while (!begins && t32 < t_end) {
+            const int64_t t = t32 + lane, mine = t < t_end ? page_of(t) : -1;
+            begins = __ballot_sync(~0u, mine >= 0 && (t == 0 || page_of(t - 1) != mine));
+            t32 += 32;
+        }
+        if (!begins) break;
+        t0 = t32 - 32 + __ffs(begins) - 1;
         const int64_t page = page_of(t0);
-        if (page < 0 || (t0 > 0 && page_of(t0 - 1) == page)) continue;  // not the first token of a run
         const int place = (int)(p.slots[t0] & (page_size - 1));
         // the run: the tokens of the same page that follow
         int n = 1;
@@ -113,25 +137,36 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
         const int pieces = n << per_row_log2;
         auto piece = [&](int i) { return row0 + (int64_t)(i >> per_row_log2) * ldx + ((i & ((1 << per_row_log2) - 1)) << 3); };
         uint4 held[kHeld];
-        float m = 0.0f;
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) {
             const int i = tid + j * kThreads;
-            if (i < pieces) held[j] = load8<kBf16, kVec>(piece(i));
+            held[j] = i < pieces ? load8<kBf16, kVec>(piece(i)) : make_uint4(0, 0, 0, 0);
         }
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-            if (tid + j * kThreads < pieces) m = fmaxf(m, largest8<kBf16>(held[j]));
-        for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) m = fmaxf(m, largest8<kBf16>(load8<kBf16, kVec>(piece(i))));
-#pragma unroll
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-        __syncthreads();  // the run before has read warp_max and its scale
-        if (lane == 0) warp_max[tid >> 5] = m;
         float* scale = scales + page * p.heads + head;
         const float before = place > 0 ? *scale : 0.0f;
-        __syncthreads();
+        auto block_max = [&](uint32_t m) {
+            m = __reduce_max_sync(~0u, max(m & 0xFFFFu, m >> 16));
+            __syncthreads();  // whoever read warp_max before has it
+            if (lane == 0) warp_max[tid >> 5] = m;
+            __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, warp_max[w]);
+            for (int w = 0; w < kThreads / 32; ++w) m = max(m, warp_max[w]);
+            return m;
+        };
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) top = largest8(held[j], top);
+        for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) top = largest8(load8<kBf16, kVec>(piece(i)), top);
+        top = block_max(top);
+        const bool finite = top < kInfinity;
+        if (!finite) {
+            top = 0;
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) top = largest_finite8<kBf16>(held[j], top);
+            for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) top = largest_finite8<kBf16>(load8<kBf16, kVec>(piece(i)), top);
+            top = block_max(top);
+        }
+        const float m = Half<kBf16>::unpack(top).x;
         const float wanted = m < 7.888609052e-31f ? 0.0f : __fmul_rn(m, 1.0f / 127.0f);  // 2^-100: its reciprocal stays finite
         const float after = fmaxf(before, wanted);
         const float inverse = after > 0.0f ? 1.0f / after : 0.0f;
@@ -145,10 +180,14 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
             const int at = (int)(p.slots[t0 + (i >> per_row_log2)] & (page_size - 1));
             return reinterpret_cast<uint2*>(block + (at << p.dim_log2)) + (i & ((1 << per_row_log2) - 1));
         };
+        auto store = [&](auto quantise_piece) {
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-            if (tid + j * kThreads < pieces) *out(tid + j * kThreads) = quantise8<kBf16>(held[j], inverse);
-        for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) *out(i) = quantise8<kBf16>(load8<kBf16, kVec>(piece(i)), inverse);
+            for (int j = 0; j < kHeld; ++j)
+                if (tid + j * kThreads < pieces) *out(tid + j * kThreads) = quantise_piece(held[j]);
+            for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) *out(i) = quantise_piece(load8<kBf16, kVec>(piece(i)));
+        };
+        if (finite) store([&](uint4 w) { return quantise8<kBf16>(w, inverse); });
+        else store([&](uint4 w) { return quantise8_any<kBf16>(w, inverse); });
         __syncthreads();  // every thread has read the old scale
         if (tid == 0) *scale = after;
     }

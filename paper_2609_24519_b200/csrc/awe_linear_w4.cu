@@ -8,10 +8,11 @@
 // the bound.
 //
 // A block takes 64 rows of the weight and a part of K; up to 8 blocks along K form a cluster and add their sums
-// through each other's shared memory in a fixed order.  A warp's 16 rows pass through a ring of cp.async stages of
-// 256 k.  Thread (g, t) of a warp reads 8 consecutive k of its rows as one word; which k takes which place in the
-// instruction does not matter as long as x is placed alike, so codes are used in the order in which they unpack:
-// (0,4), (1,5), (2,6), (3,7).
+// through each other's shared memory in a fixed order.  Each of its four warps has 16 rows and a ring of its own: a
+// stage is 256 k of the codes (cp.async, 16 bytes a piece), and the stage that begins a slab (1,024 to 4,096 k) brings the slab's
+// scales and zero points along, so that a warp waits for nobody but itself within a slab.  Thread (g, t) of a warp reads
+// 8 consecutive k of its rows as one word; which k takes which place in the instruction does not matter as long as x
+// is placed alike, so codes are used in the order in which they unpack: (0,4), (1,5), (2,6), (3,7).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -26,36 +27,32 @@ using namespace serve;
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kRowsN = 16 * kWarps;      // rows of the weight per block
-constexpr int kStageK = 256;             // k per stage
-constexpr int kPitch = kStageK / 2 + 16; // bytes per row and stage: the last 16 hold what an unaligned row spills over, and
-                                         // make 8 rows x 4 words hit all banks
-constexpr int kGroupsMax = kStageK / 32;
-constexpr int kStages = 4;
+constexpr int kWarpRows = 16;
+constexpr int kRowsN = kWarpRows * kWarps;  // rows of the weight per block
+constexpr int kStageK = 256;                // k per stage
+constexpr int kPitch = kStageK / 2 + 16;    // bytes per row and stage: the last 16 hold what an unaligned row spills over, and
+                                            // make 8 rows x 4 words hit all banks
+constexpr int kStageBytes = kWarpRows * kPitch;
+constexpr int kStages = 3;
+constexpr int kZeroBytes = kStageK * 2 + 128;  // read in the place of rows of x that do not exist
 constexpr int kMaxCluster = 8;
-constexpr int kSlabK = 2048;             // k of x held at a time
+constexpr int kSlabK = 1024;     // k whose x, scales and zero points are held at a time: this or, for few rows of x,
+constexpr int kSlabKMost = 4096; // two or four times as many
+constexpr int kSumPitch = kRowsN + 4;        // floats
 
 struct LinearParams {
     const uint8_t* codes;
-    const void* scale;
-    const int8_t* zero;
+    const uint8_t* scale;
+    const uint8_t* zero;
     const void* x;
     void* y;
-    int64_t row_bytes, ldx, ldy, codes_bytes;
+    int64_t row_bytes, ldx, ldy;
     int M, N, K, group_log2, groups, k_per_block;
     int scale_bf16, y_f32, x_vec;
-};
-
-template <int kMT>
-struct Config {
-    static constexpr int kRowsM = 8 * kMT;
-    static constexpr int kSlabPitch = kSlabK * 2 + 64;  // bytes
-    static constexpr int kStageBytes = kRowsN * kPitch;
-    static constexpr int kScaleBytes = kRowsN * (kGroupsMax + 1) * 8;  // (scale, zero constant) of a stage
-    static constexpr int kXBytes = kRowsM * kSlabPitch;
-    static constexpr int kRingBytes = kStages * (kStageBytes + kScaleBytes);
-    static constexpr int kSmemBytes = kXBytes + kRingBytes;
-    static constexpr int kSumBytes = kRowsM * (kRowsN + 4) * 4;  // in the place of x
+    int scale_pitch, zero_pitch;  // bytes of a row's scales and zero points of a slab, with room for what an unaligned row spills over
+    int ring_at, slab_at;         // byte offsets in shared memory: x first
+    int slabs;                    // 2 where a block has more than one
+    int slab_stages;              // a power of two
 };
 
 // Nibbles i and i + 4 of a word as a pair of 16-bit floats, less `offset` = pattern bias + 8 + zero.
@@ -86,79 +83,113 @@ __device__ __forceinline__ void unpack_word(uint32_t w, uint32_t offset, uint32_
     }
 }
 
-template <int kMT, bool kBf16, bool kAligned>
+// The first 16 bytes of an unaligned row whose 16-byte piece begins in front of the array: bytes from `first` on.
+__device__ __noinline__ void copy_first_piece(uint32_t dst, const uint8_t* piece, int first, int bytes) {
+    for (int e = 0; e < 16; ++e)
+        asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + e), "r"((uint32_t)(e >= first && e < bytes ? piece[e] : 0)) : "memory");
+}
+// Piece c of the copy of [src, src + n) to dst + (src mod 16), in pieces of 16 bytes that start on 16-byte boundaries.
+// What lies in front of `base` is not ours to read.
+__device__ __forceinline__ void copy_piece(uint32_t dst, const uint8_t* src, int n, int c, const uint8_t* base) {
+    const int shift = (int)((uintptr_t)src & 15);
+    const uint8_t* piece = src - shift + 16 * c;
+    const int bytes = min(16, max(0, n + shift - 16 * c));
+    if (piece >= base) cp_async16(dst + 16 * c, bytes ? piece : src - shift + 16, bytes);
+    else copy_first_piece(dst + 16 * c, piece, (int)(base - piece), bytes);
+}
+// 8 consecutive 16-bit values of x at any 2-byte alignment.
+__device__ __forceinline__ uint4 load_x8(const uint16_t* src, bool vec, int n) {
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (n >= 8) {
+        if (vec) return __ldg(reinterpret_cast<const uint4*>(src));
+        if (((uintptr_t)src & 2) == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __ldg(reinterpret_cast<const uint32_t*>(src) + e);
+        } else {  // the first and the last half word by themselves
+            uint32_t v[5];
+            v[0] = (uint32_t)__ldg(src) << 16;
+#pragma unroll
+            for (int e = 0; e < 3; ++e) v[e + 1] = __ldg(reinterpret_cast<const uint32_t*>(src + 1) + e);
+            v[4] = __ldg(src + 7);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = __funnelshift_r(v[e], v[e + 1], 16);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) w[e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int kMT, int kGroupSteps, bool kBf16, bool kAligned>
 __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams p) {
     namespace cg = cooperative_groups;
-    using C = Config<kMT>;
-    using T16 = typename Half<kBf16>::type;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * kRowsN, m0 = blockIdx.z * C::kRowsM, k0 = blockIdx.y * p.k_per_block;
+    const int n0 = blockIdx.x * kRowsN, m0 = blockIdx.z * 8 * kMT, k0 = blockIdx.y * p.k_per_block;
     const int k1 = min(p.K, k0 + p.k_per_block), n_stages = k1 > k0 ? (k1 - k0 + kStageK - 1) / kStageK : 0;
-    const int rows_m = min(C::kRowsM, p.M - m0);
-    const uint32_t smem_at = (uint32_t)__cvta_generic_to_shared(smem), ring = smem_at + C::kXBytes;
-    uint8_t* scales = smem + C::kXBytes + kStages * C::kStageBytes;
+    const int rows_m = min(8 * kMT, p.M - m0), slab_k = p.slab_stages * kStageK, x_pitch = slab_k * 2 + 64;
+    // Rows of the weight below the last one are computed from the last one and not written.
+    const int n_warp = n0 + warp * kWarpRows;
+    auto row_of = [&](int row) { return (int64_t)min(n_warp + row, p.N - 1); };
+    const uint32_t smem_at = (uint32_t)__cvta_generic_to_shared(smem), ring = smem_at + p.ring_at + warp * kStages * kStageBytes;
+    const int slab_bytes = kWarpRows * (p.scale_pitch + p.zero_pitch);
+    const uint32_t slabs = smem_at + p.slab_at + warp * p.slabs * slab_bytes;
+    auto slab_of = [&](int i) { return slabs + (p.slabs == 2 && (i & p.slab_stages) ? slab_bytes : 0); };
 
-    // 16-byte pieces of a stage: 8 per row, and a ninth where rows start between 16-byte boundaries
-    constexpr int kPieces = kAligned ? 8 : 9;
+    // aligned rows: this lane copies piece lane % 8 of the rows lane / 8 + 4 j
+    const uint8_t* codes[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) codes[j] = p.codes + row_of((lane >> 3) + 4 * j) * p.row_bytes + (k0 >> 1) + 16 * (lane & 7);
+    const uint32_t codes_dst = ring + (lane >> 3) * kPitch + 16 * (lane & 7);
     auto fetch = [&](int i) {
         if (i < n_stages) {
-            const int kb = (k0 + i * kStageK) >> 1, k_bytes = (min(k1 - k0 - i * kStageK, kStageK) + 1) >> 1;
-            const uint32_t stage = ring + (i % kStages) * C::kStageBytes;
-            for (int j = tid; j < kRowsN * kPieces; j += kThreads) {
-                const int row = j / kPieces, c = j % kPieces;
-                const bool live = n0 + row < p.N;
-                const uint8_t* src = p.codes + (int64_t)(n0 + (live ? row : 0)) * p.row_bytes + kb;
-                const int shift = kAligned ? 0 : (int)((uintptr_t)src & 15);
-                const uint8_t* piece = src - shift + 16 * c;
-                const int bytes = live ? min(16, max(0, k_bytes + shift - 16 * c)) : 0;
-                const uint32_t dst = stage + row * kPitch + 16 * c;
-                if (kAligned || piece >= p.codes) cp_async16(dst, bytes ? piece : p.codes - ((uintptr_t)p.codes & 15), bytes);
-                else  // the bytes in front of the matrix are not ours to read
-                    for (int e = 0; e < 16; ++e)
-                        asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + e), "r"((uint32_t)(piece + e >= p.codes && e < bytes ? piece[e] : 0)) : "memory");
+            const int k = k0 + i * kStageK, slot = i % kStages;
+            if constexpr (kAligned) {
+                const int bytes = k + kStageK <= k1 ? 16 : min(16, max(0, ((k1 - k + 1) >> 1) - 16 * (lane & 7)));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) cp_async16(codes_dst + slot * kStageBytes + 4 * j * kPitch, codes[j] + (bytes ? i * (kStageK / 2) : 0), bytes);
+            } else {  // a ninth piece per row; half a warp per row
+                const int k_bytes = (min(k1 - k, kStageK) + 1) >> 1, c = lane & 15;
+#pragma unroll 4
+                for (int row = lane >> 4; row < kWarpRows; row += 2)
+                    if (c < 9) copy_piece(ring + slot * kStageBytes + row * kPitch, p.codes + row_of(row) * p.row_bytes + (k >> 1), k_bytes, c, p.codes);
+            }
+            if ((i & (p.slab_stages - 1)) == 0) {  // two lanes per row
+                const uint32_t slab = slab_of(i);
+                const int first = k >> p.group_log2, n = ((min(k1, k + slab_k) - 1) >> p.group_log2) + 1 - first, row = lane >> 1;
+                const int64_t at = row_of(row) * p.groups + first;
+#pragma unroll 1
+                for (int c = lane & 1; 16 * c < p.scale_pitch; c += 2) copy_piece(slab + row * p.scale_pitch, p.scale + 2 * at, 2 * n, c, p.scale);
+#pragma unroll 1
+                for (int c = lane & 1; 16 * c < p.zero_pitch; c += 2)
+                    copy_piece(slab + kWarpRows * p.scale_pitch + row * p.zero_pitch, p.zero + at, n, c, p.zero);
             }
         }
         cp_async_commit();
     };
-    // scale and zero constants of a stage: element (row, group of the stage)
-    const int per_stage = p.group_log2 >= 8 ? 1 : kStageK >> p.group_log2;
-    auto put_scales = [&](int i) {
-        if (i >= n_stages) return;
-        const int first = (k0 + i * kStageK) >> p.group_log2;
-        for (int j = tid; j < kRowsN * per_stage; j += kThreads) {
-            const int row = j / per_stage, gi = j % per_stage;
-            float s = 0.0f;
-            int z = 0;
-            if (n0 + row < p.N && first + gi < p.groups) {
-                const int64_t at = (int64_t)(n0 + row) * p.groups + first + gi;
-                s = p.scale_bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p.scale)[at]) : __half2float(reinterpret_cast<const __half*>(p.scale)[at]);
-                if (p.zero) z = (int)((uint32_t)(uint8_t)p.zero[at] << 28) >> 28;
-            }
-            const float bias = kBf16 ? 136.0f : 1032.0f;
-            const uint32_t off = kBf16 ? Half<true>::pack(bias + z, bias + z) : Half<false>::pack(bias + z, 0.0f - (72.0f + z));
-            *reinterpret_cast<uint2*>(scales + (i % kStages) * C::kScaleBytes + (row * (kGroupsMax + 1) + gi) * 8) = make_uint2(__float_as_uint(s), off);
-        }
-    };
-    // x for [k0 + at, + kSlabK), zeros behind the block's part of K and below the last row
+    // x for [k0 + at, + slab_k), zeros behind the block's part of K: the warps take pieces of 1,024 k of a row in turn
     auto load_x = [&](int at) {
-        const int n_k = min(kSlabK, k1 - k0 - at), n_round = (n_k + kStageK - 1) / kStageK * kStageK;
-        for (int j = tid; j < rows_m * (n_round / 8); j += kThreads) {
-            const int row = j / (n_round / 8), k = j % (n_round / 8) * 8;
-            const T16* src = reinterpret_cast<const T16*>(p.x) + (int64_t)(m0 + row) * p.ldx + k0 + at + k;
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (p.x_vec && k + 8 <= n_k) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
-                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-            } else {
+        const int n_k = min(slab_k, k1 - k0 - at), n_round = (n_k + kStageK - 1) / kStageK * kStageK;
+        for (int j = warp; j < rows_m * (slab_k / kSlabK); j += kWarps) {
+            const int row = j / (slab_k / kSlabK), from = j % (slab_k / kSlabK) * kSlabK;
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(p.x) + (m0 + row) * p.ldx + k0 + at;
+            uint4 w[kSlabK / kStageK];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (k + e < n_k) w[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(src)[e] << (16 * (e & 1));
+            for (int u = 0; u < kSlabK / kStageK; ++u) {
+                const int k = from + 8 * lane + u * kStageK;
+                w[u] = load_x8(src + min(k, n_k), p.x_vec, n_k - k);
             }
-            // pairs (0,4), (1,5), (2,6), (3,7)
-            *reinterpret_cast<uint4*>(smem + row * C::kSlabPitch + k * 2) =
-                make_uint4(__byte_perm(w[0], w[2], 0x5410), __byte_perm(w[0], w[2], 0x7632), __byte_perm(w[1], w[3], 0x5410),
-                           __byte_perm(w[1], w[3], 0x7632));
+#pragma unroll
+            for (int u = 0; u < kSlabK / kStageK; ++u) {
+                const int k = from + 8 * lane + u * kStageK;
+                // pairs (0,4), (1,5), (2,6), (3,7)
+                if (k < n_round)
+                    *reinterpret_cast<uint4*>(smem + row * x_pitch + k * 2) =
+                        make_uint4(__byte_perm(w[u].x, w[u].z, 0x5410), __byte_perm(w[u].x, w[u].z, 0x7632),
+                                   __byte_perm(w[u].y, w[u].w, 0x5410), __byte_perm(w[u].y, w[u].w, 0x7632));
+            }
         }
     };
 
@@ -166,40 +197,62 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
 #pragma unroll
     for (int mt = 0; mt < kMT; ++mt) total[mt][0] = total[mt][1] = total[mt][2] = total[mt][3] = 0.0f;
 
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < kStages - 1; ++i) fetch(i);
+    for (int k = 16 * tid; k < kZeroBytes; k += 16 * kThreads) *reinterpret_cast<uint4*>(smem + p.ring_at - kZeroBytes + k) = make_uint4(0, 0, 0, 0);
+    uint32_t x_row[kMT], x_mask[kMT];
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) put_scales(i);
-    // where a row starts inside its first 16 bytes
-    const int row_a = 16 * warp + g, row_b = row_a + 8;
-    auto shift_of = [&](int row) { return kAligned ? 0 : (int)((uintptr_t)(p.codes + (int64_t)(n0 + min(row, p.N - 1 - n0)) * p.row_bytes + (k0 >> 1)) & 15); };
+    for (int mt = 0; mt < kMT; ++mt) {
+        const bool live = 8 * mt + g < rows_m;
+        x_row[mt] = smem_at + (live ? (8 * mt + g) * x_pitch : p.ring_at - kZeroBytes) + 16 * t;
+        x_mask[mt] = live ? ~0u : 0u;
+    }
+    // where rows g, g + 8 of the warp start inside their first 16 bytes of codes
+    const int row_a = g, row_b = g + 8;
+    auto shift_of = [&](int row) { return kAligned ? 0 : (int)((uintptr_t)(p.codes + row_of(row) * p.row_bytes + (k0 >> 1)) & 15); };
     const int shift_a = shift_of(row_a), shift_b = shift_of(row_b);
-    const int steps_per_scale = p.group_log2 >= 8 ? 8 : 1 << (p.group_log2 - 5);
+    const uint32_t word_a = ring + row_a * kPitch + (shift_a & ~3) + 4 * t, word_b = ring + row_b * kPitch + (shift_b & ~3) + 4 * t;
+    constexpr int kScales = kStageK / 32 / kGroupSteps;  // of a stage
+    uint32_t scale_a = 0, scale_b = 0, zero_a = 0, zero_b = 0;
 
     for (int i = 0; i < n_stages; ++i) {
-        if (i % (kSlabK / kStageK) == 0) {
-            __syncthreads();
+        if ((i & (p.slab_stages - 1)) == 0) {
+            if (i) __syncthreads();
             load_x(i * kStageK);
+            const uint32_t slab = slab_of(i), zeros = slab + kWarpRows * p.scale_pitch;
+            const int64_t at_a = row_of(row_a) * p.groups + ((k0 + i * kStageK) >> p.group_log2), at_b = row_of(row_b) * p.groups + ((k0 + i * kStageK) >> p.group_log2);
+            scale_a = slab + row_a * p.scale_pitch + ((uint32_t)(uintptr_t)(p.scale + 2 * at_a) & 15);
+            scale_b = slab + row_b * p.scale_pitch + ((uint32_t)(uintptr_t)(p.scale + 2 * at_b) & 15);
+            zero_a = zeros + row_a * p.zero_pitch + ((uint32_t)(uintptr_t)(p.zero + at_a) & 15);
+            zero_b = zeros + row_b * p.zero_pitch + ((uint32_t)(uintptr_t)(p.zero + at_b) & 15);
+            __syncthreads();
         }
         cp_async_wait<kStages - 2>();
-        __syncthreads();
+        __syncwarp();
         fetch(i + kStages - 1);
-        put_scales(i + kStages - 1);
-        const uint32_t stage = ring + (i % kStages) * C::kStageBytes;
-        const uint32_t at_a = stage + row_a * kPitch + (shift_a & ~3) + 4 * t, at_b = stage + row_b * kPitch + (shift_b & ~3) + 4 * t;
-        const uint32_t x_at = smem_at + g * C::kSlabPitch + (i % (kSlabK / kStageK)) * kStageK * 2 + 16 * t;
-        const uint8_t* sc = scales + (i % kStages) * C::kScaleBytes;
-        for (int gi = 0; gi < per_stage; ++gi) {
-            const uint2 sa = *reinterpret_cast<const uint2*>(sc + (row_a * (kGroupsMax + 1) + gi) * 8);
-            const uint2 sb = *reinterpret_cast<const uint2*>(sc + (row_b * (kGroupsMax + 1) + gi) * 8);
-            const uint32_t off_a = __byte_perm(sa.y, 0, 0x1010), off_b = __byte_perm(sb.y, 0, 0x1010);
-            const uint32_t off16_a = __byte_perm(sa.y, 0, 0x3232), off16_b = __byte_perm(sb.y, 0, 0x3232);
+        const uint32_t at_a = word_a + (i % kStages) * kStageBytes, at_b = word_b + (i % kStages) * kStageBytes;
+        const uint32_t x_off = (i & (p.slab_stages - 1)) * kStageK * 2;
+        // first group of the stage, counted from the slab's
+        const int first = ((k0 + i * kStageK) >> p.group_log2) - ((k0 + (i & ~(p.slab_stages - 1)) * kStageK) >> p.group_log2);
+#pragma unroll
+        for (int gi = 0; gi < kScales; ++gi) {
+            uint32_t raw_a, raw_b, ua = 8, ub = 8;  // zero point + 8
+            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(raw_a) : "r"(scale_a + 2 * first + 2 * gi));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(raw_b) : "r"(scale_b + 2 * first + 2 * gi));
+            if (p.zero) {
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ua) : "r"(zero_a + first + gi));
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ub) : "r"(zero_b + first + gi));
+                ua = (ua & 15) ^ 8, ub = (ub & 15) ^ 8;
+            }
+            // patterns of bias + 8 + zero, whose last place is 1 (1/16 for -(64 + 8 + zero))
+            const uint32_t off_a = ua * 0x10001u + (kBf16 ? 0x43004300u : 0x64006400u), off_b = ub * 0x10001u + (kBf16 ? 0x43004300u : 0x64006400u);
+            const uint32_t off16_a = ua * 0x100010u + 0xD400D400u, off16_b = ub * 0x100010u + 0xD400D400u;
+            const float s_a = p.scale_bf16 ? __uint_as_float(raw_a << 16) : __half2float(__ushort_as_half((unsigned short)raw_a));
+            const float s_b = p.scale_bf16 ? __uint_as_float(raw_b << 16) : __half2float(__ushort_as_half((unsigned short)raw_b));
             float acc[kMT][4];
 #pragma unroll
-            for (int mt = 0; mt < kMT; ++mt) acc[mt][0] = acc[mt][1] = acc[mt][2] = acc[mt][3] = 0.0f;
-#pragma unroll 2
-            for (int j = 0; j < steps_per_scale; ++j) {
-                const int c = gi * steps_per_scale + j;  // 32 k
+            for (int j = 0; j < kGroupSteps; ++j) {
+                const int c = gi * kGroupSteps + j;  // 32 k
                 uint32_t wa = lds32(at_a + 16 * c), wb = lds32(at_b + 16 * c);
                 if constexpr (!kAligned) {
                     wa = __funnelshift_r(wa, lds32(at_a + 16 * c + 4), 8 * (shift_a & 3));
@@ -211,13 +264,12 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
                 const uint32_t a0[4] = {fa[0], fb[0], fa[1], fb[1]}, a1[4] = {fa[2], fb[2], fa[3], fb[3]};
 #pragma unroll
                 for (int mt = 0; mt < kMT; ++mt) {
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (8 * mt + g < rows_m) x = lds128(x_at + mt * 8 * C::kSlabPitch + 64 * c);
-                    mma_16816<kBf16>(acc[mt], a0, x.x, x.y);
+                    const uint4 x = lds128(x_row[mt] + (x_off & x_mask[mt]) + 64 * c);
+                    if (j == 0) mma_16816_zero<kBf16>(acc[mt], a0, x.x, x.y);
+                    else mma_16816<kBf16>(acc[mt], a0, x.x, x.y);
                     mma_16816<kBf16>(acc[mt], a1, x.z, x.w);
                 }
             }
-            const float s_a = __uint_as_float(sa.x), s_b = __uint_as_float(sb.x);
 #pragma unroll
             for (int mt = 0; mt < kMT; ++mt) {
                 total[mt][0] = fmaf(acc[mt][0], s_a, total[mt][0]);
@@ -232,11 +284,10 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
 
     // ---- sums to shared memory as (row of x, row of the weight), then the cluster's blocks add them
     float* sums = reinterpret_cast<float*>(smem);
-    constexpr int kSumPitch = kRowsN + 4;
 #pragma unroll
     for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sums[(8 * mt + 2 * t + (j & 1)) * kSumPitch + (j >> 1 ? row_b : row_a)] = total[mt][j];
+        for (int j = 0; j < 4; ++j) sums[(8 * mt + 2 * t + (j & 1)) * kSumPitch + warp * kWarpRows + (j >> 1 ? row_b : row_a)] = total[mt][j];
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     if (parts > 1) cluster.sync();
@@ -253,21 +304,32 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
             if (r < parts) v += from[r][m * kSumPitch + n];
         const int64_t at = (int64_t)(m0 + m) * p.ldy + n0 + n;
         if (p.y_f32) reinterpret_cast<float*>(p.y)[at] = v;
-        else reinterpret_cast<T16*>(p.y)[at] = Half<kBf16>::from_float(v);
+        else reinterpret_cast<typename Half<kBf16>::type*>(p.y)[at] = Half<kBf16>::from_float(v);
     }
     if (parts > 1) cluster.sync();  // no block leaves while its sums are read
 }
 
-template <int kMT, bool kBf16, bool kAligned>
-cudaError_t launch(const LinearParams& p, int parts, cudaStream_t st) {
-    using C = Config<kMT>;
-    static_assert(C::kSumBytes <= C::kXBytes, "the sums take the place of x");
-    cudaError_t e = cudaFuncSetAttribute(linear_w4_kernel<kMT, kBf16, kAligned>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+template <int kMT, int kGroupSteps, bool kBf16, bool kAligned>
+cudaError_t launch(LinearParams p, int parts, cudaStream_t st) {
+    // Shared memory: x of a slab (and at the end the sums in its place), the rings, the slabs' scales and zeros twice.
+    const int rows = std::min(p.M, 8 * kMT), slab_k = rows == 1 ? 4 * kSlabK : (rows <= 3 ? 2 * kSlabK : kSlabK);
+    const int slab_groups = std::max(1, slab_k >> p.group_log2);
+    p.slab_stages = slab_k / kStageK;
+    p.scale_pitch = (int)round_up(2 * slab_groups, 16) + 16;
+    p.zero_pitch = p.zero ? (int)round_up(slab_groups, 16) + 16 : 0;
+    p.slabs = p.k_per_block > slab_k ? 2 : 1;
+    p.ring_at = (int)round_up(std::max(rows * (slab_k * 2 + 64), 8 * kMT * kSumPitch * 4) + kZeroBytes, 128);
+    p.slab_at = p.ring_at + kWarps * kStages * kStageBytes;
+    const int smem = p.slab_at + kWarps * p.slabs * kWarpRows * (p.scale_pitch + p.zero_pitch);
+    constexpr int kMost = std::max(8 * kMT * (kSlabK * 2 + 64), kSlabKMost * 2 + 64) + kZeroBytes + 128 + kWarps * kStages * kStageBytes +
+                          kWarps * 2 * kWarpRows * (kSlabKMost / 32 * 3 + 32);
+    static_assert(kMost <= 227 * 1024, "shared memory of a block");
+    cudaError_t e = cudaFuncSetAttribute(linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((p.N + kRowsN - 1) / kRowsN, parts, (p.M + C::kRowsM - 1) / C::kRowsM);
+    cfg.gridDim = dim3((p.N + kRowsN - 1) / kRowsN, parts, (p.M + 8 * kMT - 1) / (8 * kMT));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = C::kSmemBytes;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -276,12 +338,22 @@ cudaError_t launch(const LinearParams& p, int parts, cudaStream_t st) {
     attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, linear_w4_kernel<kMT, kBf16, kAligned>, p);
+    return cudaLaunchKernelEx(&cfg, linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, p);
+}
+template <int kMT, int kGroupSteps>
+cudaError_t launch(const LinearParams& p, bool bf16, bool aligned, int parts, cudaStream_t st) {
+    if (bf16)
+        return aligned ? launch<kMT, kGroupSteps, true, true>(p, parts, st) : launch<kMT, kGroupSteps, true, false>(p, parts, st);
+    return aligned ? launch<kMT, kGroupSteps, false, true>(p, parts, st) : launch<kMT, kGroupSteps, false, false>(p, parts, st);
 }
 template <int kMT>
 cudaError_t launch(const LinearParams& p, bool bf16, bool aligned, int parts, cudaStream_t st) {
-    if (bf16) return aligned ? launch<kMT, true, true>(p, parts, st) : launch<kMT, true, false>(p, parts, st);
-    return aligned ? launch<kMT, false, true>(p, parts, st) : launch<kMT, false, false>(p, parts, st);
+    switch (p.group_log2) {
+        case 5: return launch<kMT, 1>(p, bf16, aligned, parts, st);
+        case 6: return launch<kMT, 2>(p, bf16, aligned, parts, st);
+        case 7: return launch<kMT, 4>(p, bf16, aligned, parts, st);
+        default: return launch<kMT, 8>(p, bf16, aligned, parts, st);
+    }
 }
 
 }  // namespace
@@ -303,7 +375,7 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     if (!x_dev || !y_dev || (M > 1 && (ldx < W->K || ldy < W->N))) return AWE_ERR_INVALID_ARG;
     if ((uintptr_t)x_dev % 2 || (uintptr_t)W->scale_dev % 2 || (uintptr_t)y_dev % (y_type == AWE_F32 ? 4 : 2)) return AWE_ERR_ALIGNMENT;
     LinearParams p = {};
-    p.codes = (const uint8_t*)W->codes_dev, p.scale = W->scale_dev, p.zero = W->zero_dev, p.x = x_dev, p.y = y_dev;
+    p.codes = (const uint8_t*)W->codes_dev, p.scale = (const uint8_t*)W->scale_dev, p.zero = (const uint8_t*)W->zero_dev, p.x = x_dev, p.y = y_dev;
     p.row_bytes = W->ld / 2, p.ldx = ldx, p.ldy = ldy;
     p.M = (int)M, p.N = (int)W->N, p.K = (int)W->K;
     while ((int64_t)1 << p.group_log2 < W->group && p.group_log2 < 31) ++p.group_log2;
@@ -312,10 +384,10 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     p.x_vec = (uintptr_t)x_dev % 16 == 0 && (ldx % 8 == 0 || M == 1);
     const bool aligned = (uintptr_t)W->codes_dev % 16 == 0 && W->ld % 32 == 0;
     const int tiles_m = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
-    // Parts of K: enough blocks for about three per SM, each with two stages at least.
+    // Parts of K: as many blocks as stay within four per SM (what is resident at once), with two stages each at least.
     const int64_t tiles = (p.N + kRowsN - 1) / kRowsN * ((M + 8 * tiles_m - 1) / (8 * tiles_m));
     int parts = 1;
-    while (parts < kMaxCluster && tiles * parts < 3 * h->sm_count && p.K > 2 * parts * 2 * kStageK) parts *= 2;
+    while (parts < kMaxCluster && 2 * tiles * parts <= 4 * h->sm_count && p.K > 2 * parts * 2 * kStageK) parts *= 2;
     p.k_per_block = (int)round_up((p.K + parts - 1) / parts, kStageK);
     cudaStream_t st = (cudaStream_t)stream;
     const bool bf16 = x_type == AWE_BF16;
