@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     __shared__ int64_t found_at;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
 
+    grid_wait();
     // ---- which steps are mine: exclusive sum of units x steps over the requests
     int64_t total = 0;
     for (int pass = 0; pass < 2; ++pass) {
@@ -495,6 +496,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_join_kernel(const AttnP
     using T16 = typename Half<kBf16>::type;
     const int lane = threadIdx.x & 31, q_heads = p.heads * p.group;
     const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    grid_wait();
     if (item >= p.T * q_heads) return;
     const int token = (int)(item / q_heads), qh = (int)(item % q_heads);
     // the request of the token: last b with q_start[b] <= token
@@ -581,11 +583,9 @@ cudaError_t launch_attention(const AttnParams& p, cudaStream_t st) {
     using C = Config<kD, kNT>;
     cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<kD, kNT, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
     if (e != cudaSuccess) return e;
-    kv_attention_kernel<kD, kNT, kBf16><<<p.blocks, kThreads, C::kSmemBytes, st>>>(p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_early(kv_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     const int64_t items = p.T * p.heads * p.group;
-    kv_attention_join_kernel<kD, kNT, kBf16><<<(unsigned)((items + kWarps - 1) / kWarps), kThreads, 0, st>>>(p);
-    return cudaGetLastError();
+    return launch_early(kv_attention_join_kernel<kD, kNT, kBf16>, dim3((unsigned)((items + kWarps - 1) / kWarps)), kThreads, 0, st, p);
 }
 
 }  // namespace

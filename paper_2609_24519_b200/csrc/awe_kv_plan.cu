@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "awe_internal.h"
+#include "serve_common.cuh"
 
 namespace awe {
 namespace {
@@ -54,6 +55,7 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(PlanParams p) {
     };
     auto pages_of = [&](int64_t tokens) { return (int)((tokens + mask) >> p.page_log2); };
 
+    serve::grid_wait();
     // each thread sums a run of requests, the block sums the threads, each thread writes its run's prefix
     const int per = (p.B + kThreads - 1) / kThreads, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     Sums s = {0, 0, 0, 0};
@@ -166,8 +168,7 @@ extern "C" awe_status_t awe_kv_plan(awe_handle_t h, const int32_t* cached_len_de
         return AWE_ERR_CUDA;
     const int64_t items = std::max(max_tokens, B);
     const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>((items + kThreads - 1) / kThreads, 4 * h->sm_count));
-    kv_plan_kernel<<<blocks, kThreads, smem, (cudaStream_t)stream>>>(p);
-    if (cudaGetLastError() != cudaSuccess) return AWE_ERR_CUDA;
+    if (serve::launch_early(kv_plan_kernel, dim3(blocks), kThreads, smem, (cudaStream_t)stream, p) != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;
 }

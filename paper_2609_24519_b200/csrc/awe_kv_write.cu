@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
         const int64_t s = p.slots[t];
         return s < 0 || s >= p.n_slots ? -1 : s >> p.page_log2;
     };
+    grid_wait();
     const int64_t t_begin = (int64_t)blockIdx.x * p.window, t_end = min(p.T, t_begin + p.window);
     unsigned begins = 0;  // of the 32 tokens from t32, those that begin a run (every warp finds out for itself)
     for (int64_t t32 = t_begin, t0 = 0; t32 < t_end || begins; begins &= begins - 1) {
@@ -210,6 +211,7 @@ awe_status_t check_kv_cache(const awe_kv_cache* c) {
 }  // namespace awe
 
 using namespace awe;
+using namespace awe::serve;
 
 extern "C" awe_status_t awe_kv_write(awe_handle_t h, const awe_kv_cache* cache, const void* k_dev, const void* v_dev,
                                      awe_float_t type, int64_t T, int64_t ldk, int64_t ldv, const int64_t* slots_dev,
@@ -233,14 +235,11 @@ extern "C" awe_status_t awe_kv_write(awe_handle_t h, const awe_kv_cache* cache, 
     const dim3 grid((unsigned)((T + p.window - 1) / p.window), (unsigned)cache->n_heads, 2);
     const bool vec = (uintptr_t)k_dev % 16 == 0 && (uintptr_t)v_dev % 16 == 0 && ldk % 8 == 0 && ldv % 8 == 0;
     cudaStream_t st = (cudaStream_t)stream;
-    if (type == AWE_BF16) {
-        if (vec) kv_write_kernel<true, true><<<grid, kThreads, 0, st>>>(p);
-        else kv_write_kernel<true, false><<<grid, kThreads, 0, st>>>(p);
-    } else {
-        if (vec) kv_write_kernel<false, true><<<grid, kThreads, 0, st>>>(p);
-        else kv_write_kernel<false, false><<<grid, kThreads, 0, st>>>(p);
-    }
-    if (cudaGetLastError() != cudaSuccess) return AWE_ERR_CUDA;
+    const cudaError_t e = type == AWE_BF16 ? (vec ? launch_early(kv_write_kernel<true, true>, grid, kThreads, 0, st, p)
+                                                  : launch_early(kv_write_kernel<true, false>, grid, kThreads, 0, st, p))
+                                           : (vec ? launch_early(kv_write_kernel<false, true>, grid, kThreads, 0, st, p)
+                                                  : launch_early(kv_write_kernel<false, false>, grid, kThreads, 0, st, p));
+    if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;
 }

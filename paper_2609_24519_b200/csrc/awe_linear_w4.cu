@@ -17,8 +17,7 @@
 
 #include <algorithm>
 
-#include "awe_internal.h"
-#include "serve_common.cuh"
+#include "linear_w4.cuh"
 
 namespace awe {
 namespace {
@@ -81,45 +80,6 @@ __device__ __forceinline__ void unpack_word(uint32_t w, uint32_t offset, uint32_
             w >>= 8;
         }
     }
-}
-
-// The first 16 bytes of an unaligned row whose 16-byte piece begins in front of the array: bytes from `first` on.
-__device__ __noinline__ void copy_first_piece(uint32_t dst, const uint8_t* piece, int first, int bytes) {
-    for (int e = 0; e < 16; ++e)
-        asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + e), "r"((uint32_t)(e >= first && e < bytes ? piece[e] : 0)) : "memory");
-}
-// Piece c of the copy of [src, src + n) to dst + (src mod 16), in pieces of 16 bytes that start on 16-byte boundaries.
-// What lies in front of `base` is not ours to read.
-__device__ __forceinline__ void copy_piece(uint32_t dst, const uint8_t* src, int n, int c, const uint8_t* base) {
-    const int shift = (int)((uintptr_t)src & 15);
-    const uint8_t* piece = src - shift + 16 * c;
-    const int bytes = min(16, max(0, n + shift - 16 * c));
-    if (piece >= base) cp_async16(dst + 16 * c, bytes ? piece : src - shift + 16, bytes);
-    else copy_first_piece(dst + 16 * c, piece, (int)(base - piece), bytes);
-}
-// 8 consecutive 16-bit values of x at any 2-byte alignment.
-__device__ __forceinline__ uint4 load_x8(const uint16_t* src, bool vec, int n) {
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (n >= 8) {
-        if (vec) return __ldg(reinterpret_cast<const uint4*>(src));
-        if (((uintptr_t)src & 2) == 0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = __ldg(reinterpret_cast<const uint32_t*>(src) + e);
-        } else {  // the first and the last half word by themselves
-            uint32_t v[5];
-            v[0] = (uint32_t)__ldg(src) << 16;
-#pragma unroll
-            for (int e = 0; e < 3; ++e) v[e + 1] = __ldg(reinterpret_cast<const uint32_t*>(src + 1) + e);
-            v[4] = __ldg(src + 7);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = __funnelshift_r(v[e], v[e + 1], 16);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (e < n) w[e >> 1] |= (uint32_t)src[e] << (16 * (e & 1));
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <int kMT, int kGroupSteps, bool kBf16, bool kAligned>
@@ -331,11 +291,7 @@ cudaError_t launch(LinearParams p, int parts, cudaStream_t st) {
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 1;
-    attr.val.clusterDim.y = parts;
-    attr.val.clusterDim.z = 1;
+    cudaLaunchAttribute attr = cluster_attribute(parts);
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, p);
@@ -383,13 +339,19 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     p.scale_bf16 = W->scale_type == AWE_BF16, p.y_f32 = y_type == AWE_F32;
     p.x_vec = (uintptr_t)x_dev % 16 == 0 && (ldx % 8 == 0 || M == 1);
     const bool aligned = (uintptr_t)W->codes_dev % 16 == 0 && W->ld % 32 == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    // tcgen05 pays where its 128 x 16 to 128 x 128 tiles are many enough or x has more rows than one or two columns blocks of
+    // the small instruction: M = 128, 8,192 x 8,192: 38 us against 175; M = 16, 4,096 x 4,096: 9.4 against 10.3; M = 32, 1,024 x
+    // 1,024: 8.8 against 11.0.  Below that the small kernel has less to set up: M = 1, 8,192 x 8,192: 16.6 us against 22.6;
+    // M = 16, 1,024 x 1,024: 6.8 against 7.6; M = 96, 1,024 x 1,024: 11.0 against 17.6.
+    if ((M > 8 && W->N >= 2048) || (M > 16 && M <= 64))
+        return linear_w4_tc(h, *W, x_dev, x_type == AWE_BF16, M, ldx, y_dev, y_type == AWE_F32, ldy, st);
     const int tiles_m = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
     // Parts of K: as many blocks as stay within four per SM (what is resident at once), with two stages each at least.
     const int64_t tiles = (p.N + kRowsN - 1) / kRowsN * ((M + 8 * tiles_m - 1) / (8 * tiles_m));
     int parts = 1;
     while (parts < kMaxCluster && 2 * tiles * parts <= 4 * h->sm_count && p.K > 2 * parts * 2 * kStageK) parts *= 2;
     p.k_per_block = (int)round_up((p.K + parts - 1) / parts, kStageK);
-    cudaStream_t st = (cudaStream_t)stream;
     const bool bf16 = x_type == AWE_BF16;
     const cudaError_t e = tiles_m == 1   ? launch<1>(p, bf16, aligned, parts, st)
                           : tiles_m == 2 ? launch<2>(p, bf16, aligned, parts, st)

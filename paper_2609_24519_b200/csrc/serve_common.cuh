@@ -38,6 +38,13 @@ struct Half<true> {
     }
 };
 
+// The small serving kernels may be launched while the kernel before them on the stream still runs; nothing of global
+// memory is touched before this wait for that kernel's end.  (It saves 0.3 to 0.5 us a launch.  Letting the kernel behind
+// come as early as this one begins made every case of several waves slower, attention over 64 requests by 45 %.)
+__device__ __forceinline__ void grid_wait() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // 2^x to 2 units in the last place of FP32 (2^-inf = 0).
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -106,6 +113,33 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
     return v;
+}
+
+inline cudaLaunchAttribute early_launch_attribute() {
+    cudaLaunchAttribute a = {};
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    return a;
+}
+inline cudaLaunchAttribute cluster_attribute(int parts) {  // `parts` blocks along y
+    cudaLaunchAttribute a = {};
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = 1;
+    a.val.clusterDim.y = parts;
+    a.val.clusterDim.z = 1;
+    return a;
+}
+template <class... Params, class... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+    cudaLaunchAttribute attr = early_launch_attribute();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace serve
