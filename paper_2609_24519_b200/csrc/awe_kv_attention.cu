@@ -16,10 +16,10 @@
 // Products are transposed (rows of the matrix instruction are tokens, then dimensions; its 8 columns are query
 // rows), which wastes the least where a group has few heads.  Each warp keeps its own running maximum and sums.
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
-#include "awe_internal.h"
-#include "serve_common.cuh"
+#include "kv_attention.cuh"
 
 namespace awe {
 awe_status_t check_kv_cache(const awe_kv_cache* c);
@@ -31,22 +31,6 @@ using namespace serve;
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStepTokens = 16 * kWarps;
-
-struct AttnParams {
-    const int8_t *k, *v;
-    const float *k_scale, *v_scale;
-    const void* q;
-    void* out;
-    float* lse;
-    const int32_t *q_start, *ctx_len, *table;
-    int64_t* unit_steps;  // B + 1: exclusive sum over the requests of units x steps
-    float* part_vec;      // [2 * blocks][8 * kNT rows][head_dim]
-    float4* part_stat;    // [2 * blocks][8 * kNT rows]: reference (base-2 logarithm), sum of the rounded exponentials, sum
-    int64_t ldq, ldo, ld_table, T;
-    float scale_log2;     // scale / ln 2
-    int B, heads, group, page_log2, n_pages, max_pages, causal, blocks;
-    int64_t window;
-};
 
 // The steps of one request: tokens [lo, hi) in steps of kStepTokens, for each of `units` units.
 struct Request {
@@ -66,22 +50,6 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int b) {
     return r;
 }
 
-// The steps are dealt out to the blocks in order, as evenly as whole numbers go: the first `extra` blocks take one more.
-struct Deal {
-    int64_t each;
-    int extra, blocks;
-    __device__ __forceinline__ Deal(int64_t total, int most_blocks) {
-        blocks = (int)min((int64_t)most_blocks, max(total, (int64_t)1));
-        each = total / blocks;
-        extra = (int)(total - each * blocks);
-    }
-    __device__ __forceinline__ int64_t begin(int i) const { return each * i + min(i, extra); }
-    __device__ __forceinline__ int block_of(int64_t step) const {
-        const int64_t cut = (each + 1) * extra;
-        return step < cut ? (int)(step / (each + 1)) : extra + (int)((step - cut) / each);
-    }
-};
-
 template <int kD, int kNT>
 struct Config {
     static constexpr int kRows = 8 * kNT;
@@ -99,14 +67,6 @@ template <int kD>
 __device__ __forceinline__ uint32_t piece_at(int r, int c) {
     if constexpr (kD == 64) return (r >> 1) * 128 + (((((r & 1) << 2) + c) ^ (((r >> 1) & 3) << 1)) << 4);
     return r * kD + ((c & ~7) << 4) + (((c & 7) ^ (r & 7)) << 4);
-}
-
-// Four signed bytes as two pairs of FP16: the byte with its sign bit flipped is u = x + 128, the FP16 pattern
-// 0x6400 | u is 1024 + u, and subtracting 1152 is exact.
-__device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped, uint32_t selector) {
-    const uint32_t w = __byte_perm(flipped, 0x64646464u, selector);
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1152.0f));
-    return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 template <int kD, int kNT, bool kBf16>
@@ -556,6 +516,16 @@ int row_tiles(int64_t T, int64_t B, int64_t group, int64_t head_dim) {
     return head_dim < 256 && T * group > 8 * B ? 2 : 1;
 }
 
+// tcgen05 pays from about 64 query rows per request and head on, where the work fills its units of 256 rows x 128
+// tokens: 8 heads of 128, one request of 4,096 tokens, 128 rows 36 us against 39, 1,024 rows 81 against 184; 16 or 32 rows
+// 32 us against 25; 512 tokens, 512 rows 32 us against 25, 1,024 rows 36 against 45.  The host knows the tokens only by the
+// table's width.
+bool use_tc(int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t head_dim, int64_t tokens, int64_t window) {
+    if (head_dim > 128 || T * group < 64 * B) return false;
+    if (window > 0) tokens = std::min(tokens, window + T / B + 128);
+    return (double)T * n_q_heads * head_dim * tokens >= (double)(1 << 29);
+}
+
 struct Workspace {
     size_t vec, stat, total;
 };
@@ -599,7 +569,7 @@ extern "C" size_t awe_kv_attention_workspace_bytes(awe_handle_t h, const awe_kv_
     size_t most = 0;
     for (int nt = 1; nt <= (cache->head_dim < 256 ? 2 : 1); ++nt)
         most = std::max(most, workspace_of(blocks_of(h->sm_count, cache->head_dim, nt), 8 * nt, cache->head_dim, B).total);
-    return most;
+    return std::max(most, kv_attention_tc_workspace_bytes(h, T, n_q_heads, B, cache->head_dim));
 }
 
 extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const void* q_dev, awe_float_t type,
@@ -637,6 +607,8 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     p.B = (int)B, p.heads = (int)cache->n_heads, p.group = (int)group, p.page_log2 = page_log2;
     p.n_pages = (int)cache->n_pages, p.max_pages = (int)max_pages, p.causal = causal != 0;
     p.window = window;
+    if (getenv("AWE_ATC") ? (cache->head_dim <= 128 && atoi(getenv("AWE_ATC")) == 0) : use_tc(T, B, n_q_heads, group, cache->head_dim, max_pages * cache->page_size, window))
+        return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, workspace_dev, (cudaStream_t)stream);
     p.blocks = blocks_of(h->sm_count, cache->head_dim, nt);
     const Workspace w = workspace_of(p.blocks, 8 * nt, cache->head_dim, B);
     p.unit_steps = (int64_t*)workspace_dev;

@@ -1,0 +1,53 @@
+// What the two attention kernels share: one for few query rows (awe_kv_attention.cu), one on tcgen05 for many
+// (awe_kv_attention_tc.cu).
+#pragma once
+#include "awe_internal.h"
+#include "serve_common.cuh"
+
+namespace awe {
+
+struct AttnParams {
+    const int8_t *k, *v;
+    const float *k_scale, *v_scale;
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t *q_start, *ctx_len, *table;
+    int64_t* unit_steps;  // B + 1: exclusive sum over the requests of units x steps
+    float* part_vec;      // [2 * blocks][8 * kNT rows][head_dim]
+    float4* part_stat;    // [2 * blocks][8 * kNT rows]: reference (base-2 logarithm), sum of the rounded exponentials, sum
+    int64_t ldq, ldo, ld_table, T;
+    float scale_log2;     // scale / ln 2
+    int B, heads, group, page_log2, n_pages, max_pages, causal, blocks;
+    int64_t window;
+};
+
+// The steps are dealt out to the blocks in order, as evenly as whole numbers go: the first `extra` blocks take one more.
+struct Deal {
+    int64_t each;
+    int extra, blocks;
+    __device__ __forceinline__ Deal(int64_t total, int most_blocks) {
+        blocks = (int)min((int64_t)most_blocks, max(total, (int64_t)1));
+        each = total / blocks;
+        extra = (int)(total - each * blocks);
+    }
+    __device__ __forceinline__ int64_t begin(int i) const { return each * i + min(i, extra); }
+    __device__ __forceinline__ int block_of(int64_t step) const {
+        const int64_t cut = (each + 1) * extra;
+        return step < cut ? (int)(step / (each + 1)) : extra + (int)((step - cut) / each);
+    }
+};
+
+// Four signed bytes as two pairs of FP16: the byte with its sign bit flipped is u = x + 128, the FP16 pattern
+// 0x6400 | u is 1024 + u, and subtracting 1152 is exact.
+__device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped, uint32_t selector) {
+    const uint32_t w = __byte_perm(flipped, 0x64646464u, selector);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1152.0f));
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Prompts: the tcgen05 kernel; the arguments have been checked, p's pointers into the workspace are not set.
+size_t kv_attention_tc_workspace_bytes(awe_ctx* h, int64_t T, int64_t n_q_heads, int64_t B, int64_t head_dim);
+awe_status_t kv_attention_tc(awe_ctx* h, AttnParams p, int64_t head_dim, bool bf16, void* workspace, cudaStream_t st);
+
+}  // namespace awe
