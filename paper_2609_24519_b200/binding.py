@@ -143,17 +143,18 @@ def _check(status: int, where: str) -> None:
 
 def _ptr(x) -> int:
     """Address of a torch tensor (device or host) or a numpy array."""
-    if x is None:
-        return 0
-    if isinstance(x, np.ndarray):
-        return x.ctypes.data
-    return x.data_ptr()
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return 0 if x is None else x.ctypes.data
 
 
 def _stream(stream) -> int:
+    """cudaStream_t of a torch stream, an address, or (None) torch's current stream on the current device.  The raw
+    lookup takes 0.1 us; building a Stream object to read its address takes 3."""
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(getattr(stream, "cuda_stream", stream))
 
 
@@ -321,24 +322,28 @@ def kv_cache(k, v, k_scale, v_scale, n_pages: int, n_heads: int, page_size: int,
 
 
 def awe_linear_w4(h: Handle, W: W4Matrix, x, x_type: int, M: int, ldx: int, y, y_type: int, ldy: int, stream=None) -> None:
-    _check(lib().awe_linear_w4(h.raw, W, _ptr(x), x_type, M, ldx, _ptr(y), y_type, ldy, _stream(stream)), "awe_linear_w4")
+    status = _lib.awe_linear_w4(h._h, W, _ptr(x), x_type, M, ldx, _ptr(y), y_type, ldy, _stream(stream))
+    if status:
+        raise AweError(status, "awe_linear_w4")
 
 
 def awe_kv_plan(h: Handle, cached_len, new_len, B: int, page_size: int, free_pages, n_free: int, block_table,
                 max_pages: int, ld_table: int, slots, positions, max_tokens: int, q_start, ctx_len, counts,
                 stream=None) -> None:
-    _check(lib().awe_kv_plan(h.raw, _ptr(cached_len), _ptr(new_len), B, page_size, _ptr(free_pages), n_free,
+    status = _lib.awe_kv_plan(h._h, _ptr(cached_len), _ptr(new_len), B, page_size, _ptr(free_pages), n_free,
                              _ptr(block_table), max_pages, ld_table, _ptr(slots), _ptr(positions), max_tokens,
-                             _ptr(q_start), _ptr(ctx_len), _ptr(counts), _stream(stream)), "awe_kv_plan")
+                             _ptr(q_start), _ptr(ctx_len), _ptr(counts), _stream(stream))
+    if status:
+        raise AweError(status, "awe_kv_plan")
 
 
 def awe_kv_write(h: Handle, cache: KvCache, k, v, dtype: int, T: int, ldk: int, ldv: int, slots, stream=None) -> None:
-    _check(lib().awe_kv_write(h.raw, cache, _ptr(k), _ptr(v), dtype, T, ldk, ldv, _ptr(slots), _stream(stream)),
+    _check(_lib.awe_kv_write(h._h, cache, _ptr(k), _ptr(v), dtype, T, ldk, ldv, _ptr(slots), _stream(stream)),
            "awe_kv_write")
 
 
 def awe_kv_attention_workspace_bytes(h: Handle, cache: KvCache, T: int, n_q_heads: int, B: int) -> int:
-    return int(lib().awe_kv_attention_workspace_bytes(h.raw, cache, T, n_q_heads, B))
+    return int(lib().awe_kv_attention_workspace_bytes(h._h, cache, T, n_q_heads, B))
 
 
 def awe_kv_attention(h: Handle, cache: KvCache, q, dtype: int, T: int, n_q_heads: int, ldq: int, q_start, ctx_len, B: int,
@@ -346,9 +351,11 @@ def awe_kv_attention(h: Handle, cache: KvCache, q, dtype: int, T: int, n_q_heads
                      lse, workspace, workspace_bytes: Optional[int] = None, stream=None) -> None:
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
-    _check(lib().awe_kv_attention(h.raw, cache, _ptr(q), dtype, T, n_q_heads, ldq, _ptr(q_start), _ptr(ctx_len), B,
+    status = _lib.awe_kv_attention(h._h, cache, _ptr(q), dtype, T, n_q_heads, ldq, _ptr(q_start), _ptr(ctx_len), B,
                                   _ptr(block_table), max_pages, ld_table, scale, causal, window, _ptr(out), ldo, _ptr(lse),
-                                  _ptr(workspace), workspace_bytes, _stream(stream)), "awe_kv_attention")
+                                  _ptr(workspace), workspace_bytes, _stream(stream))
+    if status:
+        raise AweError(status, "awe_kv_attention")
 
 
 def awe_last_device_status(h: Handle, stream=None):

@@ -16,7 +16,6 @@
 // Products are transposed (rows of the matrix instruction are tokens, then dimensions; its 8 columns are query
 // rows), which wastes the least where a group has few heads.  Each warp keeps its own running maximum and sums.
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "kv_attention.cuh"
@@ -520,8 +519,10 @@ int row_tiles(int64_t T, int64_t B, int64_t group, int64_t head_dim) {
 // tokens: 8 heads of 128, one request of 4,096 tokens, 128 rows 36 us against 39, 1,024 rows 81 against 184; 16 or 32 rows
 // 32 us against 25; 512 tokens, 512 rows 32 us against 25, 1,024 rows 36 against 45.  The host knows the tokens only by the
 // table's width.
-bool use_tc(int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t head_dim, int64_t tokens, int64_t window) {
+bool use_tc(const awe_kv_cache& cache, int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t tokens, int64_t window) {
+    const int64_t head_dim = cache.head_dim;
     if (head_dim > 128 || T * group < 64 * B) return false;
+    if (cache.n_pages * cache.n_heads * cache.page_size * head_dim >= (int64_t)15 << 32) return false;  // its offsets are 32 bits of 16-byte units
     if (window > 0) tokens = std::min(tokens, window + T / B + 128);
     return (double)T * n_q_heads * head_dim * tokens >= (double)(1 << 29);
 }
@@ -549,9 +550,10 @@ int blocks_of(int sm_count, int64_t head_dim, int nt) {
 }
 
 template <int kD, int kNT, bool kBf16>
-cudaError_t launch_attention(const AttnParams& p, cudaStream_t st) {
+cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
     using C = Config<kD, kNT>;
-    cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<kD, kNT, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(kv_attention_kernel<kD, kNT, kBf16>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     const int64_t items = p.T * p.heads * p.group;
@@ -607,7 +609,7 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     p.B = (int)B, p.heads = (int)cache->n_heads, p.group = (int)group, p.page_log2 = page_log2;
     p.n_pages = (int)cache->n_pages, p.max_pages = (int)max_pages, p.causal = causal != 0;
     p.window = window;
-    if (getenv("AWE_ATC") ? (cache->head_dim <= 128 && atoi(getenv("AWE_ATC")) == 0) : use_tc(T, B, n_q_heads, group, cache->head_dim, max_pages * cache->page_size, window))
+    if (use_tc(*cache, T, B, n_q_heads, group, max_pages * cache->page_size, window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, workspace_dev, (cudaStream_t)stream);
     p.blocks = blocks_of(h->sm_count, cache->head_dim, nt);
     const Workspace w = workspace_of(p.blocks, 8 * nt, cache->head_dim, B);
@@ -616,8 +618,8 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     p.part_stat = (float4*)((uint8_t*)workspace_dev + w.stat);
     auto run = [&](auto dim, auto tiles) {
         constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
-        return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, (cudaStream_t)stream)
-                                : launch_attention<kD, kNT, false>(p, (cudaStream_t)stream);
+        return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)
+                                : launch_attention<kD, kNT, false>(p, h->device, (cudaStream_t)stream);
     };
     using std::integral_constant;
     cudaError_t e;

@@ -282,14 +282,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 return page;
             };
             uint4 kr[kPieces], vr[kPieces];
-            auto load = [&](const int8_t* pool, int pages, int j, uint4 (&x)[kPieces]) {
+            uint32_t at[kPieces];  // of the pieces of a step, in units of 16 bytes; ~0 where there is nothing
+            auto places = [&](int pages, int j) {
+                const int place = (u.lo + j * kStep) & ((1 << p.page_log2) - 1);
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                     const int row = i * kPassRows + r, page = __shfl_sync(~0u, pages, row >> 4);
-                    const int tok = u.lo + j * kStep + row;
+                    const uint32_t block = (uint32_t)(page * p.heads + head) << p.page_log2;
+                    at[i] = page < 0 ? ~0u : (block + ((place + row) & ((1 << p.page_log2) - 1))) * kPieces + c;
+                }
+            };
+            auto load = [&](const int8_t* pool, uint4 (&x)[kPieces]) {
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
                     x[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);  // becomes -128: finite, under a weight of 0
-                    if (page >= 0)
-                        x[i] = __ldg(reinterpret_cast<const uint4*>(pool + (((((int64_t)page * p.heads + head) << p.page_log2) + (tok & ((1 << p.page_log2) - 1))) * kD + 16 * c)));
+                    if (at[i] != ~0u) x[i] = __ldg(reinterpret_cast<const uint4*>(pool) + at[i]);
                 }
             };
             auto store = [&](uint32_t to, uint4 (&x)[kPieces]) {
@@ -318,8 +325,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             };
             int page = page_of(s0), next_page = page_of(s0 + 1);
             float2 scale = constants_of(page);
-            load(p.k, page, s0, kr);
-            load(p.v, page, s0, vr);
+            places(page, s0);
+            load(p.k, kr);
+            load(p.v, vr);
             for (int j = s0; j < s1; ++j, ++step) {
                 if (!__all_sync(~0u, wait(sh->k_empty[step & 1], ((step >> 1) & 1) ^ 1, 34))) return false;
                 store(base + C::kKAt + (step & 1) * C::kKBytes, kr);
@@ -335,13 +343,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh->k_full[step & 1]));
                 const int after = page_of(j + 2);
                 const float2 next_scale = constants_of(next_page);
-                if (j + 1 < s1) load(p.k, next_page, j + 1, kr);
+                if (j + 1 < s1) {
+                    places(next_page, j + 1);
+                    load(p.k, kr);
+                }
                 if (!__all_sync(~0u, wait(sh->v_empty[step & 1], ((step >> 1) & 1) ^ 1, 35))) return false;
                 store(base + C::kVAt + (step & 1) * C::kKBytes, vr);
                 ptx::fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh->v_full[step & 1]));
-                if (j + 1 < s1) load(p.v, next_page, j + 1, vr);
+                if (j + 1 < s1) load(p.v, vr);
                 page = next_page, next_page = after, scale = next_scale;
             }
             return true;
@@ -605,9 +616,10 @@ Workspace workspace_of(int blocks, int64_t T, int64_t group, int64_t B, int64_t 
 }
 
 template <int kD, bool kBf16>
-cudaError_t launch(const TcAttnParams& p, cudaStream_t st) {
+cudaError_t launch(const TcAttnParams& p, int device, cudaStream_t st) {
     using C = Config<kD>;
-    cudaError_t e = cudaFuncSetAttribute(kv_attention_tc_kernel<kD, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(kv_attention_tc_kernel<kD, kBf16>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_units_kernel, dim3(1), kPlanThreads, 0, st, p)) != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16>, dim3(p.a.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
@@ -627,8 +639,8 @@ awe_status_t kv_attention_tc(awe_ctx* h, AttnParams a, int64_t head_dim, bool bf
     uint8_t* at = (uint8_t*)workspace;
     a.part_vec = (float*)(at + w.vec), a.part_stat = (float4*)(at + w.stat);
     TcAttnParams p = {a, (int64_t*)(at + w.steps), (int2*)(at + w.of), (int32_t*)(at + w.base), (int)(a.T * a.group / kRows + a.B), h->status_dev};
-    const cudaError_t e = head_dim == 64 ? (bf16 ? launch<64, true>(p, st) : launch<64, false>(p, st))
-                                         : (bf16 ? launch<128, true>(p, st) : launch<128, false>(p, st));
+    const cudaError_t e = head_dim == 64 ? (bf16 ? launch<64, true>(p, h->device, st) : launch<64, false>(p, h->device, st))
+                                         : (bf16 ? launch<128, true>(p, h->device, st) : launch<128, false>(p, h->device, st));
     if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 3;
     return AWE_OK;

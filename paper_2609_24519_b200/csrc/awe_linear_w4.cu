@@ -52,6 +52,7 @@ struct LinearParams {
     int ring_at, slab_at;         // byte offsets in shared memory: x first
     int slabs;                    // 2 where a block has more than one
     int slab_stages;              // a power of two
+    int device;
 };
 
 // Nibbles i and i + 4 of a word as a pair of 16-bit floats, less `offset` = pattern bias + 8 + zero.
@@ -284,7 +285,8 @@ cudaError_t launch(LinearParams p, int parts, cudaStream_t st) {
     constexpr int kMost = std::max(8 * kMT * (kSlabK * 2 + 64), kSlabKMost * 2 + 64) + kZeroBytes + 128 + kWarps * kStages * kStageBytes +
                           kWarps * 2 * kWarpRows * (kSlabKMost / 32 * 3 + 32);
     static_assert(kMost <= 227 * 1024, "shared memory of a block");
-    cudaError_t e = cudaFuncSetAttribute(linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, kMost, p.device, done);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((p.N + kRowsN - 1) / kRowsN, parts, (p.M + 8 * kMT - 1) / (8 * kMT));
@@ -332,7 +334,7 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     if ((uintptr_t)x_dev % 2 || (uintptr_t)W->scale_dev % 2 || (uintptr_t)y_dev % (y_type == AWE_F32 ? 4 : 2)) return AWE_ERR_ALIGNMENT;
     LinearParams p = {};
     p.codes = (const uint8_t*)W->codes_dev, p.scale = (const uint8_t*)W->scale_dev, p.zero = (const uint8_t*)W->zero_dev, p.x = x_dev, p.y = y_dev;
-    p.row_bytes = W->ld / 2, p.ldx = ldx, p.ldy = ldy;
+    p.row_bytes = W->ld / 2, p.ldx = ldx, p.ldy = ldy, p.device = h->device;
     p.M = (int)M, p.N = (int)W->N, p.K = (int)W->K;
     while ((int64_t)1 << p.group_log2 < W->group && p.group_log2 < 31) ++p.group_log2;
     p.groups = (int)((W->K + W->group - 1) / W->group);

@@ -539,8 +539,8 @@ awe_status_t make_map_2d(awe_ctx* h, const void* at, bool bytes, int64_t inner, 
 template <int kMt, bool kBf16, bool kAligned>
 awe_status_t launch(awe_ctx* h, const CUtensorMap& mc, const CUtensorMap& mx, const TcParams& p, int parts, cudaStream_t st) {
     using C = Config<kMt, kAligned>;
-    if (cudaFuncSetAttribute(linear_w4_tc_kernel<kMt, kBf16, kAligned>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes) != cudaSuccess)
-        return AWE_ERR_CUDA;
+    static std::atomic<uint64_t> done{0};
+    if (allow_smem(linear_w4_tc_kernel<kMt, kBf16, kAligned>, C::kSmemBytes, h->device, done) != cudaSuccess) return AWE_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((p.N + kRowsN - 1) / kRowsN, parts, (p.M + kMt - 1) / kMt);
     cfg.blockDim = dim3(kThreads);

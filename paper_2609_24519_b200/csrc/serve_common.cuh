@@ -4,6 +4,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "awe.h"
 
 namespace awe {
@@ -115,6 +117,15 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     return v;
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory: asked of the runtime once per device (`done`: a bit each).
+template <class Kernel>
+cudaError_t allow_smem(Kernel kernel, int bytes, int device, std::atomic<uint64_t>& done) {
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 inline cudaLaunchAttribute early_launch_attribute() {
     cudaLaunchAttribute a = {};
     a.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -298,6 +298,52 @@ def test_attention_of_several_tokens(kind, dim, heads, group, page, causal, wind
     check_attention(rng, heads, group, dim, page, kind, new, ctx, causal, window, ld_extra=8)
 
 
+# A table that could hold long requests, and many queries: what the library takes for prompts.
+PROMPT = 40000
+
+
+@pytest.mark.parametrize("kind,dim,heads,group,page", [("f16", 128, 2, 4, 16), ("bf16", 128, 1, 1, 64), ("bf16", 64, 2, 5, 32), ("f16", 64, 1, 16, 128),
+                                                       ("bf16", 128, 1, 8, 256), ("f16", 256, 1, 2, 16)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 3), (True, 100), (False, 0)])
+def test_attention_of_prompts(kind, dim, heads, group, page, causal, window):
+    rng = np.random.default_rng(dim + heads * group + page + window)
+    new = [100, 0, 1, 129, 64, 0, 300, 2]
+    ctx = [100, 9, 1, 200, 700, 0, 301, 128]
+    check_attention(rng, heads, group, dim, page, kind, new, ctx, causal, window, ld_extra=8, width_extra=PROMPT // page)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_of_prompts_whose_rows_see_nothing_and_pages_that_are_gone(dim):
+    rng = np.random.default_rng(12)
+    check_attention(rng, 2, 4, dim, 16, "bf16", [70, 40, 64, 130], [3, 0, 640, 257], width_extra=PROMPT,
+                    hide=[(2, 1, -1), (2, 7, 10 ** 9), (2, 20, -7), (3, 0, -1), (3, 16, -1)])
+
+
+@pytest.mark.parametrize("kind,q_scale", [("bf16", 1e-30), ("bf16", 1e4), ("f16", 1e-3), ("f16", 30.0), ("bf16", 0.0)])
+def test_attention_of_prompts_of_small_and_large_queries(kind, q_scale):
+    rng = np.random.default_rng(5)
+    check_attention(rng, 2, 4, 128, 16, kind, [100, 30], [300, 90], q_scale=q_scale, width_extra=PROMPT)
+
+
+def test_attention_of_prompts_with_scales_far_apart():
+    """Value scales over 12 orders of magnitude and scales of 0: the tolerance follows the weighted magnitudes."""
+    rng = np.random.default_rng(8)
+    cache = list(make_cache(rng, 40, 2, 16, 128))
+    cache[3] *= (10.0 ** rng.integers(-6, 7, cache[3].shape)).astype(np.float32)
+    for at in ((3, 0), (7, 1), (11, 0), (12, 0), (13, 0)):
+        cache[3][at] = 0.0
+        cache[1][at] = 0
+    cache[2][5, 0] = 0.0
+    cache[0][5, 0] = 0
+    start, ctx, table = [0, 200], [640], np.concatenate([rng.permutation(40), -np.ones(4000, int)])[None]
+    q = torch.from_numpy(rng.standard_normal((200, 4, 128)).astype(np.float32)).to(torch.bfloat16)
+    for rows in (q, q[:3]):  # the kernel for prompts and the one for few rows
+        start[1] = len(rows)
+        out, lse = run_attention(cache, rows, "bf16", start, ctx, table, 0.09)
+        want, want_lse, tol, lse_tol = plain_attention(cache, rows.double().numpy(), start, ctx, table, 0.09, True, 0)
+        assert (np.abs(out - want) <= tol + 2.0 ** -8 * np.abs(want)).all() and (np.abs(lse - want_lse) <= lse_tol).all()
+
+
 def test_attention_rows_that_see_nothing_and_pages_that_are_gone():
     rng = np.random.default_rng(11)
     # more queries than tokens (the first ones stand before the first token), an empty cache, hidden pages
