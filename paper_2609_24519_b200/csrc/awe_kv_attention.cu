@@ -234,39 +234,43 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             const int tok = tok0 + i * kStepTokens;
             if (i >= n_tiles || tok >= r.ctx) return -1;
             const int page = table[tok >> p.page_log2];
-            return page < 0 || page >= p.n_pages ? -1 : page;
+            return (unsigned)page < (unsigned)p.n_pages ? page : -1;
         };
+        // tiles of 16 tokens lie one behind the other in the pools, a page and head's together
+        const int tile_log2 = p.page_log2 - 4, tile_mask = (1 << tile_log2) - 1;
+        const int8_t *k_from = p.k + 16 * lane, *v_from = p.v + 16 * lane;
+        const float* scale_from = lane == 0 ? p.k_scale : p.v_scale;
+        uint32_t write_at = ring;
         auto fetch = [&](int i, int page) {
-            if (i < n_tiles) {
-                const uint32_t stage = ring + (i % C::kStages) * C::kStageBytes;
-                if (page >= 0) {
-                    const int64_t block = (int64_t)page * p.heads + head;
-                    const int place = (tok0 + i * kStepTokens) & ((1 << p.page_log2) - 1);
-                    const int64_t off = ((block << p.page_log2) + place) * kD;
+            if (page >= 0) {
+                const uint32_t block = (uint32_t)page * p.heads + head;
+                const uint64_t off = (uint64_t)((block << tile_log2) + (((tok0 + i * kStepTokens) >> 4) & tile_mask)) * (16 * kD);
+                const int8_t *k_at = k_from + off, *v_at = v_from + off;
 #pragma unroll
-                    for (int j = 0; j < kD / 32; ++j) {
-                        const int c = lane + 32 * j;
-                        const uint32_t dst = stage + piece_at<kD>(c / (kD / 16), c % (kD / 16));
-                        cp_async16(dst, p.k + off + 16 * c, 16);
-                        cp_async16(dst + 16 * kD, p.v + off + 16 * c, 16);
-                    }
-                    if (lane == 0) cp_async4(stage + 32 * kD, p.k_scale + block);
-                    if (lane == 1) cp_async4(stage + 32 * kD + 4, p.v_scale + block);
+                for (int j = 0; j < kD / 32; ++j) {
+                    const int c = lane + 32 * j;
+                    const uint32_t dst = write_at + piece_at<kD>(c / (kD / 16), c % (kD / 16));
+                    cp_async16_whole(dst, k_at + 512 * j);
+                    cp_async16_whole(dst + 16 * kD, v_at + 512 * j);
                 }
-                if (lane == 2) asm volatile("st.shared.b32 [%0], %1;" ::"r"(stage + 32 * kD + 8), "r"(page) : "memory");
+                if (lane < 2) cp_async4(write_at + 32 * kD + 4 * lane, scale_from + block);
             }
+            if (lane == 2) asm volatile("st.shared.b32 [%0], %1;" ::"r"(write_at + 32 * kD + 8), "r"(page) : "memory");
             cp_async_commit();
+            write_at = write_at + C::kStageBytes == ring + C::kStages * C::kStageBytes ? ring : write_at + C::kStageBytes;
         };
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < C::kStages - 1; ++i) fetch(i, page_of(i));
         int next_page = page_of(C::kStages - 1);
 
+        uint32_t read_at = ring;
         for (int i = 0; i < n_tiles; ++i) {
             cp_async_wait<C::kStages - 2>();
             __syncwarp();
             fetch(i + C::kStages - 1, next_page);
             next_page = page_of(i + C::kStages);
-            const uint32_t ks_at = ring + (i % C::kStages) * C::kStageBytes, vs_at = ks_at + 16 * kD;
+            const uint32_t ks_at = read_at, vs_at = ks_at + 16 * kD;
+            read_at = read_at + C::kStageBytes == ring + C::kStages * C::kStageBytes ? ring : read_at + C::kStageBytes;
             if ((int)lds32(ks_at + 32 * kD + 8) < 0) continue;
             const float ks = __uint_as_float(lds32(ks_at + 32 * kD)), vs = __uint_as_float(lds32(ks_at + 32 * kD + 4));
 
@@ -278,7 +282,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                 const uint4 a = lds128(ks_at + piece_at<kD>(g, piece)), b8 = lds128(ks_at + piece_at<kD>(g + 8, piece));
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const uint32_t x = (&a.x)[w] ^ 0x80808080u, y = (&b8.x)[w] ^ 0x80808080u;
+                    const uint32_t x = flip_signs((&a.x)[w]), y = flip_signs((&b8.x)[w]);
                     const uint32_t f[4] = {bytes_to_half2(x, 0x4140), bytes_to_half2(y, 0x4140), bytes_to_half2(x, 0x4342),
                                            bytes_to_half2(y, 0x4342)};
 #pragma unroll
@@ -363,8 +367,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                 }
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
-                    const uint32_t x0 = v[0][w] ^ 0x80808080u, x1 = v[1][w] ^ 0x80808080u, y0 = v[2][w] ^ 0x80808080u,
-                                   y1 = v[3][w] ^ 0x80808080u;
+                    const uint32_t x0 = flip_signs(v[0][w]), x1 = flip_signs(v[1][w]), y0 = flip_signs(v[2][w]), y1 = flip_signs(v[3][w]);
 #pragma unroll
                     for (int pair = 0; pair < 2; ++pair) {
                         const uint32_t sel = pair ? 0x7362 : 0x5140;

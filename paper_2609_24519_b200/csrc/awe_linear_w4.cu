@@ -65,7 +65,7 @@ __device__ __forceinline__ void unpack_word(uint32_t w, uint32_t offset, uint32_
         const __nv_bfloat162 off = *reinterpret_cast<const __nv_bfloat162*>(&offset);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t v = ((w >> (4 * i)) & 0x000F000Fu) ^ 0x43084308u;
+            const uint32_t v = and_xor(w >> (4 * i), 0x000F000Fu, 0x43084308u);
             const __nv_bfloat162 h = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), off);
             f[i] = *reinterpret_cast<const uint32_t*>(&h);
         }
@@ -73,7 +73,7 @@ __device__ __forceinline__ void unpack_word(uint32_t w, uint32_t offset, uint32_
         const __half2 off = *reinterpret_cast<const __half2*>(&offset), off16 = *reinterpret_cast<const __half2*>(&offset16);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t lo = (w & 0x000F000Fu) ^ 0x64086408u, hi = (w & 0x00F000F0u) ^ 0x64806480u;
+            const uint32_t lo = and_xor(w, 0x000F000Fu, 0x64086408u), hi = and_xor(w, 0x00F000F0u, 0x64806480u);
             const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&lo), off);
             const __half2 b = __hfma2(*reinterpret_cast<const __half2*>(&hi), __float2half2_rn(0.0625f), off16);
             f[2 * i] = *reinterpret_cast<const uint32_t*>(&a);
@@ -351,9 +351,9 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     const int tiles_m = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
     // Parts of K: as many blocks as stay within four per SM (what is resident at once), with two stages each at least.
     const int64_t tiles = (p.N + kRowsN - 1) / kRowsN * ((M + 8 * tiles_m - 1) / (8 * tiles_m));
-    int parts = 1;
-    while (parts < kMaxCluster && 2 * tiles * parts <= 4 * h->sm_count && p.K > 2 * parts * 2 * kStageK) parts *= 2;
+    int parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, 4 * h->sm_count / tiles, p.K / (2 * kStageK)}));
     p.k_per_block = (int)round_up((p.K + parts - 1) / parts, kStageK);
+    parts = (p.K + p.k_per_block - 1) / p.k_per_block;
     const bool bf16 = x_type == AWE_BF16;
     const cudaError_t e = tiles_m == 1   ? launch<1>(p, bf16, aligned, parts, st)
                           : tiles_m == 2 ? launch<2>(p, bf16, aligned, parts, st)

@@ -100,7 +100,7 @@ __device__ __forceinline__ void unpack_in_order(uint32_t w, uint32_t offset, uin
         const uint32_t w4 = w >> 4;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const uint32_t v = (__byte_perm(w, w4, 0x4400 + 0x1111 * b) & 0x000F000Fu) ^ 0x43084308u;
+            const uint32_t v = and_xor(__byte_perm(w, w4, 0x4400 + 0x1111 * b), 0x000F000Fu, 0x43084308u);
             const __nv_bfloat162 h = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), off);
             f[b] = *reinterpret_cast<const uint32_t*>(&h);
         }
@@ -109,7 +109,7 @@ __device__ __forceinline__ void unpack_in_order(uint32_t w, uint32_t offset, uin
         const uint32_t mul = 0x2C003C00u;  // (1, 1/16)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const uint32_t v = (__byte_perm(w, 0x64u, 0x4040 + 0x0101 * b) & 0xFFF0FF0Fu) ^ 0x00800008u;
+            const uint32_t v = and_xor(__byte_perm(w, 0x64u, 0x4040 + 0x0101 * b), 0xFFF0FF0Fu, 0x00800008u);
             const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&mul), off);
             f[b] = *reinterpret_cast<const uint32_t*>(&h);
         }
@@ -584,10 +584,10 @@ awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, boo
     if (p.x_tma && (s = make_map_2d(h, x, false, W.K, M, M == 1 ? round_up(2 * W.K, 16) : 2 * ldx, 64, mt, CU_TENSOR_MAP_SWIZZLE_128B, &mx)) != AWE_OK)
         return s;
     // Parts of K: as many blocks as are resident at once, with two stages each at least.
-    const int64_t tiles = (W.N + kRowsN - 1) / kRowsN * ((M + mt - 1) / mt), room = h->sm_count;
-    int parts = 1;
-    while (parts < kMaxCluster && 2 * tiles * parts <= room && W.K > 2 * parts * 2 * kStageK) parts *= 2;
+    const int64_t tiles = (W.N + kRowsN - 1) / kRowsN * ((M + mt - 1) / mt);
+    int parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, h->sm_count / tiles, W.K / (2 * kStageK)}));
     p.k_per_block = (int)round_up((W.K + parts - 1) / parts, kStageK);
+    parts = (int)((W.K + p.k_per_block - 1) / p.k_per_block);
     switch (mt) {
         case 16: return launch<16>(h, mc, mx, p, bf16, aligned, parts, st);
         case 32: return launch<32>(h, mc, mx, p, bf16, aligned, parts, st);

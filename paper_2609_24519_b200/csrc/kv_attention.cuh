@@ -41,9 +41,16 @@ struct Deal {
 // Four signed bytes as two pairs of FP16: the byte with its sign bit flipped is u = x + 128, the FP16 pattern
 // 0x6400 | u is 1024 + u, and subtracting 1152 is exact.
 __device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped, uint32_t selector) {
-    const uint32_t w = __byte_perm(flipped, 0x64646464u, selector);
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(1152.0f));
-    return *reinterpret_cast<const uint32_t*>(&h);
+    uint32_t w, h;
+    asm("prmt.b32 %0, %1, 0x64646464, %2;" : "=r"(w) : "r"(flipped), "r"(selector));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(w), "r"(0x64806480u));
+    return h;
+}
+// The four bytes' sign bits flipped.  Volatile: left to itself the compiler flips them after the permutations, twice as often.
+__device__ __forceinline__ uint32_t flip_signs(uint32_t w) {
+    uint32_t f;
+    asm volatile("xor.b32 %0, %1, 0x80808080;" : "=r"(f) : "r"(w));
+    return f;
 }
 
 // Prompts: the tcgen05 kernel; the arguments have been checked, p's pointers into the workspace are not set.
