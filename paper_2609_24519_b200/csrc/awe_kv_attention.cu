@@ -30,6 +30,7 @@ using namespace serve;
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStepTokens = 16 * kWarps;
+constexpr int kWholeTokens = 256;
 
 // The steps of one request: tokens [lo, hi) in steps of kStepTokens, for each of `units` units.
 struct Request {
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             int64_t w = 0;
             if (b < p.B) {
                 const Request r = request_of<kRows>(p, b);
-                w = (int64_t)r.units * r.steps;
+                w = p.whole ? r.units : (int64_t)r.units * r.steps;
             }
             int64_t inc = w;
 #pragma unroll
@@ -132,15 +133,15 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     float4* join_stat = reinterpret_cast<float4*>(join_vec + kWarps * kRows * C::kVecPitch);
 
     for (int64_t pos = begin; pos < end;) {
-        while (pos >= at + (int64_t)r.units * r.steps) {
-            at += (int64_t)r.units * r.steps;
+        while (pos >= at + (p.whole ? r.units : (int64_t)r.units * r.steps)) {
+            at += p.whole ? r.units : (int64_t)r.units * r.steps;
             r = request_of<kRows>(p, ++b);
         }
-        const int unit = (int)((pos - at) / r.steps), step0 = (int)((pos - at) % r.steps);
-        const int step1 = (int)min((int64_t)r.steps, step0 + end - pos);
+        const int unit = p.whole ? (int)(pos - at) : (int)((pos - at) / r.steps), step0 = p.whole ? 0 : (int)((pos - at) % r.steps);
+        const int step1 = p.whole ? r.steps : (int)min((int64_t)r.steps, step0 + end - pos);
         const int head = unit % p.heads, row0 = unit / p.heads * kRows, n_rows = min(kRows, r.n * p.group - row0);
         const int32_t* table = p.table + (int64_t)b * p.ld_table;
-        pos += step1 - step0;
+        pos += p.whole ? 1 : step1 - step0;
 
         // ---- the query rows, as the matrix instruction's 16 x 8 operand: thread (g, t) holds of row g the
         // dimensions whose cache pieces it reads.  BF16 rows are scaled by a power of two so that FP16 holds them.
@@ -274,24 +275,51 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             if ((int)lds32(ks_at + 32 * kD + 8) < 0) continue;
             const float ks = __uint_as_float(lds32(ks_at + 32 * kD)), vs = __uint_as_float(lds32(ks_at + 32 * kD + 4));
 
-            // scores of 16 tokens (rows g, g + 8) and the query rows (columns 2t, 2t + 1)
-            float s[kNT][4];
+            // what the tile holds, all of it on its way before the first product waits for any: keys of the tokens g, g + 8,
+            // values of the thread's kD / 8 dimensions of the tokens 2t, 2t + 1, 2t + 8, 2t + 9
+            constexpr int kValueParts = kD == 256 ? 2 : 1, kWords = kD == 64 ? 2 : 4;
+            uint4 ka[kD / 64], kb[kD / 64];
+            uint32_t v[kValueParts][4][kWords];
 #pragma unroll
             for (int c = 0; c < kD / 64; ++c) {
                 const int piece = kD == 64 ? t : 8 * (c >> 1) + 2 * t + (c & 1);
-                const uint4 a = lds128(ks_at + piece_at<kD>(g, piece)), b8 = lds128(ks_at + piece_at<kD>(g + 8, piece));
+                ka[c] = lds128(ks_at + piece_at<kD>(g, piece)), kb[c] = lds128(ks_at + piece_at<kD>(g + 8, piece));
+            }
+#pragma unroll
+            for (int c = 0; c < kValueParts; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int row = 2 * t + (j & 1) + 8 * (j >> 1);
+                    if constexpr (kD == 64) {
+                        const uint2 x = lds64(vs_at + piece_at<kD>(row, g >> 1) + 8 * (g & 1));
+                        v[c][j][0] = x.x, v[c][j][1] = x.y;
+                    } else {
+                        const uint4 x = lds128(vs_at + piece_at<kD>(row, g + 8 * c));
+                        v[c][j][0] = x.x, v[c][j][1] = x.y, v[c][j][2] = x.z, v[c][j][3] = x.w;
+                    }
+                }
+
+            // scores of 16 tokens (rows g, g + 8) and the query rows (columns 2t, 2t + 1), in two sums that do not wait for each other
+            float s[kNT][4], s_odd[kNT][4];
+#pragma unroll
+            for (int c = 0; c < kD / 64; ++c) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const uint32_t x = flip_signs((&a.x)[w]), y = flip_signs((&b8.x)[w]);
+                    const uint32_t x = flip_signs((&ka[c].x)[w]), y = flip_signs((&kb[c].x)[w]);
                     const uint32_t f[4] = {bytes_to_half2(x, 0x4140), bytes_to_half2(y, 0x4140), bytes_to_half2(x, 0x4342),
                                            bytes_to_half2(y, 0x4342)};
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt) {
-                        if (c == 0 && w == 0) mma_16816_zero<false>(s[nt], f, qf[nt][0][0], qf[nt][0][1]);
-                        else mma_16816<false>(s[nt], f, qf[nt][4 * c + w][0], qf[nt][4 * c + w][1]);
+                        float(&to)[4] = w & 1 ? s_odd[nt] : s[nt];
+                        if (c == 0 && w < 2) mma_16816_zero<false>(to, f, qf[nt][w][0], qf[nt][w][1]);
+                        else mma_16816<false>(to, f, qf[nt][4 * c + w][0], qf[nt][4 * c + w][1]);
                     }
                 }
             }
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[nt][j] += s_odd[nt][j];
 
             const int tile = tok0 + i * kStepTokens, tok = tile + g;
             uint32_t pf[kNT][2];
@@ -349,25 +377,11 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                     pf[nt][half] = movmatrix_trans(w);  // thread (g, t): row g, tokens 2t, 2t + 1 (+ 8 half)
                 }
 
-            // values: thread (g, t) reads its kD / 8 dimensions of the tokens 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-            for (int c = 0; c < (kD == 256 ? 2 : 1); ++c) {
-                constexpr int kWords = kD == 64 ? 2 : 4;
-                uint32_t v[4][kWords];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int row = 2 * t + (j & 1) + 8 * (j >> 1);
-                    if constexpr (kD == 64) {
-                        const uint2 x = lds64(vs_at + piece_at<kD>(row, g >> 1) + 8 * (g & 1));
-                        v[j][0] = x.x, v[j][1] = x.y;
-                    } else {
-                        const uint4 x = lds128(vs_at + piece_at<kD>(row, g + 8 * c));
-                        v[j][0] = x.x, v[j][1] = x.y, v[j][2] = x.z, v[j][3] = x.w;
-                    }
-                }
+            for (int c = 0; c < kValueParts; ++c) {
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
-                    const uint32_t x0 = flip_signs(v[0][w]), x1 = flip_signs(v[1][w]), y0 = flip_signs(v[2][w]), y1 = flip_signs(v[3][w]);
+                    const uint32_t x0 = flip_signs(v[c][0][w]), x1 = flip_signs(v[c][1][w]), y0 = flip_signs(v[c][2][w]), y1 = flip_signs(v[c][3][w]);
 #pragma unroll
                     for (int pair = 0; pair < 2; ++pair) {
                         const uint32_t sel = pair ? 0x7362 : 0x5140;
@@ -559,6 +573,7 @@ cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
     cudaError_t e = allow_smem(kv_attention_kernel<kD, kNT, kBf16>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
+    if (p.whole) return cudaSuccess;
     const int64_t items = p.T * p.heads * p.group;
     return launch_early(kv_attention_join_kernel<kD, kNT, kBf16>, dim3((unsigned)((items + kWarps - 1) / kWarps)), kThreads, 0, st, p);
 }
@@ -615,10 +630,15 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     if (use_tc(*cache, T, B, n_q_heads, group, max_pages * cache->page_size, window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, workspace_dev, (cudaStream_t)stream);
     p.blocks = blocks_of(h->sm_count, cache->head_dim, nt);
+    // Short contexts: a block per unit and no second launch (777 tokens of 8 heads: 9.0 us in parts with the join).
+    int64_t tokens = max_pages * cache->page_size;
+    if (window > 0) tokens = std::min(tokens, window + T / B + kStepTokens);
+    p.whole = tokens <= kWholeTokens;
     const Workspace w = workspace_of(p.blocks, 8 * nt, cache->head_dim, B);
     p.unit_steps = (int64_t*)workspace_dev;
     p.part_vec = (float*)((uint8_t*)workspace_dev + w.vec);
     p.part_stat = (float4*)((uint8_t*)workspace_dev + w.stat);
+    if (p.whole) p.blocks = (int)std::min<int64_t>((T * group / (8 * nt) + B) * cache->n_heads, INT32_MAX);
     auto run = [&](auto dim, auto tiles) {
         constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
         return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)
@@ -632,6 +652,6 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     else
         e = nt == 2 ? run(integral_constant<int, 64>(), integral_constant<int, 2>()) : run(integral_constant<int, 64>(), integral_constant<int, 1>());
     if (e != cudaSuccess) return AWE_ERR_CUDA;
-    h->launches += 2;
+    h->launches += p.whole ? 1 : 2;
     return AWE_OK;
 }

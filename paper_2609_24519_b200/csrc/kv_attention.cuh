@@ -20,6 +20,7 @@ struct AttnParams {
     float scale_log2;     // scale / ln 2
     int B, heads, group, page_log2, n_pages, max_pages, causal, blocks;
     int64_t window;
+    int whole;            // a block per unit, which nothing cuts
 };
 
 // The steps are dealt out to the blocks in order, as evenly as whole numbers go: the first `extra` blocks take one more.
@@ -46,12 +47,7 @@ __device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped, uint32_t se
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(w), "r"(0x64806480u));
     return h;
 }
-// The four bytes' sign bits flipped.  Volatile: left to itself the compiler flips them after the permutations, twice as often.
-__device__ __forceinline__ uint32_t flip_signs(uint32_t w) {
-    uint32_t f;
-    asm volatile("xor.b32 %0, %1, 0x80808080;" : "=r"(f) : "r"(w));
-    return f;
-}
+__device__ __forceinline__ uint32_t flip_signs(uint32_t w) { return w ^ 0x80808080u; }  // of four bytes
 
 // Prompts: the tcgen05 kernel; the arguments have been checked, p's pointers into the workspace are not set.
 size_t kv_attention_tc_workspace_bytes(awe_ctx* h, int64_t T, int64_t n_q_heads, int64_t B, int64_t head_dim);
