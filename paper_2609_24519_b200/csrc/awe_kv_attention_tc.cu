@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
 #pragma unroll
                         for (int i = 0; i < kD / 8; ++i) {
                             const uint4 x = __ldg(reinterpret_cast<const uint4*>(src) + i);
-                            m = __vmaxu2(__vmaxu2(__vmaxu2(m, x.x & 0x7FFF7FFFu), x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
+                            m = __vimax3_u16x2(__vimax3_u16x2(m, x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu);
                         }
                     }
                     const int e = min(max((int)(max(m & 0xFFFFu, m >> 16) >> 7) - 127, -120), 120);

@@ -16,7 +16,7 @@ namespace {
 using namespace serve;
 
 constexpr int kThreads = 128;
-constexpr int kHeld = 4;  // 16-byte pieces a thread keeps in registers between the two passes
+constexpr int kHeld = 8;  // 16-byte pieces a thread keeps in registers between the two passes
 
 struct WriteParams {
     const void *k, *v;
@@ -44,9 +44,8 @@ __device__ __forceinline__ uint4 load8(const typename Half<kBf16>::type* x) {
 // Two unsigned maxima of 16-bit magnitudes: the patterns of finite values order like the values, and a maximum of
 // kInfinity or more says that an infinity or a NaN is among them.
 __device__ __forceinline__ uint32_t largest8(uint4 w, uint32_t m) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, (&w.x)[i] & 0x7FFF7FFFu);
-    return m;
+    m = __vimax3_u16x2(m, w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu);
+    return __vimax3_u16x2(m, w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu);
 }
 template <bool kBf16>
 __device__ __forceinline__ uint32_t largest_finite8(uint4 w, uint32_t m) {
@@ -124,25 +123,28 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
         if (!begins) break;
         t0 = t32 - 32 + __ffs(begins) - 1;
         const int64_t page = page_of(t0);
-        const int place = (int)(p.slots[t0] & (page_size - 1));
-        // the run: the tokens of the same page that follow
+        const int64_t slot0 = p.slots[t0];
+        const int place = (int)(slot0 & (page_size - 1));
+        // the run: the tokens of the same page that follow, and whether they follow place by place
         int n = 1;
+        bool in_order = true;
         while (true) {
-            const int64_t t = t0 + n + lane;
-            const unsigned ok = __ballot_sync(~0u, t < p.T && page_of(t) == page);
+            const int64_t t = t0 + n + lane, slot = t < p.T ? p.slots[t] : -1;
+            const unsigned ok = __ballot_sync(~0u, slot >= 0 && slot < p.n_slots && slot >> p.page_log2 == page);
+            const unsigned next = __ballot_sync(~0u, slot == slot0 + n + lane);
             const int more = ok == ~0u ? 32 : __ffs(~ok) - 1;
+            in_order = in_order && (~next & (more == 32 ? ~0u : (1u << more) - 1u)) == 0;
             n += more;
             if (more < 32) break;
         }
-        const T16* row0 = x + t0 * ldx + (int64_t)head * dim;
-        const int pieces = n << per_row_log2;
-        auto piece = [&](int i) { return row0 + (int64_t)(i >> per_row_log2) * ldx + ((i & ((1 << per_row_log2) - 1)) << 3); };
+        // this thread's pieces: column `col` of the rows row, row + step, ... (a power of two of pieces per row divides the block)
+        const int pieces = n << per_row_log2, row = tid >> per_row_log2, col = (tid & ((1 << per_row_log2) - 1)) << 3, step = kThreads >> per_row_log2;
+        const T16* first = x + (t0 + row) * ldx + (int64_t)head * dim + col;
+        auto piece = [&](int j) { return first + (int64_t)j * step * ldx; };  // the j-th
         uint4 held[kHeld];
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) {
-            const int i = tid + j * kThreads;
-            held[j] = i < pieces ? load8<kBf16, kVec>(piece(i)) : make_uint4(0, 0, 0, 0);
-        }
+        for (int j = 0; j < kHeld; ++j)
+            held[j] = tid + j * kThreads < pieces ? load8<kBf16, kVec>(piece(j)) : make_uint4(0, 0, 0, 0);
         float* scale = scales + page * p.heads + head;
         const float before = place > 0 ? *scale : 0.0f;
         auto block_max = [&](uint32_t m) {
@@ -157,14 +159,14 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
         uint32_t top = 0;
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) top = largest8(held[j], top);
-        for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) top = largest8(load8<kBf16, kVec>(piece(i)), top);
+        for (int j = kHeld; tid + j * kThreads < pieces; ++j) top = largest8(load8<kBf16, kVec>(piece(j)), top);
         top = block_max(top);
         const bool finite = top < kInfinity;
         if (!finite) {
             top = 0;
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) top = largest_finite8<kBf16>(held[j], top);
-            for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) top = largest_finite8<kBf16>(load8<kBf16, kVec>(piece(i)), top);
+            for (int j = kHeld; tid + j * kThreads < pieces; ++j) top = largest_finite8<kBf16>(load8<kBf16, kVec>(piece(j)), top);
             top = block_max(top);
         }
         const float m = Half<kBf16>::unpack(top).x;
@@ -177,15 +179,17 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
             uint32_t* old = reinterpret_cast<uint32_t*>(block);
             for (int i = tid; i < place << (p.dim_log2 - 2); i += kThreads) old[i] = rescale4(old[i], ratio);
         }
-        auto out = [&](int i) {
-            const int at = (int)(p.slots[t0 + (i >> per_row_log2)] & (page_size - 1));
-            return reinterpret_cast<uint2*>(block + (at << p.dim_log2)) + (i & ((1 << per_row_log2) - 1));
+        int8_t* to = block + (place << p.dim_log2) + 8 * tid;  // where the places follow, the pieces do
+        auto out = [&](int j) {
+            if (in_order) return reinterpret_cast<uint2*>(to + 8 * kThreads * j);
+            const int at = (int)(p.slots[t0 + row + j * step] & (page_size - 1));
+            return reinterpret_cast<uint2*>(block + (at << p.dim_log2) + col);
         };
         auto store = [&](auto quantise_piece) {
 #pragma unroll
             for (int j = 0; j < kHeld; ++j)
-                if (tid + j * kThreads < pieces) *out(tid + j * kThreads) = quantise_piece(held[j]);
-            for (int i = tid + kHeld * kThreads; i < pieces; i += kThreads) *out(i) = quantise_piece(load8<kBf16, kVec>(piece(i)));
+                if (tid + j * kThreads < pieces) *out(j) = quantise_piece(held[j]);
+            for (int j = kHeld; tid + j * kThreads < pieces; ++j) *out(j) = quantise_piece(load8<kBf16, kVec>(piece(j)));
         };
         if (finite) store([&](uint4 w) { return quantise8<kBf16>(w, inverse); });
         else store([&](uint4 w) { return quantise8_any<kBf16>(w, inverse); });

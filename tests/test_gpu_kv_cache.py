@@ -171,6 +171,21 @@ def test_write(heads, dim, page, kind, offset):
             assert np.array_equal(want, got.cpu().numpy())
 
 
+def test_write_with_places_left_out():
+    """Tokens of a page that leave places out: those keep what they had."""
+    rng = np.random.default_rng(1)
+    heads, dim, page, n_pages = 2, 64, 32, 3
+    slots = [2 * page, 2 * page + 1, 2 * page + 5, 2 * page + 31, 4, 6, 7]
+    x = torch.from_numpy(rng.standard_normal((len(slots), heads * dim)).astype(np.float32)).to(torch.float16)
+    cache, scale = rng.integers(-127, 128, (n_pages, heads, page, dim)).astype(np.int8), np.full((n_pages, heads), 0.01, np.float32)
+    dev = [cuda(cache), cuda(cache), cuda(scale), cuda(scale)]
+    b.awe_kv_write(handle(), b.kv_cache(*dev, n_pages, heads, page, dim), x.cuda(), x.cuda(), b.F16, len(slots), heads * dim, heads * dim,
+                   cuda(np.array(slots, np.int64)))
+    plain_write(cache, scale, x.float().numpy().reshape(-1, heads, dim), slots, page)
+    for want, got in zip((cache, cache, scale, scale), dev):
+        assert np.array_equal(want, got.cpu().numpy())
+
+
 def test_write_many_tokens_is_within_half_a_step():
     rng = torch.Generator(device="cuda").manual_seed(3)
     T, heads, dim, page = 20000, 4, 128, 32
