@@ -7,10 +7,12 @@
 // rows of the weight, its columns 8 rows of x.  With few rows of x the weight's bytes (K / 2 per row, read once) are
 // the bound.
 //
-// A block takes 64 rows of the weight and a part of K; up to 8 blocks along K form a cluster and add their sums
-// through each other's shared memory in a fixed order.  Each of its four warps has 16 rows and a ring of its own: a
-// stage is 256 k of the codes (cp.async, 16 bytes a piece), and the stage that begins a slab (1,024 to 4,096 k) brings the slab's
-// scales and zero points along, so that a warp waits for nobody but itself within a slab.  Thread (g, t) of a warp reads
+// A warp takes 16 rows of the weight and a part of K.  One or two rows of x: a block of eight warps cuts K into 1, 2, 4 or 8
+// slices and adds them at its end (4,096 x 4,096 for one row: 8.2 -> 5.2 us a call, since a launch of clusters takes longer
+// than the product).  Otherwise a block is four warps with 64 rows that share x, and up to 8 blocks along K form a cluster
+// and add their sums through each other's shared memory.  All sums are added in a fixed order.  A warp has a ring of its own:
+// a stage is 256 k of the codes (cp.async, 16 bytes a piece), and the stage that begins a slab (512 to 4,096 k) brings the
+// slab's scales and zero points along, so that a warp waits for nobody but itself within a slab.  Thread (g, t) of a warp reads
 // 8 consecutive k of its rows as one word; which k takes which place in the instruction does not matter as long as x
 // is placed alike, so codes are used in the order in which they unpack: (0,4), (1,5), (2,6), (3,7).
 #include <cooperative_groups.h>
@@ -24,10 +26,8 @@ namespace {
 
 using namespace serve;
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
+constexpr int kSliceWarps = 8, kShareWarps = 4;  // warps of a block that cuts K, or shares x
 constexpr int kWarpRows = 16;
-constexpr int kRowsN = kWarpRows * kWarps;  // rows of the weight per block
 constexpr int kStageK = 256;                // k per stage
 constexpr int kPitch = kStageK / 2 + 16;    // bytes per row and stage: the last 16 hold what an unaligned row spills over, and
                                             // make 8 rows x 4 words hit all banks
@@ -35,9 +35,8 @@ constexpr int kStageBytes = kWarpRows * kPitch;
 constexpr int kStages = 3;
 constexpr int kZeroBytes = kStageK * 2 + 128;  // read in the place of rows of x that do not exist
 constexpr int kMaxCluster = 8;
-constexpr int kSlabK = 1024;     // k whose x, scales and zero points are held at a time: this or, for few rows of x,
-constexpr int kSlabKMost = 4096; // two or four times as many
-constexpr int kSumPitch = kRowsN + 4;        // floats
+constexpr int kSlabKMost = 4096;   // k whose x, scales and zero points are held at a time, at most
+constexpr int kXMost = 17 * 1024;  // bytes of x of the slabs of a block, about
 
 struct LinearParams {
     const uint8_t* codes;
@@ -46,7 +45,7 @@ struct LinearParams {
     const void* x;
     void* y;
     int64_t row_bytes, ldx, ldy;
-    int M, N, K, group_log2, groups, k_per_block;
+    int M, N, K, group_log2, groups, k_per_block, k_per_slice, slice_log2, slab_count;
     int scale_bf16, y_f32, x_vec;
     int scale_pitch, zero_pitch;  // bytes of a row's scales and zero points of a slab, with room for what an unaligned row spills over
     int ring_at, slab_at;         // byte offsets in shared memory: x first
@@ -83,16 +82,22 @@ __device__ __forceinline__ void unpack_word(uint32_t w, uint32_t offset, uint32_
     }
 }
 
-template <int kMT, int kGroupSteps, bool kBf16, bool kAligned>
-__global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams p) {
+template <int kWarps, int kMT, int kGroupSteps, bool kBf16, bool kAligned>
+__global__ void __launch_bounds__(32 * kWarps) linear_w4_kernel(const LinearParams p) {
+    constexpr int kThreads = 32 * kWarps;
     namespace cg = cooperative_groups;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * kRowsN, m0 = blockIdx.z * 8 * kMT, k0 = blockIdx.y * p.k_per_block;
-    const int k1 = min(p.K, k0 + p.k_per_block), n_stages = k1 > k0 ? (k1 - k0 + kStageK - 1) / kStageK : 0;
+    grid_wait();
+    // this warp: 16 rows, a slice of k
+    const int slice_log2 = kWarps == kShareWarps ? 0 : p.slice_log2;
+    const int row_warps = kWarps >> slice_log2, slice = warp / row_warps, row_warp = warp % row_warps, block_rows = kWarpRows * row_warps;
+    const int n0 = blockIdx.x * block_rows, m0 = blockIdx.z * 8 * kMT, k0 = blockIdx.y * p.k_per_block + slice * p.k_per_slice;
+    const int k1 = min(p.K, min(k0 + p.k_per_slice, (int)(blockIdx.y + 1) * p.k_per_block)), n_stages = k1 > k0 ? (k1 - k0 + kStageK - 1) / kStageK : 0;
     const int rows_m = min(8 * kMT, p.M - m0), slab_k = p.slab_stages * kStageK, x_pitch = slab_k * 2 + 64;
     // Rows of the weight below the last one are computed from the last one and not written.
-    const int n_warp = n0 + warp * kWarpRows;
+    const int n_warp = n0 + row_warp * kWarpRows;
+    uint8_t* x_slab = smem + slice * rows_m * x_pitch;
     auto row_of = [&](int row) { return (int64_t)min(n_warp + row, p.N - 1); };
     const uint32_t smem_at = (uint32_t)__cvta_generic_to_shared(smem), ring = smem_at + p.ring_at + warp * kStages * kStageBytes;
     const int slab_bytes = kWarpRows * (p.scale_pitch + p.zero_pitch);
@@ -130,24 +135,24 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
         }
         cp_async_commit();
     };
-    // x for [k0 + at, + slab_k), zeros behind the block's part of K: the warps take pieces of 1,024 k of a row in turn
+    // x for [k0 + at, + slab_k), zeros behind the slice: the slice's warps take four pieces of 256 k in turn
     auto load_x = [&](int at) {
         const int n_k = min(slab_k, k1 - k0 - at), n_round = (n_k + kStageK - 1) / kStageK * kStageK;
-        for (int j = warp; j < rows_m * (slab_k / kSlabK); j += kWarps) {
-            const int row = j / (slab_k / kSlabK), from = j % (slab_k / kSlabK) * kSlabK;
-            const uint16_t* src = reinterpret_cast<const uint16_t*>(p.x) + (m0 + row) * p.ldx + k0 + at;
-            uint4 w[kSlabK / kStageK];
+        const int slab_log2 = __ffs(p.slab_stages) - 1;
+        for (int j0 = 4 * row_warp; j0 < rows_m * p.slab_stages; j0 += 4 * row_warps) {
+            uint4 w[4];
 #pragma unroll
-            for (int u = 0; u < kSlabK / kStageK; ++u) {
-                const int k = from + 8 * lane + u * kStageK;
-                w[u] = load_x8(src + min(k, n_k), p.x_vec, n_k - k);
+            for (int u = 0; u < 4; ++u) {
+                const int row = (j0 + u) >> slab_log2, k = ((j0 + u) & (p.slab_stages - 1)) * kStageK + 8 * lane;
+                const uint16_t* src = reinterpret_cast<const uint16_t*>(p.x) + (m0 + min(row, rows_m - 1)) * p.ldx + k0 + at;
+                w[u] = load_x8(src + min(k, n_k), p.x_vec, row < rows_m ? n_k - k : 0);
             }
 #pragma unroll
-            for (int u = 0; u < kSlabK / kStageK; ++u) {
-                const int k = from + 8 * lane + u * kStageK;
+            for (int u = 0; u < 4; ++u) {
+                const int row = (j0 + u) >> slab_log2, k = ((j0 + u) & (p.slab_stages - 1)) * kStageK + 8 * lane;
                 // pairs (0,4), (1,5), (2,6), (3,7)
-                if (k < n_round)
-                    *reinterpret_cast<uint4*>(smem + row * x_pitch + k * 2) =
+                if (row < rows_m && k < n_round)
+                    *reinterpret_cast<uint4*>(x_slab + row * x_pitch + k * 2) =
                         make_uint4(__byte_perm(w[u].x, w[u].z, 0x5410), __byte_perm(w[u].x, w[u].z, 0x7632),
                                    __byte_perm(w[u].y, w[u].w, 0x5410), __byte_perm(w[u].y, w[u].w, 0x7632));
             }
@@ -165,7 +170,7 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
 #pragma unroll
     for (int mt = 0; mt < kMT; ++mt) {
         const bool live = 8 * mt + g < rows_m;
-        x_row[mt] = smem_at + (live ? (8 * mt + g) * x_pitch : p.ring_at - kZeroBytes) + 16 * t;
+        x_row[mt] = smem_at + (live ? (slice * rows_m + 8 * mt + g) * x_pitch : p.ring_at - kZeroBytes) + 16 * t;
         x_mask[mt] = live ? ~0u : 0u;
     }
     // where rows g, g + 8 of the warp start inside their first 16 bytes of codes
@@ -176,18 +181,19 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
     constexpr int kScales = kStageK / 32 / kGroupSteps;  // of a stage
     uint32_t scale_a = 0, scale_b = 0, zero_a = 0, zero_b = 0;
 
-    for (int i = 0; i < n_stages; ++i) {
-        if ((i & (p.slab_stages - 1)) == 0) {
-            if (i) __syncthreads();
-            load_x(i * kStageK);
-            const uint32_t slab = slab_of(i), zeros = slab + kWarpRows * p.scale_pitch;
-            const int64_t at_a = row_of(row_a) * p.groups + ((k0 + i * kStageK) >> p.group_log2), at_b = row_of(row_b) * p.groups + ((k0 + i * kStageK) >> p.group_log2);
+    for (int begin = 0; begin < p.slab_count * p.slab_stages; begin += p.slab_stages) {  // slabs: as many for every warp
+        if (begin) __syncthreads();
+        if (begin < n_stages) {
+            load_x(begin * kStageK);
+            const uint32_t slab = slab_of(begin), zeros = slab + kWarpRows * p.scale_pitch;
+            const int64_t at_a = row_of(row_a) * p.groups + ((k0 + begin * kStageK) >> p.group_log2), at_b = row_of(row_b) * p.groups + ((k0 + begin * kStageK) >> p.group_log2);
             scale_a = slab + row_a * p.scale_pitch + ((uint32_t)(uintptr_t)(p.scale + 2 * at_a) & 15);
             scale_b = slab + row_b * p.scale_pitch + ((uint32_t)(uintptr_t)(p.scale + 2 * at_b) & 15);
             zero_a = zeros + row_a * p.zero_pitch + ((uint32_t)(uintptr_t)(p.zero + at_a) & 15);
             zero_b = zeros + row_b * p.zero_pitch + ((uint32_t)(uintptr_t)(p.zero + at_b) & 15);
-            __syncthreads();
         }
+        __syncthreads();
+    for (int i = begin; i < min(n_stages, begin + p.slab_stages); ++i) {
         cp_async_wait<kStages - 2>();
         __syncwarp();
         fetch(i + kStages - 1);
@@ -240,29 +246,36 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
             }
         }
     }
+    }
     cp_async_wait<0>();
     __syncthreads();
 
-    // ---- sums to shared memory as (row of x, row of the weight), then the cluster's blocks add them
+    // ---- sums to shared memory as (slice, row of x, row of the weight); the block, then the cluster, adds them
     float* sums = reinterpret_cast<float*>(smem);
+    const int pitch = block_rows + 4, slices = 1 << slice_log2;
 #pragma unroll
     for (int mt = 0; mt < kMT; ++mt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sums[(8 * mt + 2 * t + (j & 1)) * kSumPitch + warp * kWarpRows + (j >> 1 ? row_b : row_a)] = total[mt][j];
+        for (int j = 0; j < 4; ++j)
+            sums[(slice * 8 * kMT + 8 * mt + 2 * t + (j & 1)) * pitch + row_warp * kWarpRows + (j >> 1 ? row_b : row_a)] = total[mt][j];
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     if (parts > 1) cluster.sync();
     else __syncthreads();
     const float* from[kMaxCluster];
 #pragma unroll
-    for (int r = 0; r < kMaxCluster; ++r) from[r] = r < parts ? cluster.map_shared_rank(sums, r) : sums;
-    for (int j = rank * kThreads + tid; j < rows_m * kRowsN; j += parts * kThreads) {
-        const int m = j / kRowsN, n = j % kRowsN;
+    for (int r = 0; r < kMaxCluster; ++r) from[r] = kWarps == kShareWarps && r < parts ? cluster.map_shared_rank(sums, r) : sums;
+    for (int j = rank * kThreads + tid; j < rows_m * block_rows; j += parts * kThreads) {
+        const int m = j / block_rows, n = j % block_rows;
         if (n0 + n >= p.N) continue;
         float v = 0.0f;
+        if constexpr (kWarps == kShareWarps) {
 #pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r)
-            if (r < parts) v += from[r][m * kSumPitch + n];
+            for (int r = 0; r < kMaxCluster; ++r)
+                if (r < parts) v += from[r][m * pitch + n];
+        } else {
+            for (int i = 0; i < slices; ++i) v += sums[(i * 8 * kMT + m) * pitch + n];
+        }
         const int64_t at = (int64_t)(m0 + m) * p.ldy + n0 + n;
         if (p.y_f32) reinterpret_cast<float*>(p.y)[at] = v;
         else reinterpret_cast<typename Half<kBf16>::type*>(p.y)[at] = Half<kBf16>::from_float(v);
@@ -270,47 +283,52 @@ __global__ void __launch_bounds__(kThreads) linear_w4_kernel(const LinearParams 
     if (parts > 1) cluster.sync();  // no block leaves while its sums are read
 }
 
-template <int kMT, int kGroupSteps, bool kBf16, bool kAligned>
+template <int kWarps, int kMT, int kGroupSteps, bool kBf16, bool kAligned>
 cudaError_t launch(LinearParams p, int parts, cudaStream_t st) {
-    // Shared memory: x of a slab (and at the end the sums in its place), the rings, the slabs' scales and zeros twice.
-    const int rows = std::min(p.M, 8 * kMT), slab_k = rows == 1 ? 4 * kSlabK : (rows <= 3 ? 2 * kSlabK : kSlabK);
+    constexpr int kThreads = 32 * kWarps;
+    // Shared memory: x of the slices' slabs (and at the end the sums in its place), the rings, the slabs' scales and zeros.
+    const int rows = std::min(p.M, 8 * kMT), slices = 1 << p.slice_log2, block_rows = kWarpRows * kWarps / slices;
+    int slab_k = (kStages - 1) * kStageK;  // two slabs' worth of stages are under way at most
+    while (slab_k < kSlabKMost && slab_k < p.k_per_slice && 2 * slab_k * 2 * rows * slices <= kXMost) slab_k *= 2;
     const int slab_groups = std::max(1, slab_k >> p.group_log2);
     p.slab_stages = slab_k / kStageK;
+    p.slab_count = (p.k_per_slice + slab_k - 1) / slab_k;
     p.scale_pitch = (int)round_up(2 * slab_groups, 16) + 16;
     p.zero_pitch = p.zero ? (int)round_up(slab_groups, 16) + 16 : 0;
-    p.slabs = p.k_per_block > slab_k ? 2 : 1;
-    p.ring_at = (int)round_up(std::max(rows * (slab_k * 2 + 64), 8 * kMT * kSumPitch * 4) + kZeroBytes, 128);
+    p.slabs = p.slab_count > 1 ? 2 : 1;
+    p.ring_at = (int)round_up(std::max(slices * rows * (slab_k * 2 + 64), slices * 8 * kMT * (block_rows + 4) * 4) + kZeroBytes, 128);
     p.slab_at = p.ring_at + kWarps * kStages * kStageBytes;
     const int smem = p.slab_at + kWarps * p.slabs * kWarpRows * (p.scale_pitch + p.zero_pitch);
-    constexpr int kMost = std::max(8 * kMT * (kSlabK * 2 + 64), kSlabKMost * 2 + 64) + kZeroBytes + 128 + kWarps * kStages * kStageBytes +
-                          kWarps * 2 * kWarpRows * (kSlabKMost / 32 * 3 + 32);
-    static_assert(kMost <= 227 * 1024, "shared memory of a block");
+    constexpr int kMost = 227 * 1024;
+    static_assert(kMT * 8 * ((kStages - 1) * kStageK * 2 + 64) + kXMost + kWarps * 2 * kWarpRows * (kSlabKMost / 32 * 3 + 32) / (kMT > 1 ? 4 : 1) + kZeroBytes + 128 + kWarps * kStages * kStageBytes <= kMost, "shared memory of a block");
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = allow_smem(linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, kMost, p.device, done);
+    const cudaError_t e = allow_smem(linear_w4_kernel<kWarps, kMT, kGroupSteps, kBf16, kAligned>, kMost, p.device, done);
     if (e != cudaSuccess) return e;
+    const dim3 grid((p.N + block_rows - 1) / block_rows, parts, (p.M + 8 * kMT - 1) / (8 * kMT));
+    if (parts == 1) return launch_early(linear_w4_kernel<kWarps, kMT, kGroupSteps, kBf16, kAligned>, grid, kThreads, smem, st, p);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((p.N + kRowsN - 1) / kRowsN, parts, (p.M + 8 * kMT - 1) / (8 * kMT));
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr = cluster_attribute(parts);
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, linear_w4_kernel<kMT, kGroupSteps, kBf16, kAligned>, p);
+    return cudaLaunchKernelEx(&cfg, linear_w4_kernel<kWarps, kMT, kGroupSteps, kBf16, kAligned>, p);
 }
-template <int kMT, int kGroupSteps>
+template <int kWarps, int kMT, int kGroupSteps>
 cudaError_t launch(const LinearParams& p, bool bf16, bool aligned, int parts, cudaStream_t st) {
     if (bf16)
-        return aligned ? launch<kMT, kGroupSteps, true, true>(p, parts, st) : launch<kMT, kGroupSteps, true, false>(p, parts, st);
-    return aligned ? launch<kMT, kGroupSteps, false, true>(p, parts, st) : launch<kMT, kGroupSteps, false, false>(p, parts, st);
+        return aligned ? launch<kWarps, kMT, kGroupSteps, true, true>(p, parts, st) : launch<kWarps, kMT, kGroupSteps, true, false>(p, parts, st);
+    return aligned ? launch<kWarps, kMT, kGroupSteps, false, true>(p, parts, st) : launch<kWarps, kMT, kGroupSteps, false, false>(p, parts, st);
 }
-template <int kMT>
+template <int kWarps, int kMT>
 cudaError_t launch(const LinearParams& p, bool bf16, bool aligned, int parts, cudaStream_t st) {
     switch (p.group_log2) {
-        case 5: return launch<kMT, 1>(p, bf16, aligned, parts, st);
-        case 6: return launch<kMT, 2>(p, bf16, aligned, parts, st);
-        case 7: return launch<kMT, 4>(p, bf16, aligned, parts, st);
-        default: return launch<kMT, 8>(p, bf16, aligned, parts, st);
+        case 5: return launch<kWarps, kMT, 1>(p, bf16, aligned, parts, st);
+        case 6: return launch<kWarps, kMT, 2>(p, bf16, aligned, parts, st);
+        case 7: return launch<kWarps, kMT, 4>(p, bf16, aligned, parts, st);
+        default: return launch<kWarps, kMT, 8>(p, bf16, aligned, parts, st);
     }
 }
 
@@ -349,15 +367,25 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     if ((M > 8 && W->N >= 2048) || (M > 16 && M <= 64))
         return linear_w4_tc(h, *W, x_dev, x_type == AWE_BF16, M, ldx, y_dev, y_type == AWE_F32, ldy, st);
     const int tiles_m = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
-    // Parts of K: as many blocks as stay within four per SM (what is resident at once), with two stages each at least.
-    const int64_t tiles = (p.N + kRowsN - 1) / kRowsN * ((M + 8 * tiles_m - 1) / (8 * tiles_m));
-    int parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, 4 * h->sm_count / tiles, p.K / (2 * kStageK)}));
-    p.k_per_block = (int)round_up((p.K + parts - 1) / parts, kStageK);
-    parts = (p.K + p.k_per_block - 1) / p.k_per_block;
-    const bool bf16 = x_type == AWE_BF16;
-    const cudaError_t e = tiles_m == 1   ? launch<1>(p, bf16, aligned, parts, st)
-                          : tiles_m == 2 ? launch<2>(p, bf16, aligned, parts, st)
-                                         : launch<4>(p, bf16, aligned, parts, st);
+    // K is split so that about 16 warps per SM have work (what is resident at once), with two stages each at least.
+    const int64_t warps = (p.N + kWarpRows - 1) / kWarpRows * ((M + 8 * tiles_m - 1) / (8 * tiles_m));
+    const int split = (int)std::max<int64_t>(1, std::min<int64_t>({kSliceWarps * kMaxCluster, 16 * h->sm_count / warps, p.K / (2 * kStageK)}));
+    const bool bf16 = x_type == AWE_BF16, sliced = M <= 2 && split <= kSliceWarps;
+    int parts = 1;
+    if (sliced) {
+        while ((1 << p.slice_log2) < split) ++p.slice_log2;
+        p.k_per_slice = (int)round_up((p.K + (1 << p.slice_log2) - 1) >> p.slice_log2, kStageK);
+    } else {
+        const int64_t tiles = (p.N + kWarpRows * kShareWarps - 1) / (kWarpRows * kShareWarps) * ((M + 8 * tiles_m - 1) / (8 * tiles_m));
+        parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, 4 * h->sm_count / tiles, p.K / (2 * kStageK)}));
+        p.k_per_slice = (int)round_up((p.K + parts - 1) / parts, kStageK);
+        parts = (p.K + p.k_per_slice - 1) / p.k_per_slice;
+    }
+    p.k_per_block = p.k_per_slice << p.slice_log2;
+    const cudaError_t e = sliced         ? launch<kSliceWarps, 1>(p, bf16, aligned, parts, st)
+                          : tiles_m == 1 ? launch<kShareWarps, 1>(p, bf16, aligned, parts, st)
+                          : tiles_m == 2 ? launch<kShareWarps, 2>(p, bf16, aligned, parts, st)
+                                         : launch<kShareWarps, 4>(p, bf16, aligned, parts, st);
     if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;
