@@ -416,7 +416,7 @@ size_t awe_kv_attention_workspace_bytes(awe_handle_t h, const awe_kv_cache* cach
  * requests: request b has the queries q_start[b] .. q_start[b+1] - 1, which are its last ones of ctx_len[b]
  * tokens.  Query head i reads cache head i / (n_q_heads / n_heads).  causal: a query sees the tokens up to its own
  * position, else all ctx_len[b]; window > 0 (causal only): the last `window` of those.  A query that sees nothing gets zeros and
- * lse = -inf.  A table entry outside the pool hides its tokens.  q_dev: T x n_q_heads x head_dim of type AWE_F16 or AWE_BF16 with token stride
+ * lse = -inf; rows behind the last request's queries are left as they are.  The scales of the cache are not negative.  A table entry outside the pool hides its tokens.  q_dev: T x n_q_heads x head_dim of type AWE_F16 or AWE_BF16 with token stride
  * ldq, out_dev alike with ldo; lse_dev (T x n_q_heads floats, natural logarithm of the sum of exponentials) may
  * be NULL.  q_dev and out_dev 16-B aligned, ldq and ldo multiples of 8.  workspace_dev: 256-B aligned. */
 awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const void* q_dev, awe_float_t type,

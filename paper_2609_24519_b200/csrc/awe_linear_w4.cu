@@ -346,7 +346,7 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
         W->scale_type < AWE_F16 || W->scale_type > AWE_F32)
         return AWE_ERR_INVALID_ARG;
     if (!is_half_type(x_type) || !is_half_type(W->scale_type) || (y_type != x_type && y_type != AWE_F32)) return AWE_ERR_UNSUPPORTED;
-    if (W->N > INT32_MAX - 256 || W->K > INT32_MAX - 4096 || M > 65535 * 8) return AWE_ERR_UNSUPPORTED;
+    if (W->N > INT32_MAX - 256 || W->K > INT32_MAX - 65536 || M > 65535 * 8) return AWE_ERR_UNSUPPORTED;
     if (M == 0) return AWE_OK;
     if (!x_dev || !y_dev || (M > 1 && (ldx < W->K || ldy < W->N))) return AWE_ERR_INVALID_ARG;
     if ((uintptr_t)x_dev % 2 || (uintptr_t)W->scale_dev % 2 || (uintptr_t)y_dev % (y_type == AWE_F32 ? 4 : 2)) return AWE_ERR_ALIGNMENT;
