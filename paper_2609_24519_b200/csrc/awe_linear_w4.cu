@@ -360,11 +360,11 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     p.x_vec = (uintptr_t)x_dev % 16 == 0 && (ldx % 8 == 0 || M == 1);
     const bool aligned = (uintptr_t)W->codes_dev % 16 == 0 && W->ld % 32 == 0;
     cudaStream_t st = (cudaStream_t)stream;
-    // tcgen05 pays where its 128 x 16 to 128 x 128 tiles are many enough or x has more rows than one or two columns blocks of
-    // the small instruction: M = 128, 8,192 x 8,192: 38 us against 175; M = 16, 4,096 x 4,096: 9.4 against 10.3; M = 32, 1,024 x
-    // 1,024: 8.8 against 11.0.  Below that the small kernel has less to set up: M = 1, 8,192 x 8,192: 16.6 us against 22.6;
-    // M = 16, 1,024 x 1,024: 6.8 against 7.6; M = 96, 1,024 x 1,024: 11.0 against 17.6.
-    if ((M > 8 && W->N >= 2048) || (M > 16 && M <= 64))
+    // tcgen05 pays where its 128 x 16 to 128 x 128 tiles are many enough, x has more rows than one or two column blocks of the
+    // small instruction, or many rows meet a long K: M = 128, 8,192 x 8,192: 41 us against 175; M = 16, 4,096 x 4,096: 9.4
+    // against 10.3; M = 128, N = 1,024, K = 8,192: 16 against 27.  Below that the small kernel has less to set up: M = 1,
+    // 8,192 x 8,192: 16.6 us against 22.6; M = 16, 1,024 x 1,024: 5.8 against 7.8; M = 96, 1,024 x 1,024: 8.3 against 10.3.
+    if ((M > 8 && W->N >= 2048) || (M > 16 && M <= 64) || (M > 64 && W->K >= 4096))
         return linear_w4_tc(h, *W, x_dev, x_type == AWE_BF16, M, ldx, y_dev, y_type == AWE_F32, ldy, st);
     const int tiles_m = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
     // K is split so that about 16 warps per SM have work (what is resident at once), with two stages each at least.

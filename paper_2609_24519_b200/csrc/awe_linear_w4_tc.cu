@@ -537,26 +537,46 @@ awe_status_t make_map_2d(awe_ctx* h, const void* at, bool bytes, int64_t inner, 
 }
 
 template <int kMt, bool kBf16, bool kAligned>
-awe_status_t launch(awe_ctx* h, const CUtensorMap& mc, const CUtensorMap& mx, const TcParams& p, int parts, cudaStream_t st) {
+awe_status_t launch(awe_ctx* h, const CUtensorMap& mc, const CUtensorMap& mx, TcParams p, cudaStream_t st) {
     using C = Config<kMt, kAligned>;
     static std::atomic<uint64_t> done{0};
     if (allow_smem(linear_w4_tc_kernel<kMt, kBf16, kAligned>, C::kSmemBytes, h->device, done) != cudaSuccess) return AWE_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((p.N + kRowsN - 1) / kRowsN, parts, (p.M + kMt - 1) / kMt);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = C::kSmemBytes;
     cfg.stream = st;
-    cudaLaunchAttribute attr = cluster_attribute(parts);
+    cudaLaunchAttribute attr = {};
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
+    // Parts of K: as many as leave every tile's cluster resident at once, with two stages per block at least.  Fewer clusters of 8
+    // fit than the SMs have room for (128 blocks in 16 clusters of 8 take 20 us where 16 of 4 take 12), so the runtime is
+    // asked, once per size.
+    const dim3 tiles((p.N + kRowsN - 1) / kRowsN, 1, (p.M + kMt - 1) / kMt);
+    static std::atomic<int> fit[kMaxCluster + 1];  // clusters of each size that are resident at once, plus 1
+    int parts = std::max(1, std::min(kMaxCluster, p.K / (2 * kStageK)));
+    for (; parts > 1; --parts) {
+        if ((int64_t)tiles.x * tiles.z * parts > h->sm_count) continue;
+        int n = fit[parts].load(std::memory_order_relaxed) - 1;
+        if (n < 0) {
+            attr = cluster_attribute(parts);
+            cfg.gridDim = dim3(1, parts, 1);
+            if (cudaOccupancyMaxActiveClusters(&n, linear_w4_tc_kernel<kMt, kBf16, kAligned>, &cfg) != cudaSuccess) return AWE_ERR_CUDA;
+            fit[parts].store(n + 1, std::memory_order_relaxed);
+        }
+        if ((int64_t)tiles.x * tiles.z <= n) break;
+    }
+    p.k_per_block = (int)round_up((p.K + parts - 1) / parts, kStageK);
+    parts = (p.K + p.k_per_block - 1) / p.k_per_block;
+    attr = cluster_attribute(parts);
+    cfg.gridDim = dim3(tiles.x, parts, tiles.z);
     if (cudaLaunchKernelEx(&cfg, linear_w4_tc_kernel<kMt, kBf16, kAligned>, mc, mx, p) != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;
 }
 template <int kMt>
-awe_status_t launch(awe_ctx* h, const CUtensorMap& mc, const CUtensorMap& mx, const TcParams& p, bool bf16, bool aligned, int parts, cudaStream_t st) {
-    if (bf16) return aligned ? launch<kMt, true, true>(h, mc, mx, p, parts, st) : launch<kMt, true, false>(h, mc, mx, p, parts, st);
-    return aligned ? launch<kMt, false, true>(h, mc, mx, p, parts, st) : launch<kMt, false, false>(h, mc, mx, p, parts, st);
+awe_status_t launch(awe_ctx* h, const CUtensorMap& mc, const CUtensorMap& mx, const TcParams& p, bool bf16, bool aligned, cudaStream_t st) {
+    if (bf16) return aligned ? launch<kMt, true, true>(h, mc, mx, p, st) : launch<kMt, true, false>(h, mc, mx, p, st);
+    return aligned ? launch<kMt, false, true>(h, mc, mx, p, st) : launch<kMt, false, false>(h, mc, mx, p, st);
 }
 
 }  // namespace
@@ -576,23 +596,21 @@ awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, boo
     p.zero_pitch = p.zero ? (int)round_up(slab_groups, 16) + 16 : 0;
     p.status = h->status_dev;
     const bool aligned = (uintptr_t)W.codes_dev % 16 == 0 && W.ld % 32 == 0;
-    const int mt = M <= 16 ? 16 : (M <= 32 ? 32 : (M <= 64 ? 64 : 128));
+    // Above 64 rows the taller tile unpacks a weight once for 128 rows, and pays once its tiles are many: 8,192 x 8,192 for 128
+    // rows 41 us against 47 with 64, but 2,048 x 4,096 28 against 13.
+    int mt = M <= 16 ? 16 : (M <= 32 ? 32 : 64);
+    if (M > 64 && (W.N + kRowsN - 1) / kRowsN * ((M + 127) / 128) > 32) mt = 128;
     CUtensorMap mc = {}, mx = {};
     awe_status_t s;
     if (aligned && (s = make_map_2d(h, W.codes_dev, true, (W.K + 1) / 2, W.N, W.ld / 2, kStageK / 2, kRowsN, CU_TENSOR_MAP_SWIZZLE_128B, &mc)) != AWE_OK)
         return s;
     if (p.x_tma && (s = make_map_2d(h, x, false, W.K, M, M == 1 ? round_up(2 * W.K, 16) : 2 * ldx, 64, mt, CU_TENSOR_MAP_SWIZZLE_128B, &mx)) != AWE_OK)
         return s;
-    // Parts of K: as many blocks as are resident at once, with two stages each at least.
-    const int64_t tiles = (W.N + kRowsN - 1) / kRowsN * ((M + mt - 1) / mt);
-    int parts = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, h->sm_count / tiles, W.K / (2 * kStageK)}));
-    p.k_per_block = (int)round_up((W.K + parts - 1) / parts, kStageK);
-    parts = (int)((W.K + p.k_per_block - 1) / p.k_per_block);
     switch (mt) {
-        case 16: return launch<16>(h, mc, mx, p, bf16, aligned, parts, st);
-        case 32: return launch<32>(h, mc, mx, p, bf16, aligned, parts, st);
-        case 64: return launch<64>(h, mc, mx, p, bf16, aligned, parts, st);
-        default: return launch<128>(h, mc, mx, p, bf16, aligned, parts, st);
+        case 16: return launch<16>(h, mc, mx, p, bf16, aligned, st);
+        case 32: return launch<32>(h, mc, mx, p, bf16, aligned, st);
+        case 64: return launch<64>(h, mc, mx, p, bf16, aligned, st);
+        default: return launch<128>(h, mc, mx, p, bf16, aligned, st);
     }
 }
 
