@@ -9,8 +9,11 @@
 // Scales.  The keys' scale of 16 tokens of a page multiplies the scores in FP32.  The values' scale vs is folded into P as
 // an addition to the exponent: P = exp2(s + log2 vs - m) with m within 8 of the largest s + log2 vs seen so far, so
 // that P rounds to FP16 as well as it can for what it contributes, whatever the scales; the divisor is the sum of
-// P / vs in FP32.  (A page whose values are all zero has scale 0: any other scale serves it, the step's largest is taken.)
+// 2^-12 P / vs in FP32 (the power of two keeps it in range for every scale that the cache write stores, 2^-107 to 2^121).
 // m moves only when a score passes it by more than 2^8, which rescales O in tensor memory; that is rare after the first step.
+// Tokens whose page has value scale 0 stand for zeros whatever their bytes, and weigh in the divisor alone: their P is 0, so that
+// they neither add to O nor move m, and their exponentials are summed apart, against a maximum of their own, in a pass that only
+// steps with such pages take; the two sums meet at the end.
 //
 // All steps of all units in a row are dealt out evenly to one block per SM; units that were cut are joined by a second
 // kernel in the order of the tokens.  A small kernel before lists the units' steps, which causality makes uneven.
@@ -121,11 +124,17 @@ __global__ void __launch_bounds__(kPlanThreads) kv_attention_units_kernel(const 
     if (threadIdx.x == 0) p.tile_steps[tiles] = sum;
 }
 
+constexpr int kSharedBytes = 3 * 1024;  // room for Shared
+constexpr float kDivisorUnit = 1.0f / 4096, kDivisorLog2 = 12.0f;
+
 template <int kD>
 struct Config {
     static constexpr int kQBytes = 128 * kD * 2, kKBytes = kStep * kD * 2;  // of one tile
     static constexpr int kQAt = 0, kKAt = 2 * kQBytes, kVAt = kKAt + 2 * kKBytes, kEnd = kVAt + 2 * kKBytes;
-    static constexpr int kNeeded = 1024 + kEnd + 1024;
+    // 195 KB for dimension 128, and no more: with the 1 KB that every block has besides, 196 KB of the SM's 256 are shared memory
+    // and the rest caches the loads; the next larger split costs 12 us of 374 (2,048 queries of 8,192 tokens).
+    static constexpr int kNeeded = kEnd + kSharedBytes;
+    static_assert(kD != 128 || kNeeded <= 195 * 1024, "split of the SM's memory");
     // A block takes all of tensor memory, so a second one must not fit beside it.
     static constexpr int kSmemBytes = kNeeded > 120 * 1024 ? kNeeded : 120 * 1024;
 };
@@ -135,8 +144,11 @@ struct Shared {
     uint64_t c_full[4];  // constants of a step: four of them, so that no softmax warp can fall a round behind
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
-    float4 constants[4][kStep / 16];  // of 16 tokens: key scale, log2 of the value scale, its reciprocal
+    float4 constants[4][kStep / 16];  // of 16 tokens: key scale, log2 of the value scale, kDivisorUnit over it
+    uint32_t unvalued[4];             // of a step: which 16 tokens have value scale 0
+    float2 unvalued_sum[kRows];       // of a query row over those: reference, sum of the exponentials
 };
+static_assert(sizeof(Shared) <= kSharedBytes, "shared memory behind the tiles");
 
 // Descriptor of an operand whose rows run along the contraction: 64 columns (128 bytes) per row, 128-byte swizzle, 8-row
 // groups 1024 bytes apart, blocks of 64 columns `block_bytes` apart.
@@ -154,14 +166,45 @@ __device__ __noinline__ bool wait_long(volatile uint32_t* abort_flag, uint32_t b
     return gemm::bounded_wait_ns(abort_flag, bar, parity, status, site, gemm::kWaitLimitNs);
 }
 
+// The factor of 16 tokens' scores.  It is not negative, and not 0, so that a hidden score stays -inf under it.
+__device__ __forceinline__ float factor_of(float key_scale, float cq) { return fmaxf(key_scale * cq, 1.17549435e-38f); }
+
+// Adds the exponentials of a step's tokens whose page has value scale 0 (`groups`: which 16 of them) to a query row's sum of
+// those; the row's scores lie in tensor memory at `scores`, it sees the step's tokens [lo, hi).
+__device__ __forceinline__ void add_unvalued(Shared* sh, uint32_t groups, int slot, uint32_t scores, int row, int lo, int hi, float cq) {
+    float2 own = sh->unvalued_sum[row];
+#pragma unroll 1
+    for (int g = 0; g < kStep / 16; ++g, lo -= 16, hi -= 16) {
+        if (!(groups >> g & 1)) continue;
+        uint32_t v[16];
+        ptx::tmem_ld_32x16(scores + 16 * g, v);
+        ptx::tmem_wait_ld();
+        if (lo < min(hi, 16) && hi > 0) {  // this row sees some of them
+            const float a = factor_of(sh->constants[slot][g].x, cq);
+            float m = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (e < lo || e >= hi) v[e] = 0xFF800000u;
+                m = fmaxf(m, __uint_as_float(v[e]));
+            }
+            m = fmaxf(own.x, m * a);
+            own.y *= exp2_approx(own.x - m);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) own.y += exp2_approx(fmaf(__uint_as_float(v[e]), a, -m));
+            own.x = m;
+        }
+        __syncwarp();
+    }
+    sh->unvalued_sum[row] = own;
+}
+
 template <int kD, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
     using C = Config<kD>;
     using T16 = typename Half<kBf16>::type;
     const AttnParams& p = tp.a;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = ptx::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    uint8_t* smem = smem_raw + (base - raw);
+    extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles
+    const uint32_t base = ptx::smem_u32(smem);
     Shared* sh = reinterpret_cast<Shared*>(smem + C::kEnd);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -332,9 +375,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 if (!__all_sync(~0u, wait(sh->k_empty[step & 1], ((step >> 1) & 1) ^ 1, 34))) return false;
                 store(base + C::kKAt + (step & 1) * C::kKBytes, kr);
                 if (warp == kSoftWarps) {
-                    const float top = __uint_as_float(__reduce_max_sync(~0u, lane < kStep / 16 ? __float_as_uint(scale.y) : 0u));
-                    const float vs = scale.y > 0.0f ? scale.y : (top > 0.0f ? top : 1.0f);
-                    if (lane < kStep / 16) sh->constants[step & 3][lane] = page >= 0 ? make_float4(scale.x, log2f(vs), 1.0f / vs, 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+                    const bool valued = page >= 0 && scale.y != 0.0f;
+                    const uint32_t unvalued = __ballot_sync(~0u, page >= 0 && scale.y == 0.0f);  // lanes that have no tokens have no page
+                    if (lane < kStep / 16) sh->constants[step & 3][lane] = make_float4(scale.x, valued ? log2f(scale.y) : -INFINITY, valued ? kDivisorUnit / scale.y : 0.0f, 0.0f);
+                    if (lane == 0) sh->unvalued[step & 3] = unvalued;
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh->c_full[step & 3]));
                 }
@@ -412,6 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             if (!live || see_hi < 0) see_hi = 0;
             const int all_lo = __reduce_max_sync(~0u, live ? see_lo : 0), all_hi = __reduce_min_sync(~0u, live ? see_hi : 0x7FFFFFFF);
             float m_ref = -INFINITY, sum = 0.0f;
+            sh->unvalued_sum[128 * t + row] = make_float2(-INFINITY, 0.0f);  // this thread's alone
             for (int j = s0; j < s1; ++j, ++step, ++done) {
                 const int tok0 = u.lo + j * kStep;
                 const bool cut = tok0 < all_lo || tok0 + kStep > all_hi;
@@ -438,8 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                     for (int e = 0; e < 32; ++e)
                         if (e < lo || e >= hi) v[e] = 0xFF800000u;
                 };
-                // The factor of 16 tokens' scores.  It is not negative, and not 0, so that a hidden score stays -inf under it.
-                auto factor = [&](const float4& k) { return fmaxf(k.x * cq, 1.17549435e-38f); };
+                auto factor = [&](const float4& k) { return factor_of(k.x, cq); };
                 float top = -INFINITY;  // the largest exponent: of each piece the largest score decides
                 for_pieces([&](int g, uint32_t (&v)[32]) {
                     if (cut) hide(g, v);
@@ -453,12 +497,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                     }
                 });
                 const bool first = m_ref == -INFINITY;
-                if (__any_sync(~0u, top > (first ? -INFINITY : m_ref + 8.0f))) {
+                const bool grows = top > (first ? -INFINITY : m_ref + 8.0f);
+                const uint32_t unvalued = sh->unvalued[step & 3];
+                if (__any_sync(~0u, grows || unvalued)) {  // one branch on the way of most steps: with two they take 0.6 % longer
+                    if (unvalued) add_unvalued(sh, unvalued, step & 3, s_at[t] + lanes, 128 * t + row, see_lo - tok0, see_hi - tok0, cq);
                     const float before = m_ref;
                     m_ref = fmaxf(m_ref, top);
                     const float shrink = first || m_ref == before ? 1.0f : exp2_approx(before - m_ref);
                     sum *= shrink;
-                    if (j > s0) {  // O once the products of the step before are in it
+                    if (j > s0 && __any_sync(~0u, shrink != 1.0f)) {  // O once the products of the step before are in it
                         if (!__all_sync(~0u, wait(sh->o_done[t], (done - 1) & 1, 38))) return false;
                         ptx::tc_fence_after();
 #pragma unroll 1
@@ -502,7 +549,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             ptx::tc_fence_after();
             const bool whole = s0 == 0 && s1 == u.steps;
             const int64_t token = u.q0 + query, part_row = ((int64_t)2 * blockIdx.x + (s0 == 0)) * kRows + 128 * t + row;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            // sum is relative to m_ref + kDivisorLog2; with the other tokens' sum relative to the larger reference
+            float m_all = m_ref + kDivisorLog2, keep = kDivisorUnit;  // keep: what brings O to that reference
+            if (const float2 own = sh->unvalued_sum[128 * t + row]; own.y != 0.0f) {
+                const float m = fmaxf(m_all, own.x), a = exp2_approx(m_all - m);
+                sum = fmaf(sum, a, own.y * exp2_approx(own.x - m));
+                keep *= a;
+                m_all = m;
+            }
+            const float inv = sum == 0.0f ? 0.0f : keep / sum;
             T16* dst = reinterpret_cast<T16*>(p.out) + token * p.ldo + (int64_t)qh * kD;
 #pragma unroll 1
             for (int c = 0; c < kD; c += 32) {
@@ -520,15 +575,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                                                                             Half<kBf16>::pack(f[4] * inv, f[5] * inv), Half<kBf16>::pack(f[6] * inv, f[7] * inv));
                     } else {
                         float4* to = reinterpret_cast<float4*>(p.part_vec + part_row * kD + c + e);
-                        to[0] = make_float4(f[0], f[1], f[2], f[3]);
-                        to[1] = make_float4(f[4], f[5], f[6], f[7]);
+                        to[0] = make_float4(f[0] * keep, f[1] * keep, f[2] * keep, f[3] * keep);
+                        to[1] = make_float4(f[4] * keep, f[5] * keep, f[6] * keep, f[7] * keep);
                     }
                 }
             }
             ptx::tc_fence_before();
             if (live) {
-                if (!whole) p.part_stat[part_row] = make_float4(m_ref, sum, 0.0f, 0.0f);
-                else if (p.lse) p.lse[token * p.heads * p.group + qh] = sum == 0.0f ? -INFINITY : (m_ref + log2f(sum)) * 0.69314718056f;
+                if (!whole) p.part_stat[part_row] = make_float4(m_all, sum, 0.0f, 0.0f);
+                else if (p.lse) p.lse[token * p.heads * p.group + qh] = sum == 0.0f ? -INFINITY : (m_all + log2f(sum)) * 0.69314718056f;
             }
             return true;
         });

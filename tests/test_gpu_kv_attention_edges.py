@@ -1,0 +1,133 @@
+"""Attention over the 8-bit cache where it can go wrong: scales of 0, windows over prompts, places that nothing may read.
+
+The reference is the definition in 64 bits.  Tolerance, with u the unit roundoff of the output type, A = sum_j p_j |v_j|, S the
+largest sum of magnitudes behind a visible score and e = 2 (D / 16 + 3) 2^-22 S (FP32 sums of D / 16 matrix steps): the
+softmax weights, times the values' scale in the kernel for prompts, are rounded to FP16 relative to their largest so far, which
+costs 2^-11 of each or, below FP16's normal range, `floor` of the largest; each carries an integer of at most 128, so
+  |out - ref| <= u |ref| + (2^-11 + e) (A + |ref|) + n floor 128 max vs,   |lse - ref| <= e + 2^-21 (1 + |ref|).
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_24519_b200 import binding as b
+from tests.gpu_util import handle
+from tests.test_gpu_kv_cache import TYPES, make_cache, run_attention
+
+pytestmark = pytest.mark.gpu
+
+WIDE = 40000  # tokens that a block table could hold: with many queries, what the library takes for prompts
+
+
+def reference(cache, q, start, ctx, table, scale, causal, window):
+    """out, lse, A, S, n max vs; rows that see nothing have 0, -inf, 0, 0, 0."""
+    k, v, ks, vs = cache
+    n_pages, heads, page, dim = k.shape
+    T, Hq, _ = q.shape
+    group = Hq // heads
+    out, A, lse = np.zeros((T, Hq, dim)), np.zeros((T, Hq, dim)), np.full((T, Hq), -np.inf)
+    S, n_vs = np.zeros((T, Hq)), np.zeros((T, Hq))
+    for i, length in enumerate(ctx):
+        a, n = int(start[i]), int(start[i + 1] - start[i])
+        tok = np.arange(min(length, table.shape[1] * page))
+        if not n or not len(tok):
+            continue
+        entry = table[i, tok // page]
+        fine = (entry >= 0) & (entry < n_pages)
+        entry = np.where(fine, entry, 0)
+        place = length - n + np.arange(n)[:, None]
+        seen = np.broadcast_to(fine, (n, len(tok))) & ((tok <= place) if causal else True)
+        if window:
+            seen = seen & (tok > place - window)
+        some = seen.any(1)
+        used = seen.any(0)
+        for h in range(heads):
+            K = np.where(used[:, None], k[entry, h, tok % page].astype(float) * ks[entry, h, None], 0.0)
+            V = np.where(used[:, None], v[entry, h, tok % page].astype(float) * vs[entry, h, None], 0.0)
+            top_vs = np.where(seen, np.where(used, vs[entry, h], 0.0), 0.0).max(1)
+            for j in range(h * group, (h + 1) * group):
+                x = q[a:a + n, j]
+                s = np.where(seen, x @ K.T * scale, -np.inf)[some]
+                m = s.max(1, keepdims=True)
+                p = np.exp(s - m)
+                total = p.sum(1, keepdims=True)
+                rows = np.arange(a, a + n)[some]
+                out[rows, j], A[rows, j] = p @ V / total, p @ np.abs(V) / total
+                lse[rows, j] = (m + np.log(total))[:, 0]
+                S[rows, j] = np.where(seen, np.abs(x) @ np.abs(K).T * abs(scale), 0.0).max(1)[some]
+                n_vs[rows, j] = (seen.sum(1) * top_vs)[some]
+    return out, lse, A, S, n_vs
+
+
+def check(cache, q, kind, start, ctx, table, scale, causal=True, window=0, prompts=None, floor=2.0 ** -25):
+    """Compares one call with the reference; prompts: which kernel it has to be (three launches, or at most two)."""
+    launches = b.awe_launch_count(handle())
+    out, lse = run_attention(cache, q, kind, start, ctx, table, scale, causal, window)
+    launches = b.awe_launch_count(handle()) - launches
+    assert prompts is None or (launches == 3) == prompts
+    want, want_lse, A, S, n_vs = reference(cache, q.double().numpy(), start, ctx, table, scale, causal, window)
+    e = 2 * (q.shape[2] / 16 + 3) * 2.0 ** -22 * S
+    u = TYPES[kind][2]
+    tol = u * np.abs(want) + (2.0 ** -11 + e[..., None]) * (A + np.abs(want)) + (floor * 128 * n_vs)[..., None]
+    tol += 2.0 ** -25 if kind == "f16" else 1e-38  # the smallest steps of the output type
+    assert np.isfinite(out).all()
+    assert (np.abs(out - want) <= tol).all(), float(np.max(np.abs(out - want) / tol))
+    empty = np.isneginf(want_lse)
+    assert np.array_equal(empty, np.isneginf(lse)) and (out[empty] == 0).all()
+    assert (np.abs(lse - want_lse)[~empty] <= (e + 2.0 ** -21 * (1 + np.abs(want_lse)))[~empty]).all()
+    return out, lse
+
+
+def normal(rng, *shape):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32))
+
+
+def one_request(rng, n_pages, page=16):
+    """A shuffled table of one request over the whole pool, as wide as WIDE tokens."""
+    return np.concatenate([rng.permutation(n_pages), np.full(WIDE // page, -1)])[None]
+
+
+# ------------------------------------------------------------------ value scales of 0
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows", [200, 3])  # the kernel for prompts, the one for few rows
+def test_a_page_of_value_scale_0_counts_as_zeros_whatever_its_bytes(dim, rows):
+    rng = np.random.default_rng(dim + rows)
+    cache = make_cache(rng, 40, 2, 16, dim)
+    cache[3][rng.random((40, 2)) < 0.3] = 0.0  # their bytes stay
+    q = normal(rng, rows, 8 if dim == 64 else 4, dim).to(torch.bfloat16)
+    check(cache, q, "bf16", [0, rows], [633], one_request(rng, 40), dim ** -0.5, prompts=rows == 200)
+
+
+@pytest.mark.parametrize("vs", [0.02, 1e-6, 1e-9, 3e4])
+@pytest.mark.parametrize("zero", ["before", "behind", "between", "odd pages"])
+@pytest.mark.parametrize("rows", [300, 2])
+def test_whole_steps_of_value_scale_0(vs, zero, rows):
+    """Tokens without values weigh in the divisor alone, and take no bits from the others."""
+    rng = np.random.default_rng(7)
+    cache = make_cache(rng, 40, 1, 16, 128)
+    cache[3][:] *= vs / 0.02
+    table = one_request(rng, 40)
+    at = np.arange(40)
+    off = {"before": at < 16, "behind": at >= 16, "between": (at >= 8) & (at < 24), "odd pages": at % 2 == 1}[zero]
+    cache[3][table[0, :40][off]] = 0.0
+    q = normal(rng, rows, 4, 128).to(torch.bfloat16)
+    check(cache, q, "bf16", [0, rows], [640], table, 0.3, prompts=rows == 300)
+
+
+@pytest.mark.parametrize("rows", [200, 2])
+def test_nothing_but_value_scales_of_0(rows):
+    rng = np.random.default_rng(9)
+    cache = make_cache(rng, 40, 2, 16, 128)
+    cache[3][:] = 0.0
+    out, _ = check(cache, normal(rng, rows, 4, 128).to(torch.float16), "f16", [0, rows], [630], one_request(rng, 40), 0.1, prompts=rows == 200)
+    assert (out == 0).all()
+
+
+@pytest.mark.parametrize("vs", [2.0 ** -106, 2.0 ** 90])
+@pytest.mark.parametrize("rows", [200, 2])
+def test_the_smallest_and_the_largest_value_scales(vs, rows):
+    """What the cache write stores of BF16 values from 2^-99, about the least that counts for a scale, to 2^97."""
+    rng = np.random.default_rng(10)
+    cache = make_cache(rng, 40, 2, 16, 128)
+    cache[3][:] = np.float32(vs)
+    check(cache, normal(rng, rows, 4, 128).to(torch.bfloat16), "bf16", [0, rows], [640], one_request(rng, 40), 0.1, prompts=rows == 200)
