@@ -131,3 +131,21 @@ def test_the_smallest_and_the_largest_value_scales(vs, rows):
     cache = make_cache(rng, 40, 2, 16, 128)
     cache[3][:] = np.float32(vs)
     check(cache, normal(rng, rows, 4, 128).to(torch.bfloat16), "bf16", [0, rows], [640], one_request(rng, 40), 0.1, prompts=rows == 200)
+
+
+# ------------------------------------------------------------------ windows over prompts
+@pytest.mark.parametrize("kind,dim,heads,group,page,new,ctx", [
+    ("bf16", 128, 8, 4, 16, [300, 129, 64], [700, 129, 411]), ("f16", 128, 2, 16, 64, [257, 300, 1], [257, 1500, 900]),
+    ("bf16", 64, 8, 4, 32, [500, 300], [513, 1111]), ("f16", 64, 4, 5, 256, [900, 200], [900, 300]), ("f16", 128, 1, 1, 128, [5000], [5003])])
+@pytest.mark.parametrize("window", [1, 3, 100, 128, 1000])
+def test_prompts_under_a_window(kind, dim, heads, group, page, new, ctx, window):
+    rng = np.random.default_rng(dim + heads * group + page + window)
+    need = [-(-c // page) for c in ctx]
+    pages, at = rng.permutation(sum(need) + 2), 0
+    table = np.full((len(ctx), max(need) + WIDE // page), -1)
+    for i, n in enumerate(need):
+        table[i, :n] = pages[at:at + n]
+        at += n
+    cache = make_cache(rng, sum(need) + 2, heads, page, dim)
+    q = normal(rng, sum(new), heads * group, dim).to(TYPES[kind][1])
+    check(cache, q, kind, np.concatenate([[0], np.cumsum(new)]), ctx, table, dim ** -0.5, window=window, prompts=True)
