@@ -162,10 +162,10 @@ extern "C" awe_status_t awe_kv_plan(awe_handle_t h, const int32_t* cached_len_de
     PlanParams p = {cached_len_dev, new_len_dev, free_pages_dev, block_table_dev, slots_dev,       positions_dev,
                     q_start_dev,    ctx_len_dev, counts_dev,     ld_table,        max_tokens,      n_free,
                     (int)B,         page_log2,   (int)max_pages};
+    // The limit is the kernel's, not this launch's: raised to the most, so that no other thread's call finds it lower than its own.
     const size_t smem = 2 * (size_t)(B + 1) * sizeof(int);
-    if (smem > 48 * 1024 &&
-        cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-        return AWE_ERR_CUDA;
+    static std::atomic<uint64_t> done{0};
+    if (serve::allow_smem(kv_plan_kernel, 2 * (kMaxRequests + 1) * (int)sizeof(int), h->device, done) != cudaSuccess) return AWE_ERR_CUDA;
     const int64_t items = std::max(max_tokens, B);
     const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>((items + kThreads - 1) / kThreads, 4 * h->sm_count));
     if (serve::launch_early(kv_plan_kernel, dim3(blocks), kThreads, smem, (cudaStream_t)stream, p) != cudaSuccess) return AWE_ERR_CUDA;
