@@ -378,7 +378,7 @@ typedef struct {
 } awe_kv_cache;
 
 /* What a step over B requests (at most AWE_KV_MAX_REQUESTS) needs to know of its pages.  Request b holds cached_len[b] tokens and adds
- * new_len[b] (negative lengths count as 0; the sums stay below 2^31).  Its row of block_table_dev (max_pages
+ * new_len[b] (negative lengths count as 0; a sum of lengths or of pages that would pass 2^31 - 1 is taken as that).  Its row of block_table_dev (max_pages
  * entries, rows ld_table apart) names the pages of the tokens it holds; the entries of the pages it needs
  * besides are written, taken from free_pages_dev in order, request by request (-1 where the list has ended).
  * Entries before and behind those stay as they are.  Written besides:

@@ -42,6 +42,10 @@ __device__ __forceinline__ int last_not_above(const int* a, int n, int x) {
     return lo;
 }
 
+// Sums of counts stay at 2^31 - 1 where they would pass it (which is associative), so that every prefix is in order
+// and no place computed from one is negative, whatever the lengths are.
+__device__ __forceinline__ int add_sat(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7FFFFFFFu); }
+
 __global__ void __launch_bounds__(kThreads) kv_plan_kernel(PlanParams p) {
     extern __shared__ int prefix[];
     int* start = prefix;             // B + 1: first new token of each request
@@ -63,27 +67,28 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(PlanParams p) {
         int cached, added;
         lengths(b, cached, added);
         const int have = pages_of(cached), want = pages_of((int64_t)cached + added);
-        s.tokens += added;
-        s.pages += max(min(want, p.max_pages) - have, 0);
-        s.missing += want - have;
-        s.longest = max(s.longest, cached + added);
+        s.tokens = add_sat(s.tokens, added);
+        s.pages = add_sat(s.pages, max(min(want, p.max_pages) - have, 0));
+        s.missing = add_sat(s.missing, want - have);
+        s.longest = max(s.longest, add_sat(cached, added));
     }
     Sums inc = s;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const int a = __shfl_up_sync(~0u, inc.tokens, d), b = __shfl_up_sync(~0u, inc.pages, d),
                   c = __shfl_up_sync(~0u, inc.missing, d), m = __shfl_up_sync(~0u, inc.longest, d);
-        if (lane >= d) inc.tokens += a, inc.pages += b, inc.missing += c, inc.longest = max(inc.longest, m);
+        if (lane >= d) inc = {add_sat(inc.tokens, a), add_sat(inc.pages, b), add_sat(inc.missing, c), max(inc.longest, m)};
     }
     if (lane == 31) warp_sums[warp] = inc;
+    int tokens = __shfl_up_sync(~0u, inc.tokens, 1), pages = __shfl_up_sync(~0u, inc.pages, 1);  // of the lanes before
+    if (lane == 0) tokens = pages = 0;
     __syncthreads();
-    int tokens = inc.tokens - s.tokens, pages = inc.pages - s.pages;
     Sums total = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) tokens += warp_sums[w].tokens, pages += warp_sums[w].pages;
-        total.tokens += warp_sums[w].tokens, total.pages += warp_sums[w].pages, total.missing += warp_sums[w].missing;
-        total.longest = max(total.longest, warp_sums[w].longest);
+        const Sums o = warp_sums[w];
+        if (w < warp) tokens = add_sat(tokens, o.tokens), pages = add_sat(pages, o.pages);
+        total = {add_sat(total.tokens, o.tokens), add_sat(total.pages, o.pages), add_sat(total.missing, o.missing), max(total.longest, o.longest)};
     }
     for (int b = b0; b < b1; ++b) {
         int cached, added;
@@ -92,10 +97,10 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(PlanParams p) {
         base[b] = pages;
         if (blockIdx.x == 0) {
             p.q_start[b] = tokens;
-            p.ctx_len[b] = cached + added;
+            p.ctx_len[b] = add_sat(cached, added);
         }
-        tokens += added;
-        pages += max(min(pages_of((int64_t)cached + added), p.max_pages) - pages_of(cached), 0);
+        tokens = add_sat(tokens, added);
+        pages = add_sat(pages, max(min(pages_of((int64_t)cached + added), p.max_pages) - pages_of(cached), 0));
     }
     if (tid == 0) {
         start[p.B] = total.tokens;
@@ -123,14 +128,15 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(PlanParams p) {
         if (t < total.tokens) {
             const int b = last_not_above(start, p.B, (int)t);
             const int cached = max(p.cached[b], 0);
-            pos = cached + (int)t - start[b];
-            const int j = pos >> p.page_log2, have = pages_of(cached);
+            const unsigned at = (unsigned)cached + (unsigned)((int)t - start[b]);  // below 2^32
+            pos = (int)min(at, 0x7FFFFFFFu);
+            const int j = (int)(at >> p.page_log2), have = pages_of(cached);
             int page = -1;
             if (j < p.max_pages) {
                 const int64_t i = (int64_t)base[b] + j - have;
                 page = j < have ? p.table[b * p.ld_table + j] : (i < p.n_free ? p.free_pages[i] : -1);
             }
-            if (page >= 0) slot = ((int64_t)page << p.page_log2) + (pos & mask);
+            if (page >= 0) slot = ((int64_t)page << p.page_log2) + (at & mask);
         }
         p.slots[t] = slot;
         if (p.positions) p.positions[t] = pos;
