@@ -389,7 +389,8 @@ typedef struct {
  *   counts_dev[4]                      pages taken, new tokens, pages that were wanted and not had (the
  *                                      list or a table row was too short), longest request
  * Nothing is removed from the free list: the caller drops its first counts_dev[0] entries.  A call with the
- * same arguments again writes the same again. */
+ * same arguments again writes the same again.  The lengths are read until the call ends: q_start_dev, ctx_len_dev
+ * and counts_dev that share memory with them are AWE_ERR_INVALID_ARG (advance cached_len by a copy of ctx_len). */
 #define AWE_KV_MAX_REQUESTS 16384
 awe_status_t awe_kv_plan(awe_handle_t h, const int32_t* cached_len_dev, const int32_t* new_len_dev, int64_t B,
                          int64_t page_size, const int32_t* free_pages_dev, int64_t n_free, int32_t* block_table_dev,

@@ -143,6 +143,11 @@ __global__ void __launch_bounds__(kThreads) kv_plan_kernel(PlanParams p) {
     }
 }
 
+// Whether two arrays of n and m elements share memory.
+bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+    return n > 0 && m > 0 && (uintptr_t)a < (uintptr_t)(b + m) && (uintptr_t)b < (uintptr_t)(a + n);
+}
+
 }  // namespace
 }  // namespace awe
 
@@ -163,6 +168,9 @@ extern "C" awe_status_t awe_kv_plan(awe_handle_t h, const int32_t* cached_len_de
         (uintptr_t)block_table_dev % 4 || (uintptr_t)slots_dev % 8 || (uintptr_t)positions_dev % 4 ||
         (uintptr_t)q_start_dev % 4 || (uintptr_t)ctx_len_dev % 4 || (uintptr_t)counts_dev % 4)
         return AWE_ERR_ALIGNMENT;
+    // Every block reads the lengths for itself, at a time of its own: what one of them writes must not lie there.
+    for (const int32_t* lengths : {cached_len_dev, new_len_dev})
+        if (overlap(lengths, B, ctx_len_dev, B) || overlap(lengths, B, q_start_dev, B + 1) || overlap(lengths, B, counts_dev, 4)) return AWE_ERR_INVALID_ARG;
     int page_log2 = 4;
     while ((1 << page_log2) < page_size) ++page_log2;
     PlanParams p = {cached_len_dev, new_len_dev, free_pages_dev, block_table_dev, slots_dev,       positions_dev,

@@ -76,3 +76,24 @@ def test_lengths_whose_sums_pass_31_bits(cached, new, page):
     assert ctx.tolist() == [min(max(c, 0) + max(n, 0), MOST) for c, n in zip(cached, new)]
     assert counts.tolist() == [taken, tokens, min(missing, MOST) - taken, max(ctx.tolist())]
     assert pool.tolist() == [[5] * width] + table + [[5] * width]
+
+
+def test_outputs_that_lie_in_the_lengths_are_refused():
+    B, i32 = 8, dict(dtype=torch.int32, device="cuda")
+    both, new, table, slots = torch.ones(64, **i32), torch.ones(B, **i32), torch.zeros((B, 2), **i32), torch.empty(B, dtype=torch.int64, device="cuda")
+    free, start, ctx, counts = torch.arange(B, **i32), torch.empty(B + 1, **i32), torch.empty(B, **i32), torch.empty(4, **i32)
+    cached = both[20:20 + B]
+
+    def plan(cached=cached, new=new, start=start, ctx=ctx, counts=counts):
+        b.awe_kv_plan(handle(), cached, new, B, 16, free, B, table, 2, 2, slots, None, B, start, ctx, counts)
+
+    launches = b.awe_launch_count(handle())
+    for bad in (dict(ctx=cached), dict(ctx=new), dict(ctx=both[13:]), dict(ctx=both[27:]), dict(start=both[12:]), dict(start=new), dict(counts=both[17:]),
+                dict(counts=both[27:])):
+        with pytest.raises(b.AweError) as e:
+            plan(**bad)
+        assert e.value.status == 1
+    assert b.awe_launch_count(handle()) == launches
+    for fine in (dict(ctx=both[12:]), dict(ctx=both[28:]), dict(start=both[11:]), dict(counts=both[16:])):
+        plan(**fine)
+    torch.cuda.synchronize()
