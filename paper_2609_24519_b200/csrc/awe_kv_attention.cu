@@ -213,6 +213,15 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                 if (8 * nt + 2 * t + j < n_rows) all_lo = max(all_lo, see_lo[nt][j]), all_hi = min(all_hi, see_hi[nt][j]);
         all_lo = __reduce_max_sync(~0u, all_lo);
         all_hi = __reduce_min_sync(~0u, all_hi);
+        // tokens [any_lo, any_hi) that some row sees: the pages of others are not followed, which a window may have given up
+        int any_lo = 0x7FFFFFFF, any_hi = 0;
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (see_lo[nt][j] < see_hi[nt][j]) any_lo = min(any_lo, see_lo[nt][j]), any_hi = max(any_hi, see_hi[nt][j]);
+        any_lo = __reduce_min_sync(~0u, any_lo);
+        any_hi = __reduce_max_sync(~0u, any_hi);
 
         float o[kSteps16][kNT][4];
         float m_ref[kNT][2], sum[kNT][2], sum_lse[kNT][2];
@@ -233,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
         const int tok0 = r.lo + step0 * kStepTokens + warp * 16;
         auto page_of = [&](int i) {  // page of tile i, -1 where it has none
             const int tok = tok0 + i * kStepTokens;
-            if (i >= n_tiles || tok >= r.ctx) return -1;
+            if (i >= n_tiles || tok >= any_hi || tok + 16 <= any_lo) return -1;
             const int page = table[tok >> p.page_log2];
             return (unsigned)page < (unsigned)p.n_pages ? page : -1;
         };

@@ -46,6 +46,7 @@ struct TcAttnParams {
 
 struct Unit {
     int b, q0, n, ctx, row0, rows, lo, steps;
+    int first, end;  // tokens that some row may see: the pages of others are not followed, which a window may have given up
     int64_t place0;  // of the request's first query among its tokens
 };
 __device__ __forceinline__ Unit unit_of(const AttnParams& p, int b, int tile) {
@@ -59,7 +60,9 @@ __device__ __forceinline__ Unit unit_of(const AttnParams& p, int b, int tile) {
     u.rows = min(kRows, u.n * p.group - u.row0);
     const int64_t first = u.place0 + u.row0 / p.group, last = u.place0 + (u.row0 + u.rows - 1) / p.group;
     const int64_t hi = p.causal ? min((int64_t)u.ctx, last + 1) : (int64_t)u.ctx;
-    u.lo = p.window > 0 && first + 1 > p.window ? (int)min(first + 1 - p.window, (int64_t)u.ctx) & ~(kStep - 1) : 0;
+    u.first = p.window > 0 && first + 1 > p.window ? (int)min(first + 1 - p.window, (int64_t)u.ctx) : 0;
+    u.lo = u.first & ~(kStep - 1);
+    u.end = (int)max(hi, (int64_t)0);
     u.steps = max((int)((hi - u.lo + kStep - 1) / kStep), 1);  // one at least: its rows are to be written
     return u;
 }
@@ -318,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             auto page_of = [&](int j) {  // lanes below 8: page of their 16 tokens of step j, -1 where there is none
                 const int tok = u.lo + j * kStep + 16 * lane;
                 int page = -1;
-                if (j < s1 && lane < kStep / 16 && tok < u.ctx) {
+                if (j < s1 && lane < kStep / 16 && tok < u.end && tok + 16 > u.first) {
                     page = table[tok >> p.page_log2];
                     if (page < 0 || page >= p.n_pages) page = -1;
                 }

@@ -42,8 +42,8 @@ def reference(cache, q, start, ctx, table, scale, causal, window):
         some = seen.any(1)
         used = seen.any(0)
         for h in range(heads):
-            K = np.where(used[:, None], k[entry, h, tok % page].astype(float) * ks[entry, h, None], 0.0)
-            V = np.where(used[:, None], v[entry, h, tok % page].astype(float) * vs[entry, h, None], 0.0)
+            K = k[entry, h, tok % page].astype(float) * np.where(used, ks[entry, h], 0.0)[:, None]
+            V = v[entry, h, tok % page].astype(float) * np.where(used, vs[entry, h], 0.0)[:, None]
             top_vs = np.where(seen, np.where(used, vs[entry, h], 0.0), 0.0).max(1)
             for j in range(h * group, (h + 1) * group):
                 x = q[a:a + n, j]
@@ -74,7 +74,8 @@ def check(cache, q, kind, start, ctx, table, scale, causal=True, window=0, promp
     assert (np.abs(out - want) <= tol).all(), float(np.max(np.abs(out - want) / tol))
     empty = np.isneginf(want_lse)
     assert np.array_equal(empty, np.isneginf(lse)) and (out[empty] == 0).all()
-    assert (np.abs(lse - want_lse)[~empty] <= (e + 2.0 ** -21 * (1 + np.abs(want_lse)))[~empty]).all()
+    lse, want_lse, e = lse[~empty], want_lse[~empty], e[~empty]
+    assert (np.abs(lse - want_lse) <= e + 2.0 ** -21 * (1 + np.abs(want_lse))).all()
     return out, lse
 
 
@@ -149,3 +150,30 @@ def test_prompts_under_a_window(kind, dim, heads, group, page, new, ctx, window)
     cache = make_cache(rng, sum(need) + 2, heads, page, dim)
     q = normal(rng, sum(new), heads * group, dim).to(TYPES[kind][1])
     check(cache, q, kind, np.concatenate([[0], np.cumsum(new)]), ctx, table, dim ** -0.5, window=window, prompts=True)
+
+
+# ------------------------------------------------------------------ places that no row sees
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("rows,ctx", [(1, 700), (5, 700), (300, 700), (700, 1500)])  # the last is enough for the kernel for prompts
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+def test_pages_in_front_of_the_window_are_not_followed(bad, rows, ctx, kind):
+    """Their entries may name a page that has been given up since, whatever its scales are now."""
+    rng = np.random.default_rng(rows)
+    n_pages, window = -(-ctx // 16) + 2, 100
+    cache = make_cache(rng, n_pages, 2, 16, 128)
+    cache[2][-1] = cache[3][-1] = bad
+    table = one_request(rng, n_pages - 1)
+    table[0, :(ctx - rows + 1 - window) // 16] = n_pages - 1  # the pages in front of the first row's first token
+    check(cache, normal(rng, rows, 8, 128).to(TYPES[kind][1]), kind, [0, rows], [ctx], table, 0.09, window=window, prompts=rows == 700)
+
+
+@pytest.mark.parametrize("rows", [6, 300])
+def test_pages_behind_the_last_row_of_the_call_are_not_followed(rows):
+    """Rows that stand in front of the first token see nothing, and make no page visible."""
+    rng = np.random.default_rng(rows)
+    cache = make_cache(rng, 6, 1, 16, 128)
+    cache[2][5] = cache[3][5] = np.nan
+    table = np.full((2, WIDE // 16), 5)
+    table[0, :2], table[1, :3] = [1, 2], [0, 3, 4]
+    # 20 and 48 tokens; the entries behind them name the bad page
+    check(cache, normal(rng, 2 * rows, 8, 128).to(torch.bfloat16), "bf16", [0, rows, 2 * rows], [20, 48], table, 0.09, prompts=rows == 300)
