@@ -204,8 +204,8 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             }
         }
 
-        // tokens that every row of the unit sees
-        int all_lo = see_lo[0][0], all_hi = see_hi[0][0];
+        // tokens [all_lo, all_hi) that every row of the unit sees
+        int all_lo = 0, all_hi = 0x7FFFFFFF;
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
