@@ -334,7 +334,7 @@ awe_status_t awe_reconstruct(awe_handle_t h, int enc, int modulus, const float* 
  * the attention that reads it.  They keep the integer containers of this library (AWE_I4_PACKED weights,
  * AWE_I8 cache values) and multiply them with floating-point activations, so they round where the exact
  * products above do not: every sum, softmax statistic and scale is held in 32 bits, and the result is
- * rounded once to its output type.  (No counterpart in the paper.)
+ * rounded once to its output type.  The attention rounds twice besides, and says where.  (No counterpart in the paper.)
  *   - An empty batch (M, T or B equal to 0) is not an error.
  *   - Lengths, tables and slots are read on the device only.  An entry that points outside what the
  *     descriptor says exists (a page outside the pool, a slot outside it) is skipped, never followed.
@@ -419,7 +419,9 @@ size_t awe_kv_attention_workspace_bytes(awe_handle_t h, const awe_kv_cache* cach
  * position, else all ctx_len[b]; window > 0 (causal only): the last `window` of those.  A query that sees nothing gets zeros and
  * lse = -inf; rows behind the last request's queries are left as they are.  The scales of the cache are not negative.  A table entry outside the pool hides its tokens.  q_dev: T x n_q_heads x head_dim of type AWE_F16 or AWE_BF16 with token stride
  * ldq, out_dev alike with ldo; lse_dev (T x n_q_heads floats, natural logarithm of the sum of exponentials) may
- * be NULL.  q_dev and out_dev 16-B aligned, ldq and ldo multiples of 8.  workspace_dev: 256-B aligned. */
+ * be NULL.  Rounded before the sums: the softmax weights (for prompts: times the values' scales), to FP16, each by at most 2^-11 of itself
+ * or, below 2^-24 of the largest so far among the tokens that are summed together, by 2^-35 of that one; and elements of BF16 queries
+ * below 2^-32 of their row's largest, which lose bits.  q_dev and out_dev 16-B aligned, ldq and ldo multiples of 8.  workspace_dev: 256-B aligned. */
 awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const void* q_dev, awe_float_t type,
                               int64_t T, int64_t n_q_heads, int64_t ldq, const int32_t* q_start_dev,
                               const int32_t* ctx_len_dev, int64_t B, const int32_t* block_table_dev,

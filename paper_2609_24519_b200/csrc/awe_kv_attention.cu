@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
         pos += p.whole ? 1 : step1 - step0;
 
         // ---- the query rows, as the matrix instruction's 16 x 8 operand: thread (g, t) holds of row g the
-        // dimensions whose cache pieces it reads.  BF16 rows are scaled by a power of two so that FP16 holds them.
+        // dimensions whose cache pieces it reads.  BF16 rows are scaled by a power of two (query_exponent).
         uint32_t qf[kNT][kSteps16][2];
         float cq[kNT][2];        // factor of the scores of columns 2t, 2t + 1
         int see_lo[kNT][2], see_hi[kNT][2];  // tokens [see_lo, see_hi) are visible
@@ -178,10 +178,9 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                     }
                 m = fmaxf(m, __shfl_xor_sync(~0u, m, 1));
                 m = fmaxf(m, __shfl_xor_sync(~0u, m, 2));
-                // 2^-e for m in [2^e, 2^(e+1)), e kept where both powers are normal (an infinity takes the largest)
-                const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -120), 120);
-                const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-                factor *= __uint_as_float((uint32_t)(127 + e) << 23);
+                const int e = query_exponent((int)(__float_as_uint(m) >> 23));
+                const float down = power_of_2(15 - e);
+                factor *= power_of_2(e - 15);
 #pragma unroll
                 for (int i = 0; i < kSteps16; ++i)
 #pragma unroll
@@ -349,8 +348,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             }
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt)
-                grows |= fmaxf(s[nt][0], s[nt][2]) > m_ref[nt][0] + 8.0f || fmaxf(s[nt][1], s[nt][3]) > m_ref[nt][1] + 8.0f;
-            // The reference only has to stay within 2^8 of the maximum for FP16 to hold exp2(s - m_ref); it moves rarely.
+                grows |= fmaxf(s[nt][0], s[nt][2]) > m_ref[nt][0] + kMostAbove || fmaxf(s[nt][1], s[nt][3]) > m_ref[nt][1] + kMostAbove;
             if (__any_sync(~0u, grows)) {
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt)
@@ -360,7 +358,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                         m = fmaxf(m, __shfl_xor_sync(~0u, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(~0u, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(~0u, m, 16));
-                        m = fmaxf(m, m_ref[nt][j]);
+                        m = fmaxf(m - kBelow, m_ref[nt][j]);
                         const float a = m == m_ref[nt][j] ? 1.0f : exp2_approx(m_ref[nt][j] - m);
                         m_ref[nt][j] = m;
                         sum[nt][j] *= a;

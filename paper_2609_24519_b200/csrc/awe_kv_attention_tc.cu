@@ -7,10 +7,10 @@
 // softmax runs beside the other's products.
 //
 // Scales.  The keys' scale of 16 tokens of a page multiplies the scores in FP32.  The values' scale vs is folded into P as
-// an addition to the exponent: P = exp2(s + log2 vs - m) with m within 8 of the largest s + log2 vs seen so far, so
+// an addition to the exponent: P = exp2(s + log2 vs - m) with m 10 to 15 below the largest s + log2 vs seen so far, so
 // that P rounds to FP16 as well as it can for what it contributes, whatever the scales; the divisor is the sum of
 // 2^-12 P / vs in FP32 (the power of two keeps it in range for every scale that the cache write stores, 2^-107 to 2^121).
-// m moves only when a score passes it by more than 2^8, which rescales O in tensor memory; that is rare after the first step.
+// m moves only when a score passes it by more than 15, which rescales O in tensor memory; that is rare after the first step.
 // Tokens whose page has value scale 0 stand for zeros whatever their bytes, and weigh in the divisor alone: their P is 0, so that
 // they neither add to O nor move m, and their exponentials are summed apart, against a maximum of their own, in a pass that only
 // steps with such pages take; the two sums meet at the end.
@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             const bool live = 128 * t + row < u.rows;
             const int query = live ? r / p.group : 0, qh = head * p.group + (live ? r % p.group : 0);
             float cq = p.scale_log2;
-            {  // the query row to shared memory; BF16 is scaled by a power of two so that FP16 holds it
+            {  // the query row to shared memory; BF16 is scaled by a power of two (query_exponent)
                 const T16* src = reinterpret_cast<const T16*>(p.q) + (int64_t)(u.q0 + query) * p.ldq + (int64_t)qh * kD;
                 float down = 1.0f;
                 const uint32_t flip = cq < 0.0f ? 0x80008000u : 0u;  // a negative factor's sign goes to the query
@@ -431,9 +431,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                             m = __vimax3_u16x2(__vimax3_u16x2(m, x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu);
                         }
                     }
-                    const int e = min(max((int)(max(m & 0xFFFFu, m >> 16) >> 7) - 127, -120), 120);
-                    down = __uint_as_float((uint32_t)(127 - e) << 23);
-                    cq *= __uint_as_float((uint32_t)(127 + e) << 23);
+                    const int e = query_exponent((int)(max(m & 0xFFFFu, m >> 16) >> 7));
+                    down = power_of_2(15 - e);
+                    cq *= power_of_2(e - 15);
                 }
 #pragma unroll
                 for (int i = 0; i < kD / 8; ++i) {
@@ -500,12 +500,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                     }
                 });
                 const bool first = m_ref == -INFINITY;
-                const bool grows = top > (first ? -INFINITY : m_ref + 8.0f);
+                const bool grows = top > (first ? -INFINITY : m_ref + kMostAbove);
                 const uint32_t unvalued = sh->unvalued[step & 3];
                 if (__any_sync(~0u, grows || unvalued)) {  // one branch on the way of most steps: with two they take 0.6 % longer
                     if (unvalued) add_unvalued(sh, unvalued, step & 3, s_at[t] + lanes, 128 * t + row, see_lo - tok0, see_hi - tok0, cq);
                     const float before = m_ref;
-                    m_ref = fmaxf(m_ref, top);
+                    m_ref = fmaxf(m_ref, top - kBelow);
                     const float shrink = first || m_ref == before ? 1.0f : exp2_approx(before - m_ref);
                     sum *= shrink;
                     if (j > s0 && __any_sync(~0u, shrink != 1.0f)) {  // O once the products of the step before are in it

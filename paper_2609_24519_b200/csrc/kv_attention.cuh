@@ -39,6 +39,16 @@ struct Deal {
     }
 };
 
+// Weights are rounded to FP16 as exp2(s - m).  The reference m is put kBelow below the largest s so far and moves only when an s
+// passes it by more than kMostAbove, which is rare, so the largest weight lies between 2^10 and 2^15 and FP16 holds all that
+// it can beside it: a weight keeps 11 bits down to 2^-24 of the largest, and is off by 2^-35 of that at most below.
+constexpr float kBelow = 10.0f, kMostAbove = 15.0f;
+
+// BF16 queries go to FP16 times 2^(15 - e), e the exponent of the row's largest magnitude, whose biased exponent is given: that
+// one lands in [2^15, 2^16), and elements down to 2^-32 of it keep all of their 8 bits.  e stays where both powers are normal.
+__device__ __forceinline__ int query_exponent(int biased) { return min(max(biased - 127, -111), 127); }
+__device__ __forceinline__ float power_of_2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
 // Four signed bytes as two pairs of FP16: the byte with its sign bit flipped is u = x + 128, the FP16 pattern
 // 0x6400 | u is 1024 + u, and subtracting 1152 is exact.
 __device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped, uint32_t selector) {

@@ -177,3 +177,49 @@ def test_pages_behind_the_last_row_of_the_call_are_not_followed(rows):
     table[0, :2], table[1, :3] = [1, 2], [0, 3, 4]
     # 20 and 48 tokens; the entries behind them name the bad page
     check(cache, normal(rng, 2 * rows, 8, 128).to(torch.bfloat16), "bf16", [0, rows, 2 * rows], [20, 48], table, 0.09, prompts=rows == 300)
+
+
+# ------------------------------------------------------------------ range of the weights and of the queries
+FLOOR = 2.0 ** -35  # of the largest weight: what a rounded weight may be off by where it is far below
+
+
+@pytest.mark.parametrize("lead", [20, 24, 26])
+@pytest.mark.parametrize("tokens,rows", [(256, 1), (8192, 1), (8192, 200)])
+@pytest.mark.parametrize("leader", ["first", "last"])
+def test_a_token_without_values_that_leads_the_others_far(lead, tokens, rows, leader):
+    """The others' weights are 2^-lead of the leader's, and they alone make the result."""
+    rng = np.random.default_rng(lead)
+    dim, page, n_pages = 128, 16, tokens // 16
+    cache = make_cache(rng, n_pages, 1, page, dim)
+    cache[0][:], cache[2][:], cache[3][:] = 100, np.float32(0.01), np.float32(0.02)
+    cache[1][:] = rng.integers(1, 128, cache[1].shape)
+    at = (0, 0) if leader == "first" else (n_pages - 1, page - 1)
+    cache[0][at[0], 0, at[1]], cache[1][at[0], 0, at[1]] = 120, 0
+    q = torch.ones((rows, 2, dim)).to(torch.float16)
+    scale = lead * np.log(2) / (20 * dim * 0.01)
+    table = np.concatenate([np.arange(n_pages), np.full(0 if tokens == 256 else WIDE // page, -1)])[None]
+    check(cache, q, "f16", [0, rows], [tokens], table, scale, causal=False, prompts=rows == 200, floor=FLOOR)
+
+
+@pytest.mark.parametrize("rows", [200, 3])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_bf16_queries_with_one_element_far_above_the_others(rows, dim):
+    """Keys are 0 there, so the small elements alone make the scores."""
+    rng = np.random.default_rng(dim)
+    cache = make_cache(rng, 40, 2, 16, dim)
+    cache[0][..., 5] = 0
+    q = normal(rng, rows, 8, dim)
+    q[..., 5] = 2.0 ** 21
+    q[1, 0, 5], q[2, 0, 5] = -2.0 ** 20, 2.0 ** -10
+    q[0, 0], q[0, 0, 5] = 0.0, 2.0 ** 127  # by itself: scores of 0
+    check(cache, q.to(torch.bfloat16), "bf16", [0, rows], [640], one_request(rng, 40), dim ** -0.5, prompts=rows == 200, floor=FLOOR)
+
+
+@pytest.mark.parametrize("rows", [200, 3])
+@pytest.mark.parametrize("q_scale", [2.0 ** -126, 2.0 ** -115, 2.0 ** 60])
+def test_bf16_queries_at_the_ends_of_their_range(rows, q_scale):
+    rng = np.random.default_rng(4)
+    cache = make_cache(rng, 40, 2, 16, 128)
+    q = (normal(rng, rows, 8, 128) * q_scale).to(torch.bfloat16)
+    scale = float(np.float32(0.09 / max(q_scale, 2.0 ** -60)))
+    check(cache, q, "bf16", [0, rows], [640], one_request(rng, 40), scale, prompts=rows == 200, floor=FLOOR)
