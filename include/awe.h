@@ -399,12 +399,12 @@ awe_status_t awe_kv_plan(awe_handle_t h, const int32_t* cached_len_dev, const in
                          void* stream);
 
 /* Quantise T new tokens' keys and values (type AWE_F16 or AWE_BF16, T x n_heads x head_dim, token strides
- * ldk and ldv in elements) into their slots.  The tokens of one page stand together in the list and fill it in order
+ * ldk and ldv in elements) into their slots.  The tokens of one page stand together in the list (a page twice in it, apart, is a race) and fill it in order
  * (awe_kv_plan's order).  The scale of a page and head is the largest magnitude in it times 1 / 127 (both FP32); it starts anew with the
  * token at place 0 and only grows: where a new token needs a larger one, the values already there are rounded
  * again to it.  A value is stored as round(x * (1 / scale)), ties to even.  NaN is stored as 0 and an infinity
  * as +-127, and neither counts for the scale; new tokens whose magnitudes all stay below 2^-100 ask for scale 0.  A negative slot, or one outside the
- * pool, is skipped. */
+ * pool, is skipped; up to page_size of those in a row may stand between two tokens of one page. */
 awe_status_t awe_kv_write(awe_handle_t h, const awe_kv_cache* cache, const void* k_dev, const void* v_dev,
                           awe_float_t type, int64_t T, int64_t ldk, int64_t ldv, const int64_t* slots_dev,
                           void* stream);

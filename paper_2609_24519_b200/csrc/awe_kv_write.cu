@@ -2,10 +2,14 @@
 //
 // For the run of tokens of one page and head: a = max |x| over the run's finite values, s' = max(s, a * (1 / 127)) with the
 // scale s that the page has (0 where the run starts the page), q = round(x / s'); where s' > s the values already in the page
-// become round(q s / s').  Each row is read once (it waits in registers between the maximum and the rounding) and
-// written once: 3 bytes per value, bound by HBM.  The list's tokens of one page stand together, so a block finds its
-// runs by itself: it looks at `window` neighbouring slots and takes the runs that begin there.
+// become round(q s / s').  The first 8,192 values of a run are read once (they wait in registers between the maximum and the
+// rounding), the rest of a longer one twice, from L2 the second time; all are written once.
+//
+// The list's tokens of one page stand together, so a block finds its runs by itself: it looks at `window` neighbouring slots and
+// takes the runs that begin there.  Slots that are skipped may stand between a run's tokens (a list with some of its
+// tokens masked): the run goes on behind them, since two blocks that shared a page would race for its scale.
 #include <algorithm>
+#include <type_traits>
 
 #include "awe_internal.h"
 #include "serve_common.cuh"
@@ -94,9 +98,10 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
     return q;
 }
 
-// grid: (windows of tokens, heads, keys / values)
+// grid: (windows of tokens, heads, keys / values).  Eight blocks on an SM: what the 64 registers that this leaves cost is less than
+// what more loads under way bring (19.6 k tokens of 8 heads of 128: 30.1 us; six blocks of 80 registers 32.7, four of 114 39.3).
 template <bool kBf16, bool kVec>
-__global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
+__global__ void __launch_bounds__(kThreads, 8) kv_write_kernel(WriteParams p) {
     using T16 = typename Half<kBf16>::type;
     __shared__ uint32_t warp_max[kThreads / 32];
     constexpr uint32_t kInfinity = kBf16 ? 0x7F80u : 0x7C00u;
@@ -107,94 +112,123 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(WriteParams p) {
     int8_t* cache = values ? p.v_cache : p.k_cache;
     float* scales = values ? p.v_scale : p.k_scale;
     const int dim = 1 << p.dim_log2, page_size = 1 << p.page_log2, per_row_log2 = p.dim_log2 - 3;
-    auto page_of = [&](int64_t t) -> int64_t {
-        const int64_t s = p.slots[t];
-        return s < 0 || s >= p.n_slots ? -1 : s >> p.page_log2;
+    auto page_of_slot = [&](int64_t slot) -> int64_t { return slot < 0 || slot >= p.n_slots ? -1 : slot >> p.page_log2; };
+    auto page_of = [&](int64_t t) { return page_of_slot(p.slots[t]); };
+    // A run goes on behind at most this many skipped slots (31: so many that no gap inside 32 neighbours ends it).
+    const int most_skipped = max(page_size, 31);
+    // Whether none of the tokens before t that are near enough, skipped ones left out, is of this page: asked by the whole
+    // warp, 32 tokens at a time.
+    auto no_run_before = [&](int64_t t, int64_t page) {
+        for (int64_t end = t; end > 0 && t - end <= most_skipped; end -= 32) {
+            const int64_t back = end - 1 - lane, other = back >= 0 && t - 1 - back <= most_skipped ? page_of(back) : -1;
+            const unsigned found = __ballot_sync(~0u, other >= 0);
+            if (found) return __shfl_sync(~0u, other, __ffs(found) - 1) != page;
+        }
+        return true;
     };
     grid_wait();
     const int64_t t_begin = (int64_t)blockIdx.x * p.window, t_end = min(p.T, t_begin + p.window);
     unsigned begins = 0;  // of the 32 tokens from t32, those that begin a run (every warp finds out for itself)
     for (int64_t t32 = t_begin, t0 = 0; t32 < t_end || begins; begins &= begins - 1) {
         while (!begins && t32 < t_end) {
-            const int64_t t = t32 + lane, mine = t < t_end ? page_of(t) : -1;
-            begins = __ballot_sync(~0u, mine >= 0 && (t == 0 || page_of(t - 1) != mine));
+            const int64_t t = t32 + lane, mine = t < t_end ? page_of(t) : -1, before = mine >= 0 && t > 0 ? page_of(t - 1) : -1;
+            begins = __ballot_sync(~0u, mine >= 0 && before != mine);
+            for (unsigned ask = __ballot_sync(~0u, mine >= 0 && t > 0 && before < 0); ask; ask &= ask - 1) {
+                const int i = __ffs(ask) - 1;
+                if (!no_run_before(t32 + i, __shfl_sync(~0u, mine, i))) begins &= ~(1u << i);
+            }
             t32 += 32;
         }
         if (!begins) break;
         t0 = t32 - 32 + __ffs(begins) - 1;
-        const int64_t page = page_of(t0);
-        const int64_t slot0 = p.slots[t0];
+        const int64_t slot0 = p.slots[t0], page = page_of_slot(slot0);
         const int place = (int)(slot0 & (page_size - 1));
-        // the run: the tokens of the same page that follow, and whether they follow place by place
+        // the run: up to the last token of the same page, whether none in it is skipped, and whether all follow place by place
         int n = 1;
-        bool in_order = true;
-        while (true) {
-            const int64_t t = t0 + n + lane, slot = t < p.T ? p.slots[t] : -1;
-            const unsigned ok = __ballot_sync(~0u, slot >= 0 && slot < p.n_slots && slot >> p.page_log2 == page);
-            const unsigned next = __ballot_sync(~0u, slot == slot0 + n + lane);
-            const int more = ok == ~0u ? 32 : __ffs(~ok) - 1;
-            in_order = in_order && (~next & (more == 32 ? ~0u : (1u << more) - 1u)) == 0;
-            n += more;
-            if (more < 32) break;
+        bool dense = true, in_order = true;
+        for (int at = 1;; at += 32) {
+            const int64_t t = t0 + at + lane, slot = t < p.T ? p.slots[t] : -1, other = page_of_slot(slot);
+            const unsigned same = __ballot_sync(~0u, other == page), end = __ballot_sync(~0u, other >= 0 && other != page);
+            const unsigned next = __ballot_sync(~0u, slot == slot0 + at + lane);
+            const unsigned more = end ? same & ((end & -end) - 1) : same;  // those in front of the first of another page
+            if (more && at + __ffs(more) - 2 - (n - 1) <= most_skipped) {
+                const int last = 31 - __clz(more);
+                const unsigned all = last == 31 ? ~0u : (2u << last) - 1u;
+                dense = dense && n == at && more == all;
+                in_order = in_order && (~next & all) == 0;
+                n = at + last + 1;
+            }
+            if (end || at + 32 - n > most_skipped || t0 + at + 32 >= p.T) break;
         }
+        in_order = in_order && dense;
         // this thread's pieces: column `col` of the rows row, row + step, ... (a power of two of pieces per row divides the block)
         const int pieces = n << per_row_log2, row = tid >> per_row_log2, col = (tid & ((1 << per_row_log2) - 1)) << 3, step = kThreads >> per_row_log2;
         const T16* first = x + (t0 + row) * ldx + (int64_t)head * dim + col;
         auto piece = [&](int j) { return first + (int64_t)j * step * ldx; };  // the j-th
-        uint4 held[kHeld];
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-            held[j] = tid + j * kThreads < pieces ? load8<kBf16, kVec>(piece(j)) : make_uint4(0, 0, 0, 0);
-        float* scale = scales + page * p.heads + head;
-        const float before = place > 0 ? *scale : 0.0f;
-        auto block_max = [&](uint32_t m) {
-            m = __reduce_max_sync(~0u, max(m & 0xFFFFu, m >> 16));
-            __syncthreads();  // whoever read warp_max before has it
-            if (lane == 0) warp_max[tid >> 5] = m;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kThreads / 32; ++w) m = max(m, warp_max[w]);
-            return m;
-        };
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j) top = largest8(held[j], top);
-        for (int j = kHeld; tid + j * kThreads < pieces; ++j) top = largest8(load8<kBf16, kVec>(piece(j)), top);
-        top = block_max(top);
-        const bool finite = top < kInfinity;
-        if (!finite) {
-            top = 0;
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) top = largest_finite8<kBf16>(held[j], top);
-            for (int j = kHeld; tid + j * kThreads < pieces; ++j) top = largest_finite8<kBf16>(load8<kBf16, kVec>(piece(j)), top);
-            top = block_max(top);
-        }
-        const float m = Half<kBf16>::unpack(top).x;
-        const float wanted = m < 7.888609052e-31f ? 0.0f : __fmul_rn(m, 1.0f / 127.0f);  // 2^-100: its reciprocal stays finite
-        const float after = fmaxf(before, wanted);
-        const float inverse = after > 0.0f ? 1.0f / after : 0.0f;
-        int8_t* block = cache + ((page * p.heads + head) << (p.page_log2 + p.dim_log2));
-        if (after > before && place > 0) {
-            const float ratio = before / after;
-            uint32_t* old = reinterpret_cast<uint32_t*>(block);
-            for (int i = tid; i < place << (p.dim_log2 - 2); i += kThreads) old[i] = rescale4(old[i], ratio);
-        }
-        int8_t* to = block + (place << p.dim_log2) + 8 * tid;  // where the places follow, the pieces do
-        auto out = [&](int j) {
-            if (in_order) return reinterpret_cast<uint2*>(to + 8 * kThreads * j);
-            const int at = (int)(p.slots[t0 + row + j * step] & (page_size - 1));
-            return reinterpret_cast<uint2*>(block + (at << p.dim_log2) + col);
-        };
-        auto store = [&](auto quantise_piece) {
+        // kSkips: some of the rows are to be left out
+        auto write = [&](auto skips) {
+            constexpr bool kSkips = decltype(skips)::value;
+            auto live = [&](int j) { return tid + j * kThreads < pieces && (!kSkips || page_of(t0 + row + j * step) >= 0); };
+            uint4 held[kHeld];
 #pragma unroll
             for (int j = 0; j < kHeld; ++j)
-                if (tid + j * kThreads < pieces) *out(j) = quantise_piece(held[j]);
-            for (int j = kHeld; tid + j * kThreads < pieces; ++j) *out(j) = quantise_piece(load8<kBf16, kVec>(piece(j)));
+                held[j] = live(j) ? load8<kBf16, kVec>(piece(j)) : make_uint4(0, 0, 0, 0);
+            float* scale = scales + page * p.heads + head;
+            const float before = place > 0 ? *scale : 0.0f;
+            auto block_max = [&](uint32_t m) {
+                m = __reduce_max_sync(~0u, max(m & 0xFFFFu, m >> 16));
+                __syncthreads();  // whoever read warp_max before has it
+                if (lane == 0) warp_max[tid >> 5] = m;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kThreads / 32; ++w) m = max(m, warp_max[w]);
+                return m;
+            };
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) top = largest8(held[j], top);
+            for (int j = kHeld; tid + j * kThreads < pieces; ++j)
+                if (live(j)) top = largest8(load8<kBf16, kVec>(piece(j)), top);
+            top = block_max(top);
+            const bool finite = top < kInfinity;
+            if (!finite) {
+                top = 0;
+#pragma unroll
+                for (int j = 0; j < kHeld; ++j) top = largest_finite8<kBf16>(held[j], top);
+                for (int j = kHeld; tid + j * kThreads < pieces; ++j)
+                    if (live(j)) top = largest_finite8<kBf16>(load8<kBf16, kVec>(piece(j)), top);
+                top = block_max(top);
+            }
+            const float m = Half<kBf16>::unpack(top).x;
+            const float wanted = m < 7.888609052e-31f ? 0.0f : __fmul_rn(m, 1.0f / 127.0f);  // 2^-100: its reciprocal stays finite
+            const float after = fmaxf(before, wanted);
+            const float inverse = after > 0.0f ? 1.0f / after : 0.0f;
+            int8_t* block = cache + ((page * p.heads + head) << (p.page_log2 + p.dim_log2));
+            if (after > before && place > 0) {
+                const float ratio = before / after;
+                uint32_t* old = reinterpret_cast<uint32_t*>(block);
+                for (int i = tid; i < place << (p.dim_log2 - 2); i += kThreads) old[i] = rescale4(old[i], ratio);
+            }
+            int8_t* to = block + (place << p.dim_log2) + 8 * tid;  // where the places follow, the pieces do
+            auto out = [&](int j) {
+                if (in_order) return reinterpret_cast<uint2*>(to + 8 * kThreads * j);
+                const int at = (int)(p.slots[t0 + row + j * step] & (page_size - 1));
+                return reinterpret_cast<uint2*>(block + (at << p.dim_log2) + col);
+            };
+            auto store = [&](auto quantise_piece) {
+#pragma unroll
+                for (int j = 0; j < kHeld; ++j)
+                    if (live(j)) *out(j) = quantise_piece(held[j]);
+                for (int j = kHeld; tid + j * kThreads < pieces; ++j)
+                    if (live(j)) *out(j) = quantise_piece(load8<kBf16, kVec>(piece(j)));
+            };
+            if (finite) store([&](uint4 w) { return quantise8<kBf16>(w, inverse); });
+            else store([&](uint4 w) { return quantise8_any<kBf16>(w, inverse); });
+            __syncthreads();  // every thread has read the old scale
+            if (tid == 0) *scale = after;
         };
-        if (finite) store([&](uint4 w) { return quantise8<kBf16>(w, inverse); });
-        else store([&](uint4 w) { return quantise8_any<kBf16>(w, inverse); });
-        __syncthreads();  // every thread has read the old scale
-        if (tid == 0) *scale = after;
+        if (dense) write(std::false_type());
+        else write(std::true_type());
     }
 }
 
