@@ -21,6 +21,7 @@
 
 #include "gemm_common.cuh"
 #include "kv_attention.cuh"
+#include "ptx_serve.cuh"
 
 namespace awe {
 namespace {

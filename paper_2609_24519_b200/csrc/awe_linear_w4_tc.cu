@@ -17,6 +17,7 @@
 
 #include "gemm_common.cuh"
 #include "linear_w4.cuh"
+#include "ptx_serve.cuh"
 
 namespace awe {
 namespace {
