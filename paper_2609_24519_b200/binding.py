@@ -154,7 +154,10 @@ def _stream(stream) -> int:
     lookup takes 0.1 us; building a Stream object to read its address takes 3."""
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        try:  # not public, so other versions of torch may lack them
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:
+            return torch.cuda.current_stream().cuda_stream
     return int(getattr(stream, "cuda_stream", stream))
 
 
