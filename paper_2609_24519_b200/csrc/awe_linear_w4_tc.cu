@@ -591,7 +591,7 @@ awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, boo
     while ((int64_t)1 << p.group_log2 < W.group && p.group_log2 < 31) ++p.group_log2;
     p.groups = (int)((W.K + W.group - 1) / W.group);
     p.scale_bf16 = W.scale_type == AWE_BF16, p.y_f32 = y_f32;
-    p.x_tma = (uintptr_t)x % 16 == 0 && (ldx % 8 == 0 || M == 1);
+    p.x_tma = (uintptr_t)x % 16 == 0 && ldx % 8 == 0;
     const int slab_groups = std::max(1, kSlabK >> p.group_log2);
     p.scale_pitch = (int)round_up(2 * slab_groups, 16) + 16;
     p.zero_pitch = p.zero ? (int)round_up(slab_groups, 16) + 16 : 0;
@@ -605,7 +605,7 @@ awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, boo
     awe_status_t s;
     if (aligned && (s = make_map_2d(h, W.codes_dev, true, (W.K + 1) / 2, W.N, W.ld / 2, kStageK / 2, kRowsN, CU_TENSOR_MAP_SWIZZLE_128B, &mc)) != AWE_OK)
         return s;
-    if (p.x_tma && (s = make_map_2d(h, x, false, W.K, M, M == 1 ? round_up(2 * W.K, 16) : 2 * ldx, 64, mt, CU_TENSOR_MAP_SWIZZLE_128B, &mx)) != AWE_OK)
+    if (p.x_tma && (s = make_map_2d(h, x, false, W.K, M, 2 * ldx, 64, mt, CU_TENSOR_MAP_SWIZZLE_128B, &mx)) != AWE_OK)
         return s;
     switch (mt) {
         case 16: return launch<16>(h, mc, mx, p, bf16, aligned, st);
