@@ -553,16 +553,16 @@ awe_status_t launch(awe_ctx* h, const CUtensorMap& mc, const CUtensorMap& mx, Tc
     // fit than the SMs have room for (128 blocks in 16 clusters of 8 take 20 us where 16 of 4 take 12), so the runtime is
     // asked, once per size.
     const dim3 tiles((p.N + kRowsN - 1) / kRowsN, 1, (p.M + kMt - 1) / kMt);
-    static std::atomic<int> fit[kMaxCluster + 1];  // clusters of each size that are resident at once, plus 1
+    static std::atomic<int> fit[64][kMaxCluster + 1];  // by device: clusters of each size that are resident at once, plus 1
     int parts = std::max(1, std::min(kMaxCluster, p.K / (2 * kStageK)));
     for (; parts > 1; --parts) {
         if ((int64_t)tiles.x * tiles.z * parts > h->sm_count) continue;
-        int n = fit[parts].load(std::memory_order_relaxed) - 1;
+        int n = fit[h->device & 63][parts].load(std::memory_order_relaxed) - 1;
         if (n < 0) {
             attr = cluster_attribute(parts);
             cfg.gridDim = dim3(1, parts, 1);
             if (cudaOccupancyMaxActiveClusters(&n, linear_w4_tc_kernel<kMt, kBf16, kAligned>, &cfg) != cudaSuccess) return AWE_ERR_CUDA;
-            fit[parts].store(n + 1, std::memory_order_relaxed);
+            fit[h->device & 63][parts].store(n + 1, std::memory_order_relaxed);
         }
         if ((int64_t)tiles.x * tiles.z <= n) break;
     }
