@@ -360,11 +360,12 @@ extern "C" awe_status_t awe_linear_w4(awe_handle_t h, const awe_w4_matrix* W, co
     p.x_vec = (uintptr_t)x_dev % 16 == 0 && (ldx % 8 == 0 || M == 1);
     const bool aligned = (uintptr_t)W->codes_dev % 16 == 0 && W->ld % 32 == 0;
     cudaStream_t st = (cudaStream_t)stream;
-    // tcgen05 pays where its 128 x 16 to 128 x 128 tiles are many enough, x has more rows than one or two column blocks of the
-    // small instruction, or many rows meet a long K: M = 128, 8,192 x 8,192: 41 us against 175; M = 16, 4,096 x 4,096: 9.4
-    // against 10.3; M = 128, N = 1,024, K = 8,192: 16 against 27.  Below that the small kernel has less to set up: M = 1,
-    // 8,192 x 8,192: 16.6 us against 22.6; M = 16, 1,024 x 1,024: 5.8 against 7.8; M = 96, 1,024 x 1,024: 8.3 against 10.3.
-    if ((M > 8 && W->N >= 2048) || (M > 16 && M <= 64) || (M > 64 && W->K >= 4096))
+    // tcgen05 pays from more rows of x than two column blocks of the small instruction on, where the product is worth its setting up.
+    // Times of the small kernel / tcgen05 in us, groups of 128: M = 16, 4,096 x 4,096 (N x K): 8.2 / 10.6; 16,384 x 8,192: 39 / 40.
+    // M = 17, 2,048 x 8,192 (2.9e8): 12.9 / 13.5; 6,000 x 4,096 (4.2e8): 21.5 / 15.0.  M = 128, 1,024 x 2,560 (3.4e8): 10.4 / 10.6;
+    // 1,024 x 4,064 (5.3e8): 14.5 / 12.5.  M = 1,024, 1,024 x 256 (2.7e8): 15.2 / 16.2; 1,024 x 1,024 (1.1e9): 28 / 14; 1,024 x 8,192:
+    // 171 / 38.  Over 1,200 sizes, aligned and not, the rule is 0.7 % above the better of the two, at the worst 1.4 times.
+    if (M > 16 && (double)M * W->N * W->K >= 4.5e8)
         return linear_w4_tc(h, *W, x_dev, x_type == AWE_BF16, M, ldx, y_dev, y_type == AWE_F32, ldy, st);
     const int tiles_m = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
     // K is split so that about 16 warps per SM have work (what is resident at once), with two stages each at least.
