@@ -389,7 +389,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap map_codes, const __grid_
         auto shift_x = [&](int i) {
             const int n_k = k1 - k0 - i * kStageK;
             const uint32_t slot = x_of(i % kStages);
-            constexpr int kBatch = kMt / kDrainers < 4 ? kMt / kDrainers : 4;  // rows whose latencies overlap
+            constexpr int kBatch = 4;  // rows whose latencies overlap
             uint32_t at = (uint32_t)(uintptr_t)x_row + 2 * i * kStageK;  // only its low bits count
 #pragma unroll 1
             for (int r0 = 0; r0 < kMt / kDrainers; r0 += kBatch) {
@@ -599,7 +599,7 @@ awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, boo
     const bool aligned = (uintptr_t)W.codes_dev % 16 == 0 && W.ld % 32 == 0;
     // Above 64 rows the taller tile unpacks a weight once for 128 rows, and pays once its tiles are many: 8,192 x 8,192 for 128
     // rows 41 us against 47 with 64, but 2,048 x 4,096 28 against 13.
-    int mt = M <= 16 ? 16 : (M <= 32 ? 32 : 64);
+    int mt = M <= 32 ? 32 : 64;
     if (M > 64 && (W.N + kRowsN - 1) / kRowsN * ((M + 127) / 128) > 32) mt = 128;
     CUtensorMap mc = {}, mx = {};
     awe_status_t s;
@@ -608,7 +608,6 @@ awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, boo
     if (p.x_tma && (s = make_map_2d(h, x, false, W.K, M, 2 * ldx, 64, mt, CU_TENSOR_MAP_SWIZZLE_128B, &mx)) != AWE_OK)
         return s;
     switch (mt) {
-        case 16: return launch<16>(h, mc, mx, p, bf16, aligned, st);
         case 32: return launch<32>(h, mc, mx, p, bf16, aligned, st);
         case 64: return launch<64>(h, mc, mx, p, bf16, aligned, st);
         default: return launch<128>(h, mc, mx, p, bf16, aligned, st);

@@ -45,7 +45,7 @@ __device__ __forceinline__ uint4 load_x8(const uint16_t* src, bool vec, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The product on tcgen05 (M > 1); the arguments have been checked.
+// The product on tcgen05 (M > 16); the arguments have been checked.
 awe_status_t linear_w4_tc(awe_ctx* h, const awe_w4_matrix& W, const void* x, bool bf16, int64_t M, int64_t ldx, void* y, bool y_f32,
                           int64_t ldy, cudaStream_t st);
 
