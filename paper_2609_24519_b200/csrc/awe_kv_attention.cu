@@ -31,6 +31,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStepTokens = 16 * kWarps;
 constexpr int kWholeTokens = 256;
+constexpr int64_t kWholeScans = 1 << 19;
 
 // The steps of one request: tokens [lo, hi) in steps of kStepTokens, for each of `units` units.
 struct Request {
@@ -637,15 +638,18 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     if (use_tc(*cache, T, B, n_q_heads, group, max_pages * cache->page_size, window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, workspace_dev, (cudaStream_t)stream);
     p.blocks = blocks_of(h->sm_count, cache->head_dim, nt);
-    // Short contexts: a block per unit and no second launch (777 tokens of 8 heads: 9.0 us in parts with the join).
+    // Short contexts: a block per unit and no second launch.  Each block scans all requests, so it pays while the units times the
+    // requests are few: up to 256 tokens for one query, 8 heads of 4 queries each, us whole / in parts with the join: 1 request
+    // 7.0 / 7.6, 64 16.2 / 17.6, 128 25.2 / 26.6, 256 50 / 47, 2,048 902 / 337; 1 head of 8: 128 7.6 / 11.1, 512 20.7 / 22.3, 1,024 47 / 38.
     int64_t tokens = max_pages * cache->page_size;
     if (window > 0) tokens = std::min(tokens, window + T / B + kStepTokens);
-    p.whole = tokens <= kWholeTokens;
+    const int64_t units = (T * group / (8 * nt) + B) * cache->n_heads;
+    p.whole = tokens <= kWholeTokens && units * B <= kWholeScans;
     const Workspace w = workspace_of(p.blocks, 8 * nt, cache->head_dim, B);
     p.unit_steps = (int64_t*)workspace_dev;
     p.part_vec = (float*)((uint8_t*)workspace_dev + w.vec);
     p.part_stat = (float4*)((uint8_t*)workspace_dev + w.stat);
-    if (p.whole) p.blocks = (int)std::min<int64_t>((T * group / (8 * nt) + B) * cache->n_heads, INT32_MAX);
+    if (p.whole) p.blocks = (int)units;
     auto run = [&](auto dim, auto tiles) {
         constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
         return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)

@@ -223,3 +223,17 @@ def test_bf16_queries_at_the_ends_of_their_range(rows, q_scale):
     q = (normal(rng, rows, 8, 128) * q_scale).to(torch.bfloat16)
     scale = float(np.float32(0.09 / max(q_scale, 2.0 ** -60)))
     check(cache, q, "bf16", [0, rows], [640], one_request(rng, 40), scale, prompts=rows == 200, floor=FLOOR)
+
+
+# ------------------------------------------------------------------ many requests of short contexts
+@pytest.mark.parametrize("B,launches", [(100, 1), (2048, 2)])
+def test_short_contexts_of_many_requests(B, launches):
+    """A block per unit, each of which scans the requests, where those are few; else the units in parts."""
+    rng = np.random.default_rng(B)
+    ctx = rng.integers(0, 40, B).tolist()
+    cache = make_cache(rng, 500, 2, 16, 64)
+    table = rng.integers(0, 500, (B, 3))
+    q = normal(rng, B, 2, 64).to(torch.bfloat16)
+    before = b.awe_launch_count(handle())
+    check(cache, q, "bf16", np.arange(B + 1), ctx, table, 0.125, floor=FLOOR)
+    assert b.awe_launch_count(handle()) - before == launches
