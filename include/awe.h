@@ -421,7 +421,9 @@ size_t awe_kv_attention_workspace_bytes(awe_handle_t h, const awe_kv_cache* cach
  * ldq, out_dev alike with ldo; lse_dev (T x n_q_heads floats, natural logarithm of the sum of exponentials) may
  * be NULL.  Rounded before the sums: the softmax weights (for prompts: times the values' scales), to FP16, each by at most 2^-11 of itself
  * or, below 2^-24 of the largest so far among the tokens that are summed together, by 2^-35 of that one; and elements of BF16 queries
- * below 2^-32 of their row's largest, which lose bits.  q_dev and out_dev 16-B aligned, ldq and ldo multiples of 8.  workspace_dev: 256-B aligned. */
+ * below 2^-32 of their row's largest, which lose bits.  The kernel is chosen by what the host knows: T / B and max_pages, which is best no
+ * larger than the longest request needs (ld_table may be).  q_dev and out_dev 16-B aligned, ldq and ldo multiples of 8.
+ * workspace_dev: 256-B aligned. */
 awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const void* q_dev, awe_float_t type,
                               int64_t T, int64_t n_q_heads, int64_t ldq, const int32_t* q_start_dev,
                               const int32_t* ctx_len_dev, int64_t B, const int32_t* block_table_dev,

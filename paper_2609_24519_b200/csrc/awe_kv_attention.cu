@@ -541,9 +541,10 @@ int row_tiles(int64_t T, int64_t B, int64_t group, int64_t head_dim) {
 }
 
 // tcgen05 pays from about 64 query rows per request and head on, where the work fills its units of 256 rows x 128
-// tokens: 8 heads of 128, one request of 4,096 tokens, 128 rows 36 us against 39, 1,024 rows 81 against 184; 16 or 32 rows
-// 32 us against 25; 512 tokens, 512 rows 32 us against 25, 1,024 rows 36 against 45.  The host knows the tokens only by the
-// table's width.
+// tokens.  us of the kernel for few rows / on tcgen05, 8 heads of 128: one request of 4,096 tokens, 64 rows 28 / 28, 128 rows 40 / 31,
+// 1,024 rows 177 / 65; of 512 tokens, 512 rows 25 / 29, 1,024 rows 43 / 32; 16 requests of 16,384 tokens, 16 rows 186 / 334, 64 rows
+// 678 / 340.  Over 572 sizes the rule is 0.5 % above the better of the two, at the worst 1.5 times (one head, one request).  The host knows
+// the tokens only by the table's width, and a request's rows by their mean.
 bool use_tc(const awe_kv_cache& cache, int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t tokens, int64_t window) {
     const int64_t head_dim = cache.head_dim;
     if (head_dim > 128 || T * group < 64 * B) return false;
