@@ -20,7 +20,7 @@ namespace {
 using namespace serve;
 
 constexpr int kThreads = 128;
-constexpr int kHeld = 8;  // 16-byte pieces a thread keeps in registers between the two passes
+constexpr int kMostHeld = 8;  // 16-byte pieces a thread keeps in registers between the two passes
 
 struct WriteParams {
     const void *k, *v;
@@ -98,10 +98,10 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float ratio) {
     return q;
 }
 
-// grid: (windows of tokens, heads, keys / values).  Eight blocks on an SM: what the 64 registers that this leaves cost is less than
-// what more loads under way bring (19.6 k tokens of 8 heads of 128: 30.1 us; six blocks of 80 registers 32.7, four of 114 39.3).
+// grid: (windows of tokens, heads, keys / values).  Seven blocks on an SM (72 registers): more loads are under way than with six, and
+// nothing spills as it does with eight.  19.6 k tokens of 8 heads of 128: 30.4 us; with six 31.8.
 template <bool kBf16, bool kVec>
-__global__ void __launch_bounds__(kThreads, 8) kv_write_kernel(WriteParams p) {
+__global__ void __launch_bounds__(kThreads, 7) kv_write_kernel(WriteParams p) {
     using T16 = typename Half<kBf16>::type;
     __shared__ uint32_t warp_max[kThreads / 32];
     constexpr uint32_t kInfinity = kBf16 ? 0x7F80u : 0x7C00u;
@@ -129,25 +129,29 @@ __global__ void __launch_bounds__(kThreads, 8) kv_write_kernel(WriteParams p) {
     grid_wait();
     const int64_t t_begin = (int64_t)blockIdx.x * p.window, t_end = min(p.T, t_begin + p.window);
     unsigned begins = 0;  // of the 32 tokens from t32, those that begin a run (every warp finds out for itself)
+    int64_t mine = -1;    // slot of this lane's of those
     for (int64_t t32 = t_begin, t0 = 0; t32 < t_end || begins; begins &= begins - 1) {
         while (!begins && t32 < t_end) {
-            const int64_t t = t32 + lane, mine = t < t_end ? page_of(t) : -1, before = mine >= 0 && t > 0 ? page_of(t - 1) : -1;
-            begins = __ballot_sync(~0u, mine >= 0 && before != mine);
-            for (unsigned ask = __ballot_sync(~0u, mine >= 0 && t > 0 && before < 0); ask; ask &= ask - 1) {
+            const int64_t t = t32 + lane, before = t > 0 && t < t_end ? p.slots[t - 1] : -1;
+            mine = t < t_end ? p.slots[t] : -1;
+            const int64_t page = page_of_slot(mine), page_before = page_of_slot(before);
+            begins = __ballot_sync(~0u, page >= 0 && page_before != page);
+            for (unsigned ask = __ballot_sync(~0u, page >= 0 && page_before < 0 && t > 0); ask; ask &= ask - 1) {
                 const int i = __ffs(ask) - 1;
-                if (!no_run_before(t32 + i, __shfl_sync(~0u, mine, i))) begins &= ~(1u << i);
+                if (!no_run_before(t32 + i, __shfl_sync(~0u, page, i))) begins &= ~(1u << i);
             }
             t32 += 32;
         }
         if (!begins) break;
         t0 = t32 - 32 + __ffs(begins) - 1;
-        const int64_t slot0 = p.slots[t0], page = page_of_slot(slot0);
+        const int64_t slot0 = __shfl_sync(~0u, mine, __ffs(begins) - 1), page = page_of_slot(slot0);
         const int place = (int)(slot0 & (page_size - 1));
         // the run: up to the last token of the same page, whether none in it is skipped, and whether all follow place by place
-        int n = 1;
-        bool dense = true, in_order = true;
-        for (int at = 1;; at += 32) {
-            const int64_t t = t0 + at + lane, slot = t < p.T ? p.slots[t] : -1, other = page_of_slot(slot);
+        int n = 1, at = 1;
+        bool dense = true, in_order = true, more_to_see = true;
+        auto slot_of = [&](int64_t t) { return t < p.T ? p.slots[t] : -1; };
+        auto look = [&](int64_t slot) {  // at the 32 tokens from t0 + at
+            const int64_t other = page_of_slot(slot);
             const unsigned same = __ballot_sync(~0u, other == page), end = __ballot_sync(~0u, other >= 0 && other != page);
             const unsigned next = __ballot_sync(~0u, slot == slot0 + at + lane);
             const unsigned more = end ? same & ((end & -end) - 1) : same;  // those in front of the first of another page
@@ -158,18 +162,30 @@ __global__ void __launch_bounds__(kThreads, 8) kv_write_kernel(WriteParams p) {
                 in_order = in_order && (~next & all) == 0;
                 n = at + last + 1;
             }
-            if (end || at + 32 - n > most_skipped || t0 + at + 32 >= p.T) break;
+            at += 32;
+            more_to_see = !end && at - n <= most_skipped && t0 + at < p.T;
+        };
+        look(slot_of(t0 + at + lane));
+        while (more_to_see) {
+            constexpr int kAhead = 4;  // slots that are on their way together
+            int64_t ahead[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) ahead[i] = slot_of(t0 + at + 32 * i + lane);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (more_to_see) look(ahead[i]);
         }
         in_order = in_order && dense;
         // this thread's pieces: column `col` of the rows row, row + step, ... (a power of two of pieces per row divides the block)
         const int pieces = n << per_row_log2, row = tid >> per_row_log2, col = (tid & ((1 << per_row_log2) - 1)) << 3, step = kThreads >> per_row_log2;
         const T16* first = x + (t0 + row) * ldx + (int64_t)head * dim + col;
         auto piece = [&](int j) { return first + (int64_t)j * step * ldx; };  // the j-th
-        // kSkips: some of the rows are to be left out
+        // kSkips: some of the rows are to be left out (none is held: a short form for a rare case)
         auto write = [&](auto skips) {
             constexpr bool kSkips = decltype(skips)::value;
+            constexpr int kHeld = kSkips ? 0 : kMostHeld;
             auto live = [&](int j) { return tid + j * kThreads < pieces && (!kSkips || page_of(t0 + row + j * step) >= 0); };
-            uint4 held[kHeld];
+            uint4 held[kMostHeld];
 #pragma unroll
             for (int j = 0; j < kHeld; ++j)
                 held[j] = live(j) ? load8<kBf16, kVec>(piece(j)) : make_uint4(0, 0, 0, 0);
