@@ -543,7 +543,8 @@ int row_tiles(int64_t T, int64_t B, int64_t group, int64_t head_dim) {
 // tcgen05 pays from about 64 query rows per request and head on, where the work fills its units of 256 rows x 128
 // tokens.  us of the kernel for few rows / on tcgen05, 8 heads of 128: one request of 4,096 tokens, 64 rows 28 / 28, 128 rows 40 / 31,
 // 1,024 rows 177 / 65; of 512 tokens, 512 rows 25 / 29, 1,024 rows 43 / 32; 16 requests of 16,384 tokens, 16 rows 186 / 334, 64 rows
-// 678 / 340.  Over 572 sizes the rule is 0.5 % above the better of the two, at the worst 1.5 times (one head, one request).  The host knows
+// 678 / 340.  Of 4,096 tokens each, one request of 2,048 queries among 63 of one: 1,279 / 635; one of 512 among 255: 1,003 / 1,628; one
+// of 512 among 63: 504 / 476 (the rule takes the first).  Over 572 sizes of equal requests the rule is 0.5 % above the better of the two, at the worst 1.5 times (one head, one request).  The host knows
 // the tokens only by the table's width, and a request's rows by their mean.
 bool use_tc(const awe_kv_cache& cache, int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t tokens, int64_t window) {
     const int64_t head_dim = cache.head_dim;

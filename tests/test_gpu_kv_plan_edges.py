@@ -1,4 +1,4 @@
-"""The cache plan from several host threads."""
+"""The cache plan from several host threads, with lengths that pass 31 bits, and with outputs that lie in its inputs."""
 import threading
 
 import pytest
