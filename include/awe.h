@@ -431,6 +431,86 @@ awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const v
                               void* out_dev, int64_t ldo, float* lse_dev, void* workspace_dev,
                               size_t workspace_bytes, void* stream);
 
+/* ---- A paged cache of half that size: keys and values of 4 bits with a scale and a zero point for every token and head,
+ * so that a token is written once and never again.
+ *
+ * Token `i` of page p, head g: row r = (p * n_heads + g) * page_size + i of each array.  Its head_dim codes are AWE_I4_PACKED in the
+ * head_dim / 2 bytes at r * head_dim / 2; its 16-bit parameter word is FP16 of 16 times the scale with the zero point (AWE_I4) in
+ * the place of the lowest four bits.  A code stands for scale * (code - zero): 7 significant bits by at most 15, so FP16 holds the
+ * value exactly.  Scales are read as at least 2^-18 (of a word never written, 0, too) and at most 4,064. */
+typedef struct {
+    uint8_t* k_dev;          /* n_pages x n_heads x page_size x head_dim / 2 bytes, 16-B aligned         */
+    uint8_t* v_dev;
+    uint16_t* k_param_dev;   /* n_pages x n_heads x page_size, 16-B aligned                              */
+    uint16_t* v_param_dev;
+    int64_t n_pages, n_heads;
+    int64_t page_size;       /* tokens of a page: a power of two, 16 .. 256                              */
+    int64_t head_dim;        /* 64, 128 or 256                                                           */
+} awe_kv4_cache;
+
+/* Angles of the position rotation: row `pos` of table_dev holds the dim / 2 cosines, then the dim / 2 sines, of position pos.
+ * Pair i of a head's first `dim` elements, (a, b), becomes (a cos - b sin, b cos + a sin); the rest stays as it is. */
+typedef struct {
+    const float* table_dev;  /* n_positions x dim, 16-B aligned                                          */
+    int64_t n_positions;
+    int64_t dim;             /* a multiple of 8, at most head_dim                                        */
+    int32_t interleaved;     /* pair i is elements 2i, 2i + 1; else i, i + dim / 2                       */
+} awe_rotary;
+
+/* Rotate T new tokens' queries (T x n_q_heads x head_dim, token stride ldq) into q_out_dev (token stride ldqo; q_dev itself with
+ * ldqo = ldq is allowed) and their keys, and store the rotated keys and the values (T x n_heads x head_dim, strides ldk, ldv)
+ * into their slots.  All rows are of `type` (AWE_F16, AWE_BF16), 16-B aligned, with strides that are multiples of 8 elements.
+ * positions_dev[t] is token t's position; a token whose position is outside 0 .. n_positions - 1 is left out altogether, one whose slot
+ * is negative or outside the pool is not stored.  rotary NULL: nothing is rotated and positions_dev may be NULL.  n_q_heads 0: no
+ * queries.  Each slot stands at most once in the list.
+ * Rotation in FP32: every product and sum rounded, queries rounded once more to their type.  Stored are, per token and head, with
+ * lo = min(0, smallest value), hi = max(0, largest), both cut to +-30,480: scale = (hi - lo) / 15 rounded up to 7 significant bits,
+ * 2^-18 at least; zero = -8 - round(lo / scale); code = round(x / scale) + zero, cut to -8 .. 7 (divisions in FP32, round to nearest, ties to
+ * even), so that a value is off by half a scale at most.  NaN is stored as 0 and infinities as the row's ends; neither counts for the scale. */
+awe_status_t awe_kv4_append(awe_handle_t h, const awe_kv4_cache* cache, const awe_rotary* rotary, awe_float_t type, int64_t T,
+                            int64_t n_q_heads, const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev,
+                            int64_t ldv, const int32_t* positions_dev, const int64_t* slots_dev, void* q_out_dev, int64_t ldqo,
+                            void* stream);
+
+/* The values of T slots (T x n_heads x head_dim, token strides ldk and ldv) as `type`: AWE_F16, which holds them exactly, or AWE_BF16.
+ * Rows of slots that are negative or outside the pool are left as they are.  k_out_dev and v_out_dev (either may be NULL) 16-B aligned,
+ * strides multiples of 8. */
+awe_status_t awe_kv4_read(awe_handle_t h, const awe_kv4_cache* cache, int64_t T, const int64_t* slots_dev, awe_float_t type, void* k_out_dev,
+                          int64_t ldk, void* v_out_dev, int64_t ldv, void* stream);
+
+/* Low-rank adapters of one projection: adapter i adds scale[i] * B_i (A_i x). */
+typedef struct {
+    const void* a_dev;       /* n_adapters x rank x K, of `type` (AWE_F16, AWE_BF16), 16-B aligned       */
+    const void* b_dev;       /* n_adapters x N x rank, likewise                                          */
+    const float* scale_dev;  /* n_adapters, or NULL: 1                                                   */
+    int64_t n_adapters;
+    int64_t rank;            /* a multiple of 8, at most 128; smaller adapters are filled up with zeros   */
+    int64_t N, K;            /* K a multiple of 8                                                        */
+    int32_t type;
+} awe_adapters;
+
+/* y(t) = base(t) + scale[a] * B_a (A_a x(t)) for the T tokens of B requests, a = adapter_dev[b] for the tokens q_start[b] ..
+ * q_start[b + 1] - 1 of request b; y = base where a is outside 0 .. n_adapters - 1.  The rows outside every request are left as they
+ * are.  x_dev: T x K of the adapters' type, 16-B aligned, ldx a multiple of 8.  base_dev, y_dev: T x N of y_type, the adapters' type or
+ * AWE_F32, any strides; base_dev may be y_dev itself (with ldb = ldy), or NULL for zeros.  Products are exact and summed in FP32; the rank's sums
+ * enter the second product as two values of `type`, which together hold 16 bits (BF16) or 21 (FP16) of the largest of the token's; y is rounded once. */
+awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* L, const void* x_dev, int64_t T, int64_t ldx,
+                                 const int32_t* q_start_dev, const int32_t* adapter_dev, int64_t B, const void* base_dev, int64_t ldb,
+                                 void* y_dev, awe_float_t y_type, int64_t ldy, void* stream);
+
+/* Log probabilities under softmax(scale * logits) of T rows of V logits (row stride ld; AWE_F16, AWE_BF16 or AWE_F32; any alignment of the
+ * element), natural logarithms, each output FP32 and each but top_* NULL if not wanted:
+ *   logprob_dev[t]                 of token tokens_dev[t]; 0 where that is outside 0 .. V - 1
+ *   entropy_dev[t], lse_dev[t]     -sum p log p, and the logarithm of the sum of exponentials
+ *   top_logprob_dev, top_id_dev    T x top_k: the top_k (0 .. 32, at most V) largest, in order, the lower token first among equals
+ * -inf is a token of probability 0; a row of nothing else has lse -inf, log probabilities -inf and entropy 0.  A row with NaN or +inf has NaN
+ * for all of them; NaN is never among the top (id -1 where fewer than top_k are left).  scale is above 0 and at most 1e30.  One pass over the
+ * logits; sums and maxima in FP32. */
+#define AWE_MAX_TOP 32
+awe_status_t awe_token_logprobs(awe_handle_t h, const void* logits_dev, awe_float_t type, int64_t T, int64_t V, int64_t ld, float scale,
+                                const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev, float* lse_dev, int64_t top_k,
+                                float* top_logprob_dev, int32_t* top_id_dev, void* stream);
+
 /* Wait for `stream` and read the handle's device status word: AWE_OK, or AWE_ERR_TIMEOUT with
  * *site (may be NULL) naming the wait that gave up.  The word is cleared by the read. */
 awe_status_t awe_last_device_status(awe_handle_t h, void* stream, int* site);

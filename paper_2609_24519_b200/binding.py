@@ -34,12 +34,15 @@ MAX_PRODUCTS, MAX_PLANES = 16, 8
 STATIC_WORKSPACE_BYTES = 24 << 20
 F16, BF16, F32 = 0, 1, 2
 KV_MAX_REQUESTS = 16384
+MAX_TOP = 32
 
 EXPORTS = ["awe_create", "awe_destroy", "awe_encoding_info", "awe_encoding_lut", "awe_planes_bytes",
            "awe_workspace_bytes", "awe_host_staging_bytes", "awe_encode", "awe_gemm_planes", "awe_gemm_exact",
            "awe_gemm_exact_host", "awe_gemm_exact_static", "awe_wide_moduli", "awe_wide_select", "awe_wide_workspace_bytes",
            "awe_wide_residues", "awe_wide_crt", "awe_gemm_exact_wide", "awe_reconstruct", "awe_fp4_product_raw", "awe_fp8_product_raw", "awe_last_device_status", "awe_selftest_bounded_wait", "awe_last_gemm_clock_mhz", "awe_launch_count",
-           "awe_status_string", "awe_linear_w4", "awe_kv_plan", "awe_kv_write", "awe_kv_attention_workspace_bytes", "awe_kv_attention"]
+           "awe_status_string", "awe_linear_w4", "awe_kv_plan", "awe_kv_write", "awe_kv_attention_workspace_bytes", "awe_kv_attention",
+           "awe_kv4_append", "awe_kv4_read", "awe_linear_adapters",
+           "awe_token_logprobs"]
 
 
 class EncodingDesc(ctypes.Structure):
@@ -65,6 +68,26 @@ class KvCache(ctypes.Structure):
     _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("k_scale_dev", ctypes.c_void_p),
                 ("v_scale_dev", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_heads", ctypes.c_int64),
                 ("page_size", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
+
+
+class Kv4Cache(ctypes.Structure):
+    """awe_kv4_cache; keeps the tensors it points into alive."""
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("k_param_dev", ctypes.c_void_p),
+                ("v_param_dev", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_heads", ctypes.c_int64),
+                ("page_size", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
+
+
+class Rotary(ctypes.Structure):
+    """awe_rotary; keeps the table alive."""
+    _fields_ = [("table_dev", ctypes.c_void_p), ("n_positions", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("interleaved", ctypes.c_int32)]
+
+
+class Adapters(ctypes.Structure):
+    """awe_adapters; keeps the tensors it points into alive."""
+    _fields_ = [("a_dev", ctypes.c_void_p), ("b_dev", ctypes.c_void_p), ("scale_dev", ctypes.c_void_p),
+                ("n_adapters", ctypes.c_int64), ("rank", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("type", ctypes.c_int32)]
 
 
 class AweError(RuntimeError):
@@ -118,6 +141,11 @@ def lib() -> ctypes.CDLL:
     L.awe_kv_attention_workspace_bytes.restype = sz
     L.awe_kv_attention.argtypes = [vp, kv, vp, i32, i64, i64, i64, vp, vp, i64, vp, i64, i64, f32, i32, i64, vp, i64, vp, vp,
                                    sz, vp]
+    kv4 = ctypes.POINTER(Kv4Cache)
+    L.awe_kv4_append.argtypes = [vp, kv4, ctypes.POINTER(Rotary), i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+    L.awe_kv4_read.argtypes = [vp, kv4, i64, vp, i32, vp, i64, vp, i64, vp]
+    L.awe_linear_adapters.argtypes = [vp, ctypes.POINTER(Adapters), vp, i64, i64, vp, vp, i64, vp, i64, vp, i32, i64, vp]
+    L.awe_token_logprobs.argtypes = [vp, vp, i32, i64, i64, i64, f32, vp, vp, vp, vp, i64, vp, vp, vp]
     L.awe_last_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     L.awe_selftest_bounded_wait.argtypes = [vp, i64, vp]
     L.awe_last_gemm_clock_mhz.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_double)]
@@ -359,6 +387,57 @@ def awe_kv_attention(h: Handle, cache: KvCache, q, dtype: int, T: int, n_q_heads
                                   _ptr(workspace), workspace_bytes, _stream(stream))
     if status:
         raise AweError(status, "awe_kv_attention")
+
+
+def kv4_cache(k, v, k_param, v_param, n_pages: int, n_heads: int, page_size: int, head_dim: int) -> Kv4Cache:
+    """Describes a paged 4-bit cache (awe_kv4_cache)."""
+    c = Kv4Cache(_ptr(k), _ptr(v), _ptr(k_param), _ptr(v_param), n_pages, n_heads, page_size, head_dim)
+    c.tensors = (k, v, k_param, v_param)
+    return c
+
+
+def rotary(table, n_positions: int, dim: int, interleaved: bool = False) -> Rotary:
+    """Describes a table of cosines and sines (awe_rotary)."""
+    r = Rotary(_ptr(table), n_positions, dim, interleaved)
+    r.tensors = (table,)
+    return r
+
+
+def adapters(a, b, scale, dtype: int, n_adapters: int, rank: int, N: int, K: int) -> Adapters:
+    """Describes the low-rank adapters of a projection (awe_adapters); scale may be None."""
+    L = Adapters(_ptr(a), _ptr(b), _ptr(scale), n_adapters, rank, N, K, dtype)
+    L.tensors = (a, b, scale)
+    return L
+
+
+def awe_kv4_append(h: Handle, cache: Kv4Cache, turn: Optional[Rotary], dtype: int, T: int, n_q_heads: int, q, ldq: int, k, ldk: int, v,
+                   ldv: int, positions, slots, q_out, ldqo: int, stream=None) -> None:
+    status = _lib.awe_kv4_append(h._h, cache, turn, dtype, T, n_q_heads, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(positions),
+                                 _ptr(slots), _ptr(q_out), ldqo, _stream(stream))
+    if status:
+        raise AweError(status, "awe_kv4_append")
+
+
+def awe_kv4_read(h: Handle, cache: Kv4Cache, T: int, slots, dtype: int, k_out, ldk: int, v_out, ldv: int, stream=None) -> None:
+    status = _lib.awe_kv4_read(h._h, cache, T, _ptr(slots), dtype, _ptr(k_out), ldk, _ptr(v_out), ldv, _stream(stream))
+    if status:
+        raise AweError(status, "awe_kv4_read")
+
+
+def awe_linear_adapters(h: Handle, L: Adapters, x, T: int, ldx: int, q_start, adapter, B: int, base, ldb: int, y, y_type: int, ldy: int,
+                        stream=None) -> None:
+    status = _lib.awe_linear_adapters(h._h, L, _ptr(x), T, ldx, _ptr(q_start), _ptr(adapter), B, _ptr(base), ldb, _ptr(y), y_type, ldy,
+                                     _stream(stream))
+    if status:
+        raise AweError(status, "awe_linear_adapters")
+
+
+def awe_token_logprobs(h: Handle, logits, dtype: int, T: int, V: int, ld: int, scale: float, tokens, logprob, entropy, lse, top_k: int,
+                       top_logprob, top_id, stream=None) -> None:
+    status = _lib.awe_token_logprobs(h._h, _ptr(logits), dtype, T, V, ld, scale, _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(lse),
+                                    top_k, _ptr(top_logprob), _ptr(top_id), _stream(stream))
+    if status:
+        raise AweError(status, "awe_token_logprobs")
 
 
 def awe_last_device_status(h: Handle, stream=None):

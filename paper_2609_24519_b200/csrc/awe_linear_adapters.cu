@@ -1,0 +1,514 @@
+// Low-rank adapters of many requests beside a shared projection (awe_linear_adapters).
+//
+//   u = A x (rank sums over K),   y = base + scale * B u (N sums over the rank)
+//
+// A unit is up to kTokens tokens of one request, and a cluster of blocks computes it in one launch: K is cut over the cluster's
+// warps, the parts of u are added in shared memory, over the blocks in distributed shared memory, and then N is cut over the same
+// warps.  Both products run on the 16-bit matrix instruction with FP32 sums.  The bytes of x, base, y and the adapters bound many
+// tokens, latency few; no operand is read by more than a few flops a byte, so operands go from global memory to registers directly:
+// the order of k (and of the rank) inside an instruction is free, and a thread takes eight (four) neighbours of a row.
+// u enters the second product as two 16-bit values, the rounded u and the rounded rest.
+//
+// Units are numbered without a scan: request b's first is q_start[b] / kTokens + b, which leaves room for all of its units before
+// those of request b + 1.  Some numbers have no unit; their clusters end at once.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "awe_internal.h"
+#include "serve_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace awe {
+namespace {
+
+using namespace serve;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMostCluster = 8;
+constexpr int kFew = 8, kMany = 32;  // tokens of a unit
+
+struct AdapterParams {
+    const void *a, *b, *x, *base;
+    void* y;
+    const float* scale;
+    const int32_t *q_start, *adapter;
+    int64_t ldx, ldb, ldy, n_adapters;
+    int T, B, N, K, rank;
+    int y_f32, vec;  // vec: rows of base and y lie on 16 bytes
+};
+
+struct Unit {
+    int token, n, adapter;  // n = 0: none
+};
+template <int kTokens>
+__device__ __forceinline__ Unit unit_of(const AdapterParams& p, int number) {
+    const int lane = threadIdx.x & 31;
+    // last request whose first unit is not behind `number`: 32 requests are asked at a time
+    int b = 0, first = -1, q0 = 0;
+    for (int n = p.B;;) {
+        const int stride = (n + 31) / 32, i = lane * stride;
+        const int start = i < n ? min(max(p.q_start[b + i], 0), p.T) : 0, unit = start / kTokens + b + i;
+        const unsigned fits = __ballot_sync(~0u, i < n && unit <= number);
+        if (!fits) return {0, 0, -1};
+        const int last = 31 - __clz(fits);
+        first = __shfl_sync(~0u, unit, last), q0 = __shfl_sync(~0u, start, last);
+        b += last * stride, n = min(stride, n - last * stride);
+        if (n == 1) break;
+    }
+    const int q1 = min(p.q_start[b + 1], p.T), adapter = p.adapter[b];
+    const int64_t token = q0 + (int64_t)(number - first) * kTokens;
+    return {(int)min(token, (int64_t)p.T), (int)max(min((int64_t)kTokens, q1 - token), (int64_t)0), adapter};
+}
+
+// A value as two of 16 bits.  FP16's range is narrow, so the values of a token are brought to [-2^15, 2^15] first (`down`).
+template <bool kBf16>
+__device__ __forceinline__ void split2(float x, float y, float down, uint32_t& hi, uint32_t& lo) {
+    if constexpr (!kBf16) x *= down, y *= down;
+    hi = Half<kBf16>::pack(x, y);
+    const float2 f = Half<kBf16>::unpack(hi);
+    lo = Half<kBf16>::pack(x - f.x, y - f.y);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// Exponent that brings magnitudes up to `largest` below 2^15; both powers of it stay normal.
+__device__ __forceinline__ int down_exponent(float largest) { return min(max((int)(__float_as_uint(largest) >> 23) - 127 - 14, -120), 120); }
+
+__device__ __forceinline__ uint4 load16_if(const void* from, bool live) {
+    return live ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ uint2 load8_if(const void* from, bool live) {
+    return live ? __ldg(reinterpret_cast<const uint2*>(from)) : make_uint2(0, 0);
+}
+template <bool kBf16>
+__device__ __forceinline__ float load_base(const AdapterParams& p, int64_t token, int n) {
+    if (!p.base) return 0.0f;
+    const int64_t at = token * p.ldb + n;
+    return p.y_f32 ? reinterpret_cast<const float*>(p.base)[at] : Half<kBf16>::to_float(reinterpret_cast<const typename Half<kBf16>::type*>(p.base)[at]);
+}
+template <bool kBf16>
+__device__ __forceinline__ void store_y(const AdapterParams& p, int64_t token, int n, float y) {
+    const int64_t at = token * p.ldy + n;
+    if (p.y_f32) reinterpret_cast<float*>(p.y)[at] = y;
+    else reinterpret_cast<typename Half<kBf16>::type*>(p.y)[at] = Half<kBf16>::from_float(y);
+}
+
+// A unit without an adapter: y = base, by all threads of the cluster.
+template <bool kBf16>
+__device__ __forceinline__ void copy_base(const AdapterParams& p, const Unit& u, int part, int parts) {
+    if (p.base == p.y) return;
+    for (int i = 0; i < u.n; ++i)
+        for (int n = part * kThreads + threadIdx.x; n < p.N; n += parts * kThreads) store_y<kBf16>(p, u.token + i, n, load_base<kBf16>(p, u.token + i, n));
+}
+
+// Few tokens: they are the instruction's 8 columns, ranks (then n) its 16 rows.  kRT tiles of 16 ranks.
+template <bool kBf16, int kRT>
+__global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterParams p) {
+    using T16 = typename Half<kBf16>::type;
+    constexpr int kValues = kRT * 16 * kFew;
+    constexpr int kAhead = kRT <= 2 ? 4 : (kRT == 4 ? 2 : 1);  // steps of k, and tiles of n, that are on their way together
+    __shared__ float sums[kWarps][kValues];
+    __shared__ float part_sums[kValues];
+    __shared__ float low[kValues];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    grid_wait();
+    const Unit u = unit_of<kFew>(p, blockIdx.x / parts);
+    if (u.n == 0) return;  // the whole cluster
+    if (u.adapter < 0 || u.adapter >= p.n_adapters) return copy_base<kBf16>(p, u, part, parts);
+    const int me = part * kWarps + warp, all = parts * kWarps;
+
+    // ---- u = A x
+    const T16* a = reinterpret_cast<const T16*>(p.a) + (int64_t)u.adapter * p.rank * p.K;
+    const T16* x = reinterpret_cast<const T16*>(p.x) + (int64_t)(u.token + min(g, u.n - 1)) * p.ldx;
+    float acc[kRT][4];
+#pragma unroll
+    for (int r = 0; r < kRT; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[r][i] = 0.0f;
+    const int steps = (p.K + 31) / 32;
+    for (int s0 = me; s0 < steps; s0 += all * kAhead) {
+        uint4 xw[kAhead], aw[kAhead][kRT][2];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = (s0 + i * all) * 32 + 8 * t;
+            const bool in = s0 + i * all < steps && k < p.K;
+            xw[i] = load16_if(x + k, in && g < u.n);
+#pragma unroll
+            for (int r = 0; r < kRT; ++r)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 16 * r + 8 * j + g;
+                    aw[i][r][j] = load16_if(a + (int64_t)row * p.K + k, in && row < p.rank);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int r = 0; r < kRT; ++r) {
+                const uint4 &lo = aw[i][r][0], &hi = aw[i][r][1];
+                const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
+                mma_16816<kBf16>(acc[r], f0, xw[i].x, xw[i].y);
+                mma_16816<kBf16>(acc[r], f1, xw[i].z, xw[i].w);
+            }
+    }
+    // rows of B and of base for the first tiles of n are fetched while u is put together
+    const T16* b = reinterpret_cast<const T16*>(p.b) + (int64_t)u.adapter * p.N * p.rank;
+    const int tiles = (p.N + 15) / 16;
+    uint2 bw[kAhead][kRT][2];
+    float base[kAhead][4];
+    auto fetch = [&](int tile0) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int tile = tile0 + i * all;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int n = 16 * tile + 8 * j + g;
+#pragma unroll
+                for (int r = 0; r < kRT; ++r) bw[i][r][j] = load8_if(b + (int64_t)n * p.rank + 16 * r + 4 * t, tile < tiles && n < p.N && 16 * r + 4 * t < p.rank);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) base[i][2 * j + c] = tile < tiles && n < p.N && 2 * t + c < u.n ? load_base<kBf16>(p, u.token + 2 * t + c, n) : 0.0f;
+            }
+        }
+    };
+    fetch(me);
+#pragma unroll
+    for (int r = 0; r < kRT; ++r)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(&sums[warp][(16 * r + 8 * j + g) * kFew + 2 * t]) = make_float2(acc[r][2 * j], acc[r][2 * j + 1]);
+    __syncthreads();
+    for (int i = tid; i < kValues; i += kThreads) {
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) s += sums[w][i];
+        part_sums[i] = s;
+    }
+    cluster.sync();
+    const float scale = p.scale ? p.scale[u.adapter] : 1.0f;
+    for (int i = tid; i < kValues; i += kThreads) {
+        float s[kMostCluster];
+#pragma unroll
+        for (int j = 0; j < kMostCluster; ++j) s[j] = j < parts ? cluster.map_shared_rank(part_sums, j)[i] : 0.0f;
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kMostCluster; ++j) v += s[j];
+        low[i] = v * scale;
+    }
+    cluster.barrier_arrive();  // this block has read the others' sums
+    __syncthreads();
+
+    // ---- y = base + B u: thread (g, t) holds of token g the ranks 4 t .. 4 t + 3 of each tile
+    uint32_t vh[kRT][2], vl[kRT][2];
+    float back[2] = {1.0f, 1.0f};  // of the tokens 2 t, 2 t + 1
+    {
+        float v[kRT][4], most = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRT; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[r][i] = low[(16 * r + 4 * t + i) * kFew + g], most = fmaxf(most, fabsf(v[r][i]));
+        float down = 1.0f;
+        if constexpr (!kBf16) {
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+            const int e = down_exponent(most);
+            down = power_of_two(-e);
+            back[0] = __shfl_sync(~0u, power_of_two(e), 8 * t), back[1] = __shfl_sync(~0u, power_of_two(e), 8 * t + 4);
+        }
+#pragma unroll
+        for (int r = 0; r < kRT; ++r)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) split2<kBf16>(v[r][2 * i], v[r][2 * i + 1], down, vh[r][i], vl[r][i]);
+    }
+    for (int tile0 = me; tile0 < tiles; tile0 += all * kAhead) {
+        if (tile0 != me) fetch(tile0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int tile = tile0 + i * all;
+            if (tile >= tiles) break;
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int r = 0; r < kRT; ++r) {
+                const uint32_t f[4] = {bw[i][r][0].x, bw[i][r][1].x, bw[i][r][0].y, bw[i][r][1].y};
+                mma_16816<kBf16>(d, f, vl[r][0], vl[r][1]);
+                mma_16816<kBf16>(d, f, vh[r][0], vh[r][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (const int n = 16 * tile + 8 * j + g; n < p.N && 2 * t + c < u.n)
+                        store_y<kBf16>(p, u.token + 2 * t + c, n, fmaf(d[2 * j + c], back[c], base[i][2 * j + c]));
+        }
+    }
+    cluster.barrier_wait();  // no block leaves while its sums are read
+}
+
+// Many tokens: 32 of them, in two tiles of the instruction's 16 rows; ranks (then n) are its 8 columns.  kRN tiles of 8 ranks.
+template <int kRN>
+struct Many {
+    static constexpr int kPitch = 8 * kRN + 4;  // floats of a token's sums
+    static constexpr int kSumsBytes = kWarps * kMany * kPitch * 4;
+    static constexpr int kOutPitch = 64 + 4;
+    static constexpr int kOutBytes = kWarps * 16 * kOutPitch * 4;  // in the sums' place once they are added
+    static constexpr int kPartAt = kSumsBytes > kOutBytes ? kSumsBytes : kOutBytes;
+    static constexpr int kLowAt = kPartAt + kMany * kPitch * 4;
+    static constexpr int kSmemBytes = kLowAt + kMany * kPitch * 4;
+};
+
+template <bool kBf16, int kRN>
+__global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterParams p) {
+    using M = Many<kRN>;
+    using T16 = typename Half<kBf16>::type;
+    extern __shared__ __align__(16) uint8_t smem[];
+    float* sums = reinterpret_cast<float*>(smem);
+    float* part_sums = reinterpret_cast<float*>(smem + M::kPartAt);
+    float* low = reinterpret_cast<float*>(smem + M::kLowAt);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    grid_wait();
+    const Unit u = unit_of<kMany>(p, blockIdx.x / parts);
+    if (u.n == 0) return;  // the whole cluster
+    if (u.adapter < 0 || u.adapter >= p.n_adapters) return copy_base<kBf16>(p, u, part, parts);
+    const int me = part * kWarps + warp, all = parts * kWarps;
+
+    // ---- u = A x: every warp has all tokens and ranks and its own steps of k
+    const T16* a = reinterpret_cast<const T16*>(p.a) + (int64_t)u.adapter * p.rank * p.K;
+    const T16* x = reinterpret_cast<const T16*>(p.x) + (int64_t)u.token * p.ldx;
+    {
+        float acc[2][kRN][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < kRN; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][r][i] = 0.0f;
+        const int steps = (p.K + 31) / 32;
+        constexpr int kAhead = kRN <= 4 ? 2 : 1;
+        for (int s0 = me; s0 < steps; s0 += all * kAhead) {
+            uint4 xw[kAhead][4], aw[kAhead][kRN];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int k = (s0 + i * all) * 32 + 8 * t;
+                const bool in = s0 + i * all < steps && k < p.K;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xw[i][j] = load16_if(x + (8 * j + g) * p.ldx + k, in && 8 * j + g < u.n);
+#pragma unroll
+                for (int r = 0; r < kRN; ++r) aw[i][r] = load16_if(a + (int64_t)(8 * r + g) * p.K + k, in && 8 * r + g < p.rank);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const uint4 &lo = xw[i][2 * m], &hi = xw[i][2 * m + 1];
+                    const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
+#pragma unroll
+                    for (int r = 0; r < kRN; ++r) {
+                        mma_16816<kBf16>(acc[m][r], f0, aw[i][r].x, aw[i][r].y);
+                        mma_16816<kBf16>(acc[m][r], f1, aw[i][r].z, aw[i][r].w);
+                    }
+                }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < kRN; ++r)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *reinterpret_cast<float2*>(sums + (warp * kMany + 16 * m + 8 * j + g) * M::kPitch + 8 * r + 2 * t) = make_float2(acc[m][r][2 * j], acc[m][r][2 * j + 1]);
+    }
+    __syncthreads();
+    for (int i = tid; i < kMany * 2 * kRN; i += kThreads) {  // four ranks of a token each
+        const int at = i / (2 * kRN) * M::kPitch + i % (2 * kRN) * 4;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float4 o = *reinterpret_cast<const float4*>(sums + w * kMany * M::kPitch + at);
+            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
+        }
+        *reinterpret_cast<float4*>(part_sums + at) = s;
+    }
+    cluster.sync();
+    const float scale = p.scale ? p.scale[u.adapter] : 1.0f;
+    for (int i = tid; i < kMany * 2 * kRN; i += kThreads) {
+        const int at = i / (2 * kRN) * M::kPitch + i % (2 * kRN) * 4;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < kMostCluster; ++j) {
+            if (j >= parts) break;
+            const float4 o = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part_sums, j) + at);
+            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
+        }
+        *reinterpret_cast<float4*>(low + at) = make_float4(s.x * scale, s.y * scale, s.z * scale, s.w * scale);
+    }
+    cluster.barrier_arrive();  // this block has read the others' sums
+    __syncthreads();
+
+    // ---- y = base + B u: a warp has one tile of 16 tokens and 64 columns of y at a time
+    constexpr int kRT = kRN / 2;
+    const int m = warp & 1;
+    uint32_t vh[kRT][4], vl[kRT][4];
+    float back[2] = {1.0f, 1.0f};  // of the tokens g, g + 8
+    {
+        const float* from[2] = {low + (16 * m + g) * M::kPitch + 4 * t, low + (16 * m + 8 + g) * M::kPitch + 4 * t};
+        float down[2] = {1.0f, 1.0f};
+        if constexpr (!kBf16) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float most = 0.0f;
+#pragma unroll
+                for (int r = 0; r < kRT; ++r) {
+                    const float4 v = *reinterpret_cast<const float4*>(from[j] + 16 * r);
+                    most = fmaxf(fmaxf(most, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
+                }
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+                const int e = down_exponent(most);
+                down[j] = power_of_two(-e), back[j] = power_of_two(e);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRT; ++r)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4 v = *reinterpret_cast<const float4*>(from[j] + 16 * r);
+                split2<kBf16>(v.x, v.y, down[j], vh[r][j], vl[r][j]);
+                split2<kBf16>(v.z, v.w, down[j], vh[r][2 + j], vl[r][2 + j]);
+            }
+    }
+    const T16* b = reinterpret_cast<const T16*>(p.b) + (int64_t)u.adapter * p.N * p.rank;
+    float* out = reinterpret_cast<float*>(smem) + warp * 16 * M::kOutPitch;
+    const int blocks = (p.N + 63) / 64, token0 = u.token + 16 * m, live_tokens = min(16, u.n - 16 * m);
+    if (live_tokens > 0) {
+        for (int block = part * (kWarps / 2) + (warp >> 1); block < blocks; block += parts * (kWarps / 2)) {
+            const int n0 = 64 * block;
+            float d[8][4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[i][j] = 0.0f;
+                uint2 w[kRT];
+                const int n = n0 + 8 * i + g;
+#pragma unroll
+                for (int r = 0; r < kRT; ++r) w[r] = load8_if(b + (int64_t)n * p.rank + 16 * r + 4 * t, n < p.N && 16 * r + 4 * t < p.rank);
+#pragma unroll
+                for (int r = 0; r < kRT; ++r) {
+                    mma_16816<kBf16>(d[i], vl[r], w[r].x, w[r].y);
+                    mma_16816<kBf16>(d[i], vh[r], w[r].x, w[r].y);
+                }
+            }
+            // through shared memory, so that a warp reads base and writes y along the rows
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *reinterpret_cast<float2*>(out + (8 * j + g) * M::kOutPitch + 8 * i + 2 * t) = make_float2(d[i][2 * j] * back[j], d[i][2 * j + 1] * back[j]);
+            __syncwarp();
+            if (p.vec && n0 + 64 <= p.N) {
+                if (p.y_f32) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = 2 * i + (lane >> 4), c = 4 * (lane & 15);
+                        if (row >= live_tokens) continue;
+                        float4 s = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c);
+                        if (p.base) {
+                            const float4 o = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
+                            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
+                        }
+                        *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) = s;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int row = 4 * i + (lane >> 3), c = 8 * (lane & 7);
+                        if (row >= live_tokens) continue;
+                        const float4 s0 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c), s1 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c + 4);
+                        uint4 o = make_uint4(0, 0, 0, 0);  // base may be y, so not by the read-only path
+                        if (p.base) o = *reinterpret_cast<const uint4*>(reinterpret_cast<const T16*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
+                        const float2 o0 = Half<kBf16>::unpack(o.x), o1 = Half<kBf16>::unpack(o.y), o2 = Half<kBf16>::unpack(o.z), o3 = Half<kBf16>::unpack(o.w);
+                        *reinterpret_cast<uint4*>(reinterpret_cast<T16*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) =
+                            make_uint4(Half<kBf16>::pack(s0.x + o0.x, s0.y + o0.y), Half<kBf16>::pack(s0.z + o1.x, s0.w + o1.y),
+                                       Half<kBf16>::pack(s1.x + o2.x, s1.y + o2.y), Half<kBf16>::pack(s1.z + o3.x, s1.w + o3.y));
+                    }
+                }
+            } else {
+#pragma unroll 8
+                for (int i = 0; i < 32; ++i) {
+                    const int row = i >> 1, c = lane + 32 * (i & 1);
+                    if (row < live_tokens && n0 + c < p.N) store_y<kBf16>(p, token0 + row, n0 + c, out[row * M::kOutPitch + c] + load_base<kBf16>(p, token0 + row, n0 + c));
+                }
+            }
+            __syncwarp();
+        }
+    }
+    cluster.barrier_wait();  // no block leaves while its sums are read
+}
+
+template <class Kernel>
+cudaError_t launch(Kernel kernel, const AdapterParams& p, int64_t units, int parts, int smem, cudaStream_t st) {
+    cudaLaunchAttribute attr[2] = {early_launch_attribute(), cluster_attribute(1)};
+    attr[1].val.clusterDim.x = parts, attr[1].val.clusterDim.y = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * parts));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+template <bool kBf16, int kRT>
+cudaError_t launch_rank(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
+    if (few) return launch(adapters_few_kernel<kBf16, kRT>, p, units, parts, 0, st);
+    using M = Many<2 * kRT>;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(adapters_many_kernel<kBf16, 2 * kRT>, M::kSmemBytes, device, done);
+    if (e != cudaSuccess) return e;
+    return launch(adapters_many_kernel<kBf16, 2 * kRT>, p, units, parts, M::kSmemBytes, st);
+}
+template <bool kBf16>
+cudaError_t launch_type(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
+    return p.rank <= 16   ? launch_rank<kBf16, 1>(p, few, units, parts, device, st)
+           : p.rank <= 32 ? launch_rank<kBf16, 2>(p, few, units, parts, device, st)
+           : p.rank <= 64 ? launch_rank<kBf16, 4>(p, few, units, parts, device, st)
+                          : launch_rank<kBf16, 8>(p, few, units, parts, device, st);
+}
+
+}  // namespace
+}  // namespace awe
+
+using namespace awe;
+
+extern "C" awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* L, const void* x_dev, int64_t T, int64_t ldx,
+                                            const int32_t* q_start_dev, const int32_t* adapter_dev, int64_t B, const void* base_dev,
+                                            int64_t ldb, void* y_dev, awe_float_t y_type, int64_t ldy, void* stream) {
+    if (!h || !L || !L->a_dev || !L->b_dev || L->n_adapters <= 0 || L->rank <= 0 || L->N <= 0 || L->K <= 0 || T < 0 || B < 0) return AWE_ERR_INVALID_ARG;
+    if (L->type < AWE_F16 || L->type > AWE_F32 || (int)y_type < AWE_F16 || (int)y_type > AWE_F32) return AWE_ERR_INVALID_ARG;
+    if (!is_half_type(L->type) || ((int)y_type != L->type && y_type != AWE_F32) || L->rank > 128 || L->rank % 8 || L->K % 8) return AWE_ERR_UNSUPPORTED;
+    if (L->N > INT32_MAX - 4096 || L->K > INT32_MAX - 65536 || T > INT32_MAX - 64 || B > AWE_KV_MAX_REQUESTS) return AWE_ERR_UNSUPPORTED;
+    if (T == 0 || B == 0) return AWE_OK;
+    if (!x_dev || !y_dev || !q_start_dev || !adapter_dev || (T > 1 && (ldx < L->K || ldy < L->N || (base_dev && ldb < L->N))) ||
+        (base_dev == y_dev && T > 1 && ldb != ldy))
+        return AWE_ERR_INVALID_ARG;
+    const int out = y_type == AWE_F32 ? 4 : 2;
+    if ((uintptr_t)L->a_dev % 16 || (uintptr_t)L->b_dev % 16 || (uintptr_t)L->scale_dev % 4 || (uintptr_t)x_dev % 16 || (T > 1 && ldx % 8) ||
+        (uintptr_t)base_dev % out || (uintptr_t)y_dev % out || (uintptr_t)q_start_dev % 4 || (uintptr_t)adapter_dev % 4)
+        return AWE_ERR_ALIGNMENT;
+    AdapterParams p = {};
+    p.a = L->a_dev, p.b = L->b_dev, p.x = x_dev, p.base = base_dev, p.y = y_dev, p.scale = L->scale_dev;
+    p.q_start = q_start_dev, p.adapter = adapter_dev, p.ldx = ldx, p.ldb = ldb, p.ldy = ldy, p.n_adapters = L->n_adapters;
+    p.T = (int)T, p.B = (int)B, p.N = (int)L->N, p.K = (int)L->K, p.rank = (int)L->rank, p.y_f32 = y_type == AWE_F32;
+    p.vec = (uintptr_t)base_dev % 16 == 0 && (uintptr_t)y_dev % 16 == 0 && (!base_dev || ldb * out % 16 == 0) && ldy * out % 16 == 0;
+    const bool few = T <= kFew * B;
+    const int64_t units = T / (few ? kFew : kMany) + B;
+    if (units > INT32_MAX / kMostCluster) return AWE_ERR_UNSUPPORTED;
+    // As large a cluster as leaves every SM two blocks, and every warp a step of k.
+    int parts = 1;
+    while (parts < kMostCluster && units * parts * 2 <= 4 * h->sm_count && (L->K + 31) / 32 >= 2 * kWarps * parts) parts *= 2;
+    const cudaError_t e = L->type == AWE_BF16 ? launch_type<true>(p, few, units, parts, h->device, (cudaStream_t)stream)
+                                              : launch_type<false>(p, few, units, parts, h->device, (cudaStream_t)stream);
+    if (e != cudaSuccess) return AWE_ERR_CUDA;
+    h->launches += 1;
+    return AWE_OK;
+}

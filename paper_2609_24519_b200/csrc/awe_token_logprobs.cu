@@ -1,0 +1,358 @@
+// Log probabilities of given tokens, entropy and the most likely tokens of rows of logits (awe_token_logprobs).
+//
+// With M the largest logit of a row and c = scale / ln 2:   t_j = (x_j - M) c,   S0 = sum 2^t_j,   S1 = sum 2^t_j t_j,
+//   z = ln S0:   lse = scale M + z,   log p_j = scale (x_j - M) - z,   entropy = z - ln 2 S1 / S0.
+// M is subtracted first: a product x c could pass FP32 where logits are a type's lowest value.
+// One pass: every thread keeps a maximum of its own and rescales its two sums when it grows.
+//
+// The most likely tokens.  A warp keeps the best so far in order, one a lane, and looks at a batch's elements one by one only if the
+// batch's maximum reaches the least of the best top_k of any warp of the block, which after a few batches is rare.  That bound
+// comes first from the top_k-th largest of the lanes' maxima of the first batch, then from the full lists.  Lists are joined in
+// pairs: of two lists in order, the larger of a[i] and b[31 - i] are the best 32, in an order that five exchanges sort.
+//
+// HBM bounds many rows; a single row is spread over a cluster of blocks that join in shared memory, which bounds it by latency.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "awe_internal.h"
+#include "serve_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace awe {
+namespace {
+
+using namespace serve;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kPieces = 4;  // 16-byte pieces a thread has on their way
+constexpr int kMostCluster = 8;
+constexpr int kNoToken = 0x7FFFFFFF;
+constexpr float kLn2 = 0.693147180559945f;
+
+struct LogprobParams {
+    const void* logits;
+    const int32_t* tokens;
+    float *logprob, *entropy, *lse, *top_logprob;
+    int32_t* top_id;
+    int64_t ld;
+    float scale;
+    int V, top;
+};
+
+// A token and its logit; `before` is the order of the answer: larger first, then the lower token.
+struct Entry {
+    float x;
+    int id;
+};
+__device__ __forceinline__ bool before(const Entry& a, const Entry& b) { return a.x > b.x || (a.x == b.x && a.id < b.id); }
+__device__ __forceinline__ Entry from_lane(const Entry& a, int lane) { return {__shfl_sync(~0u, a.x, lane), __shfl_sync(~0u, a.id, lane)}; }
+// The best 32 of two lists in order, in order; `other_reversed` is the second from its end.
+__device__ __forceinline__ Entry join_lists(Entry mine, const Entry& other_reversed, int lane) {
+    if (before(other_reversed, mine)) mine = other_reversed;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const Entry o = {__shfl_xor_sync(~0u, mine.x, d), __shfl_xor_sync(~0u, mine.id, d)};
+        if (before(o, mine) == !(lane & d)) mine = o;
+    }
+    return mine;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+
+template <int kType>
+struct Piece {  // 16 bytes of logits
+    static constexpr int kCount = kType == AWE_F32 ? 4 : 8;
+    using T = typename std::conditional<kType == AWE_F32, float, uint16_t>::type;
+    static __device__ __forceinline__ float one(const T* x) {
+        if constexpr (kType == AWE_F32) return *x;
+        else return Half<kType == AWE_BF16>::unpack(*x).x;
+    }
+    static __device__ __forceinline__ float at(const uint4& w, int i) {
+        if constexpr (kType == AWE_F32) return __uint_as_float((&w.x)[i]);
+        else {
+            const float2 f = Half<kType == AWE_BF16>::unpack((&w.x)[i >> 1]);
+            return i & 1 ? f.y : f.x;
+        }
+    }
+    // The largest; NaN if one is.
+    static __device__ __forceinline__ float largest(const uint4& w) {
+        if constexpr (kType == AWE_F32)
+            return max_nan(max_nan(__uint_as_float(w.x), __uint_as_float(w.y)), max_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
+        else if constexpr (kType == AWE_BF16) {
+            auto b = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
+            const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(b(w.x), b(w.y)), __hmax2_nan(b(w.z), b(w.w)));
+            return __bfloat162float(__hmax_nan(m.x, m.y));
+        } else {
+            auto b = [](uint32_t x) { return *reinterpret_cast<const __half2*>(&x); };
+            const __half2 m = __hmax2_nan(__hmax2_nan(b(w.x), b(w.y)), __hmax2_nan(b(w.z), b(w.w)));
+            return __half2float(__hmax_nan(m.x, m.y));
+        }
+    }
+};
+
+struct Sums {
+    float m, s0, s1;  // maximum (NaN once a NaN was seen), S0 and S1 against it
+};
+// Brings sums to a larger maximum: t becomes t - g.
+__device__ __forceinline__ void raise(Sums& s, float m, float c) {
+    if (s.s0 != 0.0f) {
+        const float g = (m - s.m) * c, a = exp2_approx(-g);
+        s.s1 = a == 0.0f ? 0.0f : fmaf(-g, s.s0, s.s1) * a;
+        s.s0 *= a;
+    }
+    s.m = m;
+}
+__device__ __forceinline__ Sums join_sums(Sums a, Sums b, float c) {
+    const float m = max_nan(a.m, b.m);
+    raise(a, m, c);
+    raise(b, m, c);
+    return {m, a.s0 + b.s0, a.s1 + b.s1};
+}
+
+struct Shared {
+    Sums sums[kWarps];
+    Entry list[kWarps][32];
+    Sums block_sums;
+    Entry block_list[32];
+    int bound;  // least of a full list's best top_k, as an ordered whole number
+};
+__device__ __forceinline__ int ordered(float x) {
+    const int b = __float_as_int(x);
+    return b < 0 ? b ^ 0x7FFFFFFF : b;
+}
+__device__ __forceinline__ float from_ordered(int b) { return __int_as_float(b < 0 ? b ^ 0x7FFFFFFF : b); }
+
+// grid: a cluster for each row.
+template <int kType, bool kTop>
+__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobParams p) {
+    using P = Piece<kType>;
+    using T = typename P::T;
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / parts;
+    const float c = p.scale * 1.44269504088896f;
+    if (kTop && tid == 0) sh.bound = ordered(-INFINITY);
+    __syncthreads();
+    grid_wait();
+    const T* x = reinterpret_cast<const T*>(p.logits) + row * p.ld;
+    // whole 16-byte pieces lie between `head` and `tail` elements at the ends of the row
+    const int head = min(p.V, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T)), pieces = (p.V - head) / P::kCount;
+    const int tail_at = head + pieces * P::kCount;
+    const int begin = (int)((int64_t)pieces * rank / parts), end = (int)((int64_t)pieces * (rank + 1) / parts);
+    const uint4* from = reinterpret_cast<const uint4*>(x + head);
+
+    // the given token's logit is on its way meanwhile
+    int token = -1;
+    float given = 0.0f;
+    if (p.logprob && rank == 0 && tid == 0) {
+        token = p.tokens[row];
+        if (token >= 0 && token < p.V) given = P::one(x + token);
+    }
+
+    Sums own = {-INFINITY, 0.0f, 0.0f};
+    Entry best = {-INFINITY, kNoToken};  // this lane's of the warp's list
+    float bound = -INFINITY;
+    // Elements first + i, i < count, of this thread's piece w.
+    auto look = [&](const uint4& w, int first, int count, float most) {
+        const unsigned any = __ballot_sync(~0u, most >= bound);
+        if (!any) return;
+#pragma unroll
+        for (int i = 0; i < P::kCount; ++i) {
+            const Entry mine = {P::at(w, i), first + i};
+            const Entry least = from_lane(best, p.top - 1);
+            unsigned ask = __ballot_sync(~0u, i < count && mine.x >= bound && before(mine, least));
+            for (; ask; ask &= ask - 1) {
+                const Entry e = from_lane(mine, __ffs(ask) - 1);
+                const bool stays = before(best, e);
+                const Entry above = {__shfl_up_sync(~0u, best.x, 1), __shfl_up_sync(~0u, best.id, 1)};
+                const unsigned keep = __ballot_sync(~0u, stays);  // lanes 0 .. n - 1
+                if (!stays) best = lane == __popc(keep) ? e : above;
+            }
+        }
+    };
+    auto raise_bound = [&] {  // to the least of this warp's best, if there are as many
+        const Entry least = from_lane(best, p.top - 1);
+        if (lane == 0 && least.id != kNoToken) atomicMax(&sh.bound, ordered(least.x));
+        bound = fmaxf(bound, from_ordered(*(volatile int*)&sh.bound));
+    };
+    auto add = [&](const uint4& w, int count) {
+        const float m = own.m == -INFINITY ? 0.0f : own.m;
+#pragma unroll
+        for (int i = 0; i < P::kCount; ++i) {
+            if (i >= count) continue;
+            const float t = fmaxf((P::at(w, i) - m) * c, -200.0f);  // of a masked token: its exponential is 0
+            const float e = exp2_approx(t);
+            own.s0 += e;
+            own.s1 = fmaf(e, t, own.s1);
+        }
+    };
+    // the ends of the row, an element a thread, by the first warp of the first block and of the last
+    auto end_of_row = [&](int first, int count) {
+        const bool live = lane < count;
+        const float one = live ? P::one(x + first + lane) : -INFINITY;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if constexpr (kType == AWE_F32) w.x = __float_as_uint(one);
+        else w.x = Half<kType == AWE_BF16>::pack(one, 0.0f);
+        const float m = max_nan(own.m, one);
+        if (m != own.m) raise(own, m, c);
+        add(w, live);
+        if constexpr (kTop) look(w, first + lane, live, live ? one : -INFINITY);
+    };
+
+    uint4 w[kPieces] = {};
+    bool is_first = true;
+    for (int i0 = begin + warp * 32; i0 < end; i0 += kThreads * kPieces) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u) {
+            const int i = i0 + lane + u * kThreads;
+            if (i < end) w[u] = __ldcs(from + i);
+        }
+        float of_piece[kPieces];
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u) {
+            of_piece[u] = i0 + lane + u * kThreads < end ? P::largest(w[u]) : -INFINITY;
+            most = max_nan(most, of_piece[u]);
+        }
+        if (!(most <= own.m)) raise(own, max_nan(own.m, most), c);
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u)
+            if (i0 + lane + u * kThreads < end) add(w[u], P::kCount);
+        if constexpr (kTop) {
+            if (is_first) {
+                // as many lanes as top_k have a maximum that is not below the top_k-th largest of them
+                float m = most == most ? most : -INFINITY;
+#pragma unroll
+                for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+                    for (int d = k >> 1; d > 0; d >>= 1) {
+                        const float o = __shfl_xor_sync(~0u, m, d);
+                        m = ((lane & d) == 0) == ((lane & k) == 0) ? fmaxf(m, o) : fminf(m, o);
+                    }
+                bound = fmaxf(bound, __shfl_sync(~0u, m, p.top - 1));
+                is_first = false;
+            }
+            if (__any_sync(~0u, !(most < bound))) {
+#pragma unroll
+                for (int u = 0; u < kPieces; ++u) {
+                    const int i = i0 + lane + u * kThreads;
+                    // a NaN hides what else its piece has, so such a piece is looked at
+                    look(w[u], head + i * P::kCount, i < end ? P::kCount : 0, of_piece[u] == of_piece[u] ? of_piece[u] : INFINITY);
+                }
+                raise_bound();
+            }
+        }
+    }
+    if (rank == 0 && warp == 0 && head > 0) end_of_row(0, head);
+    if (rank == parts - 1 && warp == kWarps - 1 && tail_at < p.V) end_of_row(tail_at, p.V - tail_at);
+
+    // ---- the warp, the block, the cluster
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const Sums o = {__shfl_xor_sync(~0u, own.m, d), __shfl_xor_sync(~0u, own.s0, d), __shfl_xor_sync(~0u, own.s1, d)};
+        own = lane & d ? join_sums(o, own, c) : join_sums(own, o, c);  // the same order on both sides
+    }
+    if (lane == 0) sh.sums[warp] = own;
+    if constexpr (kTop) sh.list[warp][lane] = best;
+    __syncthreads();
+    auto join_all = [&](int n, auto list_of) {  // lists list_of(0 .. n - 1), n a power of two: into the first
+        for (int step = 1; step < n; step <<= 1) {
+            if (warp % (2 * step) == 0 && warp + step < n) {
+                best = join_lists(best, list_of(warp + step)[31 - lane], lane);
+                list_of(warp)[lane] = best;
+            }
+            __syncthreads();
+        }
+    };
+    if constexpr (kTop) join_all(kWarps, [&](int i) { return sh.list[i]; });
+    if (tid == 0) {
+        for (int i = 1; i < kWarps; ++i) own = join_sums(own, sh.sums[i], c);
+        sh.block_sums = own;
+    }
+    if (parts > 1) {
+        if (kTop && warp == 0) sh.block_list[lane] = best;
+        cluster.sync();
+        if (rank == 0) {
+            if (tid == 0)
+                for (int i = 1; i < parts; ++i) own = join_sums(own, *cluster.map_shared_rank(&sh.block_sums, i), c);
+            if constexpr (kTop) {
+                if (warp < parts) best = cluster.map_shared_rank(&sh, warp)->block_list[lane];
+                sh.list[warp][lane] = best;
+                __syncthreads();
+                join_all(parts, [&](int i) { return sh.list[i]; });
+            }
+        }
+        cluster.sync();  // no block leaves while it is read
+    }
+    if (rank != 0 || warp != 0) return;
+    const float m = __shfl_sync(~0u, own.m, 0), s0 = __shfl_sync(~0u, own.s0, 0), s1 = __shfl_sync(~0u, own.s1, 0);
+    const bool none = m == -INFINITY, bad = !(m < INFINITY);  // nothing but masked tokens; a NaN or an infinity
+    const float z = logf(s0);
+    auto log_p = [&](float logit) {
+        if (bad) return __int_as_float(0x7FFFFFFF);
+        return none ? -INFINITY : fmaf(p.scale, logit - m, -z);
+    };
+    if (lane == 0) {
+        const float nan = __int_as_float(0x7FFFFFFF);
+        if (p.entropy) p.entropy[row] = bad ? nan : (none ? 0.0f : z - kLn2 * (s1 / s0));
+        if (p.lse) p.lse[row] = bad ? nan : (none ? -INFINITY : fmaf(p.scale, m, z));
+        if (p.logprob) p.logprob[row] = token >= 0 && token < p.V ? log_p(given) : 0.0f;
+    }
+    if (kTop && lane < p.top) {
+        const bool found = best.id != kNoToken;
+        if (p.top_id) p.top_id[row * p.top + lane] = found ? best.id : -1;
+        if (p.top_logprob) p.top_logprob[row * p.top + lane] = log_p(best.x);
+    }
+}
+
+template <int kType>
+cudaError_t launch(const LogprobParams& p, int64_t T, int parts, cudaStream_t st) {
+    cudaLaunchAttribute attr[2] = {early_launch_attribute(), cluster_attribute(1)};
+    attr[1].val.clusterDim.x = parts, attr[1].val.clusterDim.y = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(T * parts));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return p.top ? cudaLaunchKernelEx(&cfg, token_logprobs_kernel<kType, true>, p) : cudaLaunchKernelEx(&cfg, token_logprobs_kernel<kType, false>, p);
+}
+
+}  // namespace
+}  // namespace awe
+
+using namespace awe;
+
+extern "C" awe_status_t awe_token_logprobs(awe_handle_t h, const void* logits_dev, awe_float_t type, int64_t T, int64_t V, int64_t ld,
+                                           float scale, const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev,
+                                           float* lse_dev, int64_t top_k, float* top_logprob_dev, int32_t* top_id_dev, void* stream) {
+    if (!h || T < 0 || V <= 0 || top_k < 0 || !(scale > 0.0f && scale <= 1e30f)) return AWE_ERR_INVALID_ARG;
+    if ((int)type < AWE_F16 || (int)type > AWE_F32) return AWE_ERR_INVALID_ARG;
+    if (top_k > AWE_MAX_TOP || V > INT32_MAX / 2) return AWE_ERR_UNSUPPORTED;
+    if (T == 0) return AWE_OK;
+    if (!logits_dev || (T > 1 && ld < V) || top_k > V || (logprob_dev && !tokens_dev)) return AWE_ERR_INVALID_ARG;
+    if (T > INT32_MAX / kMostCluster) return AWE_ERR_UNSUPPORTED;
+    if ((uintptr_t)logits_dev % (type == AWE_F32 ? 4 : 2) || (uintptr_t)tokens_dev % 4 || (uintptr_t)logprob_dev % 4 || (uintptr_t)entropy_dev % 4 ||
+        (uintptr_t)lse_dev % 4 || (uintptr_t)top_logprob_dev % 4 || (uintptr_t)top_id_dev % 4)
+        return AWE_ERR_ALIGNMENT;
+    if (!top_logprob_dev && !top_id_dev) top_k = 0;
+    if (!logprob_dev && !entropy_dev && !lse_dev && !top_k) return AWE_OK;
+    LogprobParams p = {logits_dev, tokens_dev, logprob_dev, entropy_dev, lse_dev, top_logprob_dev, top_id_dev, ld, scale, (int)V, (int)top_k};
+    // A row goes to a cluster while the rows alone leave SMs without work and a block would still have a batch for every thread.
+    const int64_t batch = (int64_t)kThreads * kPieces * (type == AWE_F32 ? 4 : 8);
+    int parts = 1;
+    while (parts < kMostCluster && T * parts * 2 <= 4 * h->sm_count && V >= batch * parts) parts *= 2;
+    cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t e = type == AWE_F32 ? launch<AWE_F32>(p, T, parts, st) : type == AWE_BF16 ? launch<AWE_BF16>(p, T, parts, st) : launch<AWE_F16>(p, T, parts, st);
+    if (e != cudaSuccess) return AWE_ERR_CUDA;
+    h->launches += 1;
+    return AWE_OK;
+}
