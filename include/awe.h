@@ -478,6 +478,16 @@ awe_status_t awe_kv4_append(awe_handle_t h, const awe_kv4_cache* cache, const aw
 awe_status_t awe_kv4_read(awe_handle_t h, const awe_kv4_cache* cache, int64_t T, const int64_t* slots_dev, awe_float_t type, void* k_out_dev,
                           int64_t ldk, void* v_out_dev, int64_t ldv, void* stream);
 
+/* Scratch awe_kv4_attention needs for at most T queries of B requests. */
+size_t awe_kv4_attention_workspace_bytes(awe_handle_t h, const awe_kv4_cache* cache, int64_t T, int64_t n_q_heads, int64_t B);
+
+/* awe_kv_attention over the cache of 4 bits, with the same arguments, and the same answers for rows that see nothing. */
+awe_status_t awe_kv4_attention(awe_handle_t h, const awe_kv4_cache* cache, const void* q_dev, awe_float_t type, int64_t T,
+                               int64_t n_q_heads, int64_t ldq, const int32_t* q_start_dev, const int32_t* ctx_len_dev, int64_t B,
+                               const int32_t* block_table_dev, int64_t max_pages, int64_t ld_table, float scale, int causal,
+                               int64_t window, void* out_dev, int64_t ldo, float* lse_dev, void* workspace_dev,
+                               size_t workspace_bytes, void* stream);
+
 /* Low-rank adapters of one projection: adapter i adds scale[i] * B_i (A_i x). */
 typedef struct {
     const void* a_dev;       /* n_adapters x rank x K, of `type` (AWE_F16, AWE_BF16), 16-B aligned       */

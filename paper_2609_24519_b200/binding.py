@@ -41,7 +41,7 @@ EXPORTS = ["awe_create", "awe_destroy", "awe_encoding_info", "awe_encoding_lut",
            "awe_gemm_exact_host", "awe_gemm_exact_static", "awe_wide_moduli", "awe_wide_select", "awe_wide_workspace_bytes",
            "awe_wide_residues", "awe_wide_crt", "awe_gemm_exact_wide", "awe_reconstruct", "awe_fp4_product_raw", "awe_fp8_product_raw", "awe_last_device_status", "awe_selftest_bounded_wait", "awe_last_gemm_clock_mhz", "awe_launch_count",
            "awe_status_string", "awe_linear_w4", "awe_kv_plan", "awe_kv_write", "awe_kv_attention_workspace_bytes", "awe_kv_attention",
-           "awe_kv4_append", "awe_kv4_read", "awe_linear_adapters",
+           "awe_kv4_append", "awe_kv4_read", "awe_kv4_attention_workspace_bytes", "awe_kv4_attention", "awe_linear_adapters",
            "awe_token_logprobs"]
 
 
@@ -144,6 +144,10 @@ def lib() -> ctypes.CDLL:
     kv4 = ctypes.POINTER(Kv4Cache)
     L.awe_kv4_append.argtypes = [vp, kv4, ctypes.POINTER(Rotary), i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
     L.awe_kv4_read.argtypes = [vp, kv4, i64, vp, i32, vp, i64, vp, i64, vp]
+    L.awe_kv4_attention_workspace_bytes.argtypes = [vp, kv4, i64, i64, i64]
+    L.awe_kv4_attention_workspace_bytes.restype = sz
+    L.awe_kv4_attention.argtypes = [vp, kv4, vp, i32, i64, i64, i64, vp, vp, i64, vp, i64, i64, f32, i32, i64, vp, i64, vp, vp,
+                                    sz, vp]
     L.awe_linear_adapters.argtypes = [vp, ctypes.POINTER(Adapters), vp, i64, i64, vp, vp, i64, vp, i64, vp, i32, i64, vp]
     L.awe_token_logprobs.argtypes = [vp, vp, i32, i64, i64, i64, f32, vp, vp, vp, vp, i64, vp, vp, vp]
     L.awe_last_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
@@ -422,6 +426,22 @@ def awe_kv4_read(h: Handle, cache: Kv4Cache, T: int, slots, dtype: int, k_out, l
     status = _lib.awe_kv4_read(h._h, cache, T, _ptr(slots), dtype, _ptr(k_out), ldk, _ptr(v_out), ldv, _stream(stream))
     if status:
         raise AweError(status, "awe_kv4_read")
+
+
+def awe_kv4_attention_workspace_bytes(h: Handle, cache: Kv4Cache, T: int, n_q_heads: int, B: int) -> int:
+    return int(lib().awe_kv4_attention_workspace_bytes(h._h, cache, T, n_q_heads, B))
+
+
+def awe_kv4_attention(h: Handle, cache: Kv4Cache, q, dtype: int, T: int, n_q_heads: int, ldq: int, q_start, ctx_len, B: int,
+                      block_table, max_pages: int, ld_table: int, scale: float, causal: bool, window: int, out, ldo: int,
+                      lse, workspace, workspace_bytes: Optional[int] = None, stream=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    status = _lib.awe_kv4_attention(h._h, cache, _ptr(q), dtype, T, n_q_heads, ldq, _ptr(q_start), _ptr(ctx_len), B,
+                                   _ptr(block_table), max_pages, ld_table, scale, causal, window, _ptr(out), ldo, _ptr(lse),
+                                   _ptr(workspace), workspace_bytes, _stream(stream))
+    if status:
+        raise AweError(status, "awe_kv4_attention")
 
 
 def awe_linear_adapters(h: Handle, L: Adapters, x, T: int, ldx: int, q_start, adapter, B: int, base, ldb: int, y, y_type: int, ldy: int,

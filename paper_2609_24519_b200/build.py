@@ -10,7 +10,7 @@ INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 LIB = os.path.join(PKG, "libawe_b200.so")
 SOURCES = ["awe_tables.cu", "awe_encode.cu", "awe_gemm.cu", "awe_gemm_wide.cu", "awe_api.cu", "awe_static.cu", "awe_wide.cu", "awe_reconstruct.cu",
            "awe_linear_w4.cu", "awe_linear_w4_tc.cu", "awe_kv_plan.cu", "awe_kv_write.cu", "awe_kv_attention.cu", "awe_kv_attention_tc.cu",
-           "awe_kv4_append.cu", "awe_linear_adapters.cu", "awe_token_logprobs.cu"]
+           "awe_kv4_append.cu", "awe_linear_adapters.cu", "awe_token_logprobs.cu", "awe_kv4_attention.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "--threads", "0"]
 

@@ -1,0 +1,411 @@
+// Attention over the paged 4-bit cache (awe_kv4_attention), for few query rows; prompts go to awe_kv_attention_tc.cu.
+//
+//   s_j = scale * ks_j (q . K_j),   out = sum_j e^(s_j - m) vs_j V_j / sum_j e^(s_j - m)
+//
+// with the integers K_j, V_j = code - zero (exact in FP16) and the scales ks_j, vs_j of every token.  How work is dealt out to blocks and
+// warps, and that the instruction's rows are tokens (then dimensions) and its columns query rows, is as for the 8-bit cache
+// (awe_kv_attention.cu).  Different here:
+//
+//   - The value's scale goes into the weight as an addition to its exponent, w_j = 2^(s_j / ln 2 + log2 vs_j - m), with m 10 to 15 below the
+//     largest such exponent so far, so that w_j rounds to FP16 as well as it can for what it contributes, and the products of all tokens
+//     add up in one accumulator.  The divisor is the sum of w_j 2^-log2 vs_j: of the rounded weights where they keep their 11 bits, so that the
+//     rounding cancels where one token dominates, else of the others.
+//   - Codes become FP16 by inserting them into the mantissa of 1024 (or, four bits up, 16 of it) and subtracting 1024 and the zero point.  A 32-bit
+//     word's eight codes come apart in pairs (0, 4), (1, 5), (2, 6), (3, 7), so queries are laid out in that order once; of two tokens' values
+//     the 16-bit halves of their words are put together first, which pairs tokens.
+//
+// HBM bounds long contexts: a token and head of dimension 128 is 132 bytes of keys and values.
+#include <algorithm>
+#include <type_traits>
+
+#include "kv4.cuh"
+#include "kv_attention_few.cuh"
+
+namespace awe {
+namespace {
+
+using namespace serve;
+using namespace attn_few;
+
+template <int kD, int kNT>
+struct Config {
+    static constexpr int kRows = 8 * kNT;
+    static constexpr int kStages = kD == 64 ? 8 : kD == 128 ? 6 : 4;
+    static constexpr int kRowBytes = kD / 2, kTileBytes = 16 * kRowBytes;
+    static constexpr int kParamAt = 2 * kTileBytes, kPageAt = kParamAt + 64;  // behind keys and values: 16 words of each, the page
+    static constexpr int kStageBytes = kPageAt + 16;
+    static constexpr int kVecPitch = kD + 4;  // floats
+    static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
+    static constexpr int kJoinBytes = kWarps * kRows * (kVecPitch + 4) * 4;
+    static constexpr int kSmemBytes = kRingBytes > kJoinBytes ? kRingBytes : kJoinBytes;  // one after the other
+};
+
+// Byte offset of the 16-byte piece c of token row r inside a tile of 16 tokens: pieces are exchanged within 128-byte lines so that the threads
+// of one phase of a load (rows g of keys, rows 2 t and the like of values) hit all banks.
+template <int kRowBytes>
+__device__ __forceinline__ uint32_t piece_at(int r, int c) {
+    if constexpr (kRowBytes == 32) return (r >> 2) * 128 + (((((r & 3) << 1) + c) ^ (((r >> 2) & 1) << 1)) << 4);
+    else if constexpr (kRowBytes == 64) return (r >> 1) * 128 + (((((r & 1) << 2) + c) ^ (((r >> 1) & 3) << 1)) << 4);
+    else return r * 128 + ((c ^ (r & 7)) << 4);
+}
+
+// 16 times the scales of two parameter words, within the format's bounds.
+__device__ __forceinline__ float2 scales16(uint32_t words) {
+    const __half2 s = __hmin2(__hmax2(__halves2half2(__ushort_as_half(words & 0xFFF0u), __ushort_as_half((words >> 16) & 0xFFF0u)),
+                                      __float2half2_rn(16.0f * kKv4LeastScale)), __float2half2_rn(16.0f * kKv4MostScale));
+    return __half22float2(s);
+}
+__device__ __forceinline__ float log2_approx(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
+    return v;
+}
+
+template <int kD, int kNT, bool kBf16>
+__global__ void __launch_bounds__(kThreads) kv4_attention_kernel(const AttnParams p) {
+    using C = Config<kD, kNT>;
+    using T16 = typename Half<kBf16>::type;
+    constexpr int kRows = C::kRows, kSteps16 = kD / 16, kWords = kD / 32;  // kWords: of keys, a thread and token
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ Search search;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+
+    grid_wait();
+    Mine mine;
+    if (!find_steps<kRows>(p, search, mine)) return;
+    int b = mine.b;
+    int64_t at = mine.at;
+    Request r = request_of<kRows>(p, b);
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * C::kStages * C::kStageBytes;
+    float* join_vec = reinterpret_cast<float*>(smem);  // in the ring's place once it is empty
+    float4* join_stat = reinterpret_cast<float4*>(join_vec + kWarps * kRows * C::kVecPitch);
+
+    for (int64_t pos = mine.begin; pos < mine.end;) {
+        while (pos >= at + (p.whole ? r.units : (int64_t)r.units * r.steps)) {
+            at += p.whole ? r.units : (int64_t)r.units * r.steps;
+            r = request_of<kRows>(p, ++b);
+        }
+        const int unit = p.whole ? (int)(pos - at) : (int)((pos - at) / r.steps), step0 = p.whole ? 0 : (int)((pos - at) % r.steps);
+        const int step1 = p.whole ? r.steps : (int)min((int64_t)r.steps, step0 + mine.end - pos);
+        const int head = unit % p.heads, row0 = unit / p.heads * kRows, n_rows = min(kRows, r.n * p.group - row0);
+        const int32_t* table = p.table + (int64_t)b * p.ld_table;
+        pos += p.whole ? 1 : step1 - step0;
+
+        // ---- the query rows, as the matrix instruction's 16 x 8 operand: thread (g, t) holds of row g the dimensions t kD / 4 and
+        // following, eight at a time in the order of the codes' pairs
+        uint32_t qf[kNT][kSteps16][2];
+        float cq[kNT][2];                    // factor of the scores of columns 2t, 2t + 1, a sixteenth of it: scales come 16 times
+        int see_lo[kNT][2], see_hi[kNT][2];  // tokens [see_lo, see_hi) are visible
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+            const int row = row0 + 8 * nt + g;
+            const bool live = 8 * nt + g < n_rows;
+            const int query = live ? row / p.group : 0, qh = head * p.group + (live ? row % p.group : 0);
+            const T16* src = reinterpret_cast<const T16*>(p.q) + (int64_t)(r.q0 + query) * p.ldq + (int64_t)qh * kD + t * (kD / 4);
+            float factor = p.scale_log2 * 0.0625f;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (live) x = reinterpret_cast<const uint4*>(src)[w];
+                qf[nt][2 * w][0] = __byte_perm(x.x, x.z, 0x5410), qf[nt][2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
+                qf[nt][2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410), qf[nt][2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+            }
+            query_to_fp16<kBf16>(qf[nt], factor);
+            int lo_tok, hi_tok;
+            visible(p, r, b, query, live, lo_tok, hi_tok);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {  // from the thread that loaded row 2t + j
+                cq[nt][j] = __shfl_sync(~0u, factor, (2 * t + j) * 4);
+                see_lo[nt][j] = __shfl_sync(~0u, lo_tok, (2 * t + j) * 4);
+                see_hi[nt][j] = __shfl_sync(~0u, hi_tok, (2 * t + j) * 4);
+            }
+        }
+        const Sees sees = sees_of<kNT>(see_lo, see_hi, n_rows, t);
+
+        float o[kSteps16][kNT][4];
+        float m_ref[kNT][2], sum[kNT][2], sum_lse[kNT][2];
+#pragma unroll
+        for (int i = 0; i < kSteps16; ++i)
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[i][nt][j] = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+            m_ref[nt][0] = m_ref[nt][1] = -INFINITY;
+            sum[nt][0] = sum[nt][1] = sum_lse[nt][0] = sum_lse[nt][1] = 0.0f;
+        }
+
+        // ---- ring of this warp's 16-token tiles
+        const int n_tiles = step1 - step0;
+        const int tok0 = r.lo + step0 * kStepTokens + warp * 16;
+        auto page_of = [&](int i) {  // page of tile i, -1 where it has none
+            const int tok = tok0 + i * kStepTokens;
+            if (i >= n_tiles || tok >= sees.any_hi || tok + 16 <= sees.any_lo) return -1;
+            const int page = table[tok >> p.page_log2];
+            return (unsigned)page < (unsigned)p.n_pages ? page : -1;
+        };
+        // tiles of 16 tokens lie one behind the other in the pools, a page and head's together
+        const int tile_log2 = p.page_log2 - 4, tile_mask = (1 << tile_log2) - 1;
+        const int8_t *k_from = p.k + 16 * lane, *v_from = p.v + 16 * lane;
+        const uint8_t* param_from = reinterpret_cast<const uint8_t*>(lane < 2 ? p.k_param : p.v_param) + 16 * (lane & 1);
+        uint32_t write_at = ring;
+        auto fetch = [&](int i, int page) {
+            if (page >= 0) {
+                const uint64_t tile = ((uint64_t)((uint32_t)page * (uint64_t)p.heads + head) << tile_log2) + (((tok0 + i * kStepTokens) >> 4) & tile_mask);
+                const int8_t *k_at = k_from + tile * C::kTileBytes, *v_at = v_from + tile * C::kTileBytes;
+#pragma unroll
+                for (int j = 0; j < C::kTileBytes / 512; ++j) {
+                    const int c = lane + 32 * j;
+                    const uint32_t dst = write_at + piece_at<C::kRowBytes>(c / (C::kRowBytes / 16), c % (C::kRowBytes / 16));
+                    cp_async16_whole(dst, k_at + 512 * j);
+                    cp_async16_whole(dst + C::kTileBytes, v_at + 512 * j);
+                }
+                if (lane < 4) cp_async16_whole(write_at + C::kParamAt + 16 * lane, param_from + tile * 32);
+            }
+            if (lane == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(write_at + C::kPageAt), "r"(page) : "memory");
+            cp_async_commit();
+            write_at = write_at + C::kStageBytes == ring + C::kStages * C::kStageBytes ? ring : write_at + C::kStageBytes;
+        };
+#pragma unroll 1
+        for (int i = 0; i < C::kStages - 1; ++i) fetch(i, page_of(i));
+        int next_page = page_of(C::kStages - 1);
+
+        uint32_t read_at = ring;
+        for (int i = 0; i < n_tiles; ++i) {
+            cp_async_wait<C::kStages - 2>();
+            __syncwarp();
+            fetch(i + C::kStages - 1, next_page);
+            next_page = page_of(i + C::kStages);
+            const uint32_t ks_at = read_at, vs_at = ks_at + C::kTileBytes, params_at = ks_at + C::kParamAt;
+            read_at = read_at + C::kStageBytes == ring + C::kStages * C::kStageBytes ? ring : read_at + C::kStageBytes;
+            if ((int)lds32(ks_at + C::kPageAt) < 0) continue;
+
+            // what the tile holds, all of it on its way before the first product waits for any: keys of the tokens g, g + 8,
+            // values of the thread's kD / 8 dimensions of the tokens 2t, 2t + 1, 2t + 8, 2t + 9
+            constexpr int kValueWords = kD / 64;
+            uint32_t k[2][kWords], v[4][kValueWords];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if constexpr (kD == 64) {
+                    const uint2 x = lds64(ks_at + piece_at<32>(g + 8 * j, t >> 1) + 8 * (t & 1));
+                    k[j][0] = x.x, k[j][1] = x.y;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kD / 128; ++c) {
+                        const uint4 x = lds128(ks_at + piece_at<C::kRowBytes>(g + 8 * j, t * (kD / 128) + c));
+                        k[j][4 * c] = x.x, k[j][4 * c + 1] = x.y, k[j][4 * c + 2] = x.z, k[j][4 * c + 3] = x.w;
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 2 * t + (j & 1) + 8 * (j >> 1);
+                if constexpr (kD == 64) v[j][0] = lds32(vs_at + piece_at<32>(row, g >> 2) + 4 * (g & 3));
+                else if constexpr (kD == 128) {
+                    const uint2 x = lds64(vs_at + piece_at<64>(row, g >> 1) + 8 * (g & 1));
+                    v[j][0] = x.x, v[j][1] = x.y;
+                } else {
+                    const uint4 x = lds128(vs_at + piece_at<128>(row, g));
+                    v[j][0] = x.x, v[j][1] = x.y, v[j][2] = x.z, v[j][3] = x.w;
+                }
+            }
+            const uint32_t k_words = lds16(params_at + 2 * g) | lds16(params_at + 2 * g + 16) << 16;
+            const uint32_t v_words = lds16(params_at + 32 + 2 * g) | lds16(params_at + 32 + 2 * g + 16) << 16;
+            const Kv4Zeros vz[2] = {lds32(params_at + 32 + 4 * t), lds32(params_at + 32 + 4 * t + 16)};
+
+            // scores of 16 tokens (rows g, g + 8) and the query rows (columns 2t, 2t + 1), in two sums that do not wait for each other
+            float s[kNT][4], s_odd[kNT][4];
+            const Kv4Zeros kz[2] = {__byte_perm(k_words, 0, 0x1010), __byte_perm(k_words, 0, 0x3232)};
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t x = k[0][w] >> (8 * h), y = k[1][w] >> (8 * h);
+                    const uint32_t f[4] = {kv4_low_codes(x, kz[0]), kv4_low_codes(y, kz[1]), kv4_high_codes(x, kz[0]), kv4_high_codes(y, kz[1])};
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        float(&to)[4] = h ? s_odd[nt] : s[nt];
+                        if (w == 0) mma_16816_zero<false>(to, f, qf[nt][h][0], qf[nt][h][1]);
+                        else mma_16816<false>(to, f, qf[nt][2 * w + h][0], qf[nt][2 * w + h][1]);
+                    }
+                }
+            }
+            const float2 ks = scales16(k_words), vs = scales16(v_words);
+            const float lv[2] = {log2_approx(vs.x) - 4.0f, log2_approx(vs.y) - 4.0f}, back[2] = {exp2_approx(-lv[0]), exp2_approx(-lv[1])};
+            const int tile = tok0 + i * kStepTokens, tok = tile + g;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+                s[nt][0] = fmaf(s[nt][0] + s_odd[nt][0], ks.x * cq[nt][0], lv[0]), s[nt][1] = fmaf(s[nt][1] + s_odd[nt][1], ks.x * cq[nt][1], lv[0]);
+                s[nt][2] = fmaf(s[nt][2] + s_odd[nt][2], ks.y * cq[nt][0], lv[1]), s[nt][3] = fmaf(s[nt][3] + s_odd[nt][3], ks.y * cq[nt][1], lv[1]);
+            }
+            if (tile < sees.all_lo || tile + 16 > sees.all_hi) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at_tok = tok + (j >> 1) * 8;
+                        if (at_tok < see_lo[nt][j & 1] || at_tok >= see_hi[nt][j & 1]) s[nt][j] = -INFINITY;
+                    }
+            }
+            bool grows = false;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+                grows |= fmaxf(s[nt][0], s[nt][2]) > m_ref[nt][0] + kMostAbove || fmaxf(s[nt][1], s[nt][3]) > m_ref[nt][1] + kMostAbove;
+            if (__any_sync(~0u, grows)) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float m = fmaxf(s[nt][j], s[nt][j + 2]);
+                        m = fmaxf(m, __shfl_xor_sync(~0u, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(~0u, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(~0u, m, 16));
+                        m = fmaxf(m - kBelow, m_ref[nt][j]);
+                        const float a = m == m_ref[nt][j] ? 1.0f : exp2_approx(m_ref[nt][j] - m);
+                        m_ref[nt][j] = m;
+                        sum[nt][j] *= a;
+                        sum_lse[nt][j] *= a;
+#pragma unroll
+                        for (int c = 0; c < kSteps16; ++c) o[c][nt][j] *= a, o[c][nt][j + 2] *= a;
+                    }
+            }
+            uint32_t pf[kNT][2];
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float m0 = m_ref[nt][0] == -INFINITY ? 0.0f : m_ref[nt][0], m1 = m_ref[nt][1] == -INFINITY ? 0.0f : m_ref[nt][1];
+                    const float w0 = exp2_approx(s[nt][2 * half] - m0), w1 = exp2_approx(s[nt][2 * half + 1] - m1);
+                    const uint32_t w = Half<false>::pack(w0, w1);
+                    const float2 f = Half<false>::unpack(w);
+                    constexpr float kNormal = 6.103515625e-5f;  // 2^-14
+                    sum_lse[nt][0] = fmaf(w0, back[half], sum_lse[nt][0]);
+                    sum_lse[nt][1] = fmaf(w1, back[half], sum_lse[nt][1]);
+                    sum[nt][0] = fmaf(w0 >= kNormal ? f.x : w0, back[half], sum[nt][0]);
+                    sum[nt][1] = fmaf(w1 >= kNormal ? f.y : w1, back[half], sum[nt][1]);
+                    pf[nt][half] = movmatrix_trans(w);  // thread (g, t): row g, tokens 2t, 2t + 1 (+ 8 half)
+                }
+
+#pragma unroll
+            for (int w = 0; w < kValueWords; ++w)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t x = __byte_perm(v[0][w], v[1][w], half ? 0x7632 : 0x5410), y = __byte_perm(v[2][w], v[3][w], half ? 0x7632 : 0x5410);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t x2 = x >> (8 * h), y2 = y >> (8 * h);
+                        const uint32_t f[4] = {kv4_low_codes(x2, vz[0]), kv4_high_codes(x2, vz[0]), kv4_low_codes(y2, vz[1]), kv4_high_codes(y2, vz[1])};
+#pragma unroll
+                        for (int nt = 0; nt < kNT; ++nt) mma_16816<false>(o[4 * w + 2 * half + h][nt], f, pf[nt][0], pf[nt][1]);
+                    }
+                }
+        }
+        cp_async_wait<0>();
+        __syncthreads();
+
+        // ---- join the four warps
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float x = sum[nt][j], y = sum_lse[nt][j];
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(~0u, x, d), y += __shfl_xor_sync(~0u, y, d);
+                const int row = 8 * nt + 2 * t + j;
+                if (g == 0) join_stat[warp * kRows + row] = make_float4(m_ref[nt][j], x, y, 0.0f);
+                float* vec = join_vec + (warp * kRows + row) * C::kVecPitch + kD / 8 * g;
+#pragma unroll
+                for (int c = 0; c < kSteps16; ++c) vec[2 * c] = o[c][nt][j], vec[2 * c + 1] = o[c][nt][j + 2];
+            }
+        __syncthreads();
+        finish_unit<kD, kRows, kBf16>(p, r, join_vec, join_stat, step0, step1, head, row0, n_rows);
+        __syncthreads();
+    }
+}
+
+template <int kD, int kNT>
+constexpr int resident_blocks() {
+    return 228 * 1024 / (Config<kD, kNT>::kSmemBytes + 1024 + 256);
+}
+int blocks_of(int sm_count, int64_t head_dim, int nt) {
+    const int per_sm = head_dim == 64 ? (nt == 2 ? resident_blocks<64, 2>() : resident_blocks<64, 1>())
+                       : head_dim == 128 ? (nt == 2 ? resident_blocks<128, 2>() : resident_blocks<128, 1>())
+                                         : resident_blocks<256, 1>();
+    return sm_count * std::min(per_sm, 3);
+}
+
+template <int kD, int kNT, bool kBf16>
+cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
+    using C = Config<kD, kNT>;
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(kv4_attention_kernel<kD, kNT, kBf16>, C::kSmemBytes, device, done);
+    if (e != cudaSuccess) return e;
+    if ((e = launch_early(kv4_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
+    return p.whole ? cudaSuccess : launch_join<kD, kNT, kBf16>(p, st);
+}
+
+// The kernel on tcgen05 pays from about 64 query rows per request and head on, as over the 8-bit cache.
+bool use_tc(const awe_kv4_cache& cache, int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t tokens, int64_t window) {
+    const int64_t head_dim = cache.head_dim;
+    if (head_dim > 128 || T * group < 64 * B) return false;
+    if (cache.n_pages * cache.n_heads * cache.page_size >= (int64_t)1 << 31) return false;  // its token rows are 32 bits
+    if (window > 0) tokens = std::min(tokens, window + T / B + 128);
+    return (double)T * n_q_heads * head_dim * tokens >= (double)(1 << 29);
+}
+
+}  // namespace
+}  // namespace awe
+
+using namespace awe;
+
+extern "C" size_t awe_kv4_attention_workspace_bytes(awe_handle_t h, const awe_kv4_cache* cache, int64_t T, int64_t n_q_heads, int64_t B) {
+    if (!h || check_kv4_cache(cache) != AWE_OK || T <= 0 || B <= 0 || n_q_heads <= 0 || n_q_heads % cache->n_heads) return 0;
+    size_t most = 0;
+    for (int nt = 1; nt <= (cache->head_dim < 256 ? 2 : 1); ++nt)
+        most = std::max(most, workspace_of(blocks_of(h->sm_count, cache->head_dim, nt), 8 * nt, cache->head_dim, B).total);
+    return std::max(most, kv_attention_tc_workspace_bytes(h, T, n_q_heads / cache->n_heads, B, cache->head_dim));
+}
+
+extern "C" awe_status_t awe_kv4_attention(awe_handle_t h, const awe_kv4_cache* cache, const void* q_dev, awe_float_t type, int64_t T,
+                                          int64_t n_q_heads, int64_t ldq, const int32_t* q_start_dev, const int32_t* ctx_len_dev,
+                                          int64_t B, const int32_t* block_table_dev, int64_t max_pages, int64_t ld_table, float scale,
+                                          int causal, int64_t window, void* out_dev, int64_t ldo, float* lse_dev,
+                                          void* workspace_dev, size_t workspace_bytes, void* stream) {
+    if (!h || T < 0 || B < 0) return AWE_ERR_INVALID_ARG;
+    const awe_status_t s = check_kv4_cache(cache);
+    if (s != AWE_OK) return s;
+    AttnParams p = {};
+    bool empty = false;
+    const awe_status_t c = attention_params(p, empty, q_dev, type, T, n_q_heads, ldq, q_start_dev, ctx_len_dev, B, block_table_dev, max_pages, ld_table,
+                                            scale, causal, window, out_dev, ldo, lse_dev, workspace_dev, cache->n_pages, cache->n_heads,
+                                            cache->page_size, cache->head_dim);
+    if (c != AWE_OK || empty) return c;
+    if (workspace_bytes < awe_kv4_attention_workspace_bytes(h, cache, T, n_q_heads, B)) return AWE_ERR_WORKSPACE;
+    p.k = reinterpret_cast<const int8_t*>(cache->k_dev), p.v = reinterpret_cast<const int8_t*>(cache->v_dev);
+    p.k_param = cache->k_param_dev, p.v_param = cache->v_param_dev;
+    if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, window))
+        return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, true, workspace_dev, (cudaStream_t)stream);
+    const int nt = row_tiles(T, B, p.group, cache->head_dim);
+    place_few(p, blocks_of(h->sm_count, cache->head_dim, nt), nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);
+    auto run = [&](auto dim, auto tiles) {
+        constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
+        return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)
+                                : launch_attention<kD, kNT, false>(p, h->device, (cudaStream_t)stream);
+    };
+    using std::integral_constant;
+    cudaError_t e;
+    if (cache->head_dim == 256) e = run(integral_constant<int, 256>(), integral_constant<int, 1>());
+    else if (cache->head_dim == 128)
+        e = nt == 2 ? run(integral_constant<int, 128>(), integral_constant<int, 2>()) : run(integral_constant<int, 128>(), integral_constant<int, 1>());
+    else
+        e = nt == 2 ? run(integral_constant<int, 64>(), integral_constant<int, 2>()) : run(integral_constant<int, 64>(), integral_constant<int, 1>());
+    if (e != cudaSuccess) return AWE_ERR_CUDA;
+    h->launches += p.whole ? 1 : 2;
+    return AWE_OK;
+}

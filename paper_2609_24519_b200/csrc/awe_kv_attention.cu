@@ -18,7 +18,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "kv_attention.cuh"
+#include "kv_attention_few.cuh"
 
 namespace awe {
 awe_status_t check_kv_cache(const awe_kv_cache* c);
@@ -26,30 +26,7 @@ awe_status_t check_kv_cache(const awe_kv_cache* c);
 namespace {
 
 using namespace serve;
-
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kStepTokens = 16 * kWarps;
-constexpr int kWholeTokens = 256;
-constexpr int64_t kWholeScans = 1 << 19;
-
-// The steps of one request: tokens [lo, hi) in steps of kStepTokens, for each of `units` units.
-struct Request {
-    int q0, n, ctx, lo, steps, units;
-};
-template <int kRows>
-__device__ __forceinline__ Request request_of(const AttnParams& p, int b) {
-    Request r;
-    r.q0 = min(max(p.q_start[b], 0), (int)p.T);
-    r.n = max(min(p.q_start[b + 1], (int)p.T) - r.q0, 0);
-    // no token beyond the table's row
-    r.ctx = (int)min((int64_t)max(p.ctx_len[b], 0), (int64_t)p.max_pages << p.page_log2);
-    const int64_t first = (int64_t)p.ctx_len[b] - r.n + 1 - p.window;  // first token that any of its queries sees
-    r.lo = p.window > 0 && first > 0 ? (int)min(first, (int64_t)r.ctx) & ~(kStepTokens - 1) : 0;
-    r.steps = max((r.ctx - r.lo + kStepTokens - 1) / kStepTokens, 1);  // one at least: its rows are to be written
-    r.units = (r.n * p.group + kRows - 1) / kRows * p.heads;
-    return r;
-}
+using namespace attn_few;
 
 template <int kD, int kNT>
 struct Config {
@@ -76,58 +53,15 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     using T16 = typename Half<kBf16>::type;
     constexpr int kRows = C::kRows, kSteps16 = kD / 16;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t scan[kWarps];
-    __shared__ int found_b;
-    __shared__ int64_t found_at;
+    __shared__ Search search;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
 
     grid_wait();
-    // ---- which steps are mine: exclusive sum of units x steps over the requests
-    int64_t total = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        const int64_t mine = pass ? Deal(total, p.blocks).begin(blockIdx.x) : 0;
-        int64_t sum = 0;
-        for (int b0 = 0; b0 < p.B; b0 += kThreads) {
-            const int b = b0 + tid;
-            int64_t w = 0;
-            if (b < p.B) {
-                const Request r = request_of<kRows>(p, b);
-                w = p.whole ? r.units : (int64_t)r.units * r.steps;
-            }
-            int64_t inc = w;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int64_t o = __shfl_up_sync(~0u, inc, d);
-                if (lane >= d) inc += o;
-            }
-            __syncthreads();
-            if (lane == 31) scan[warp] = inc;
-            __syncthreads();
-            int64_t before = sum;
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) {
-                if (i < warp) before += scan[i];
-                sum += scan[i];
-            }
-            const int64_t at = before + inc - w;
-            if (pass && b < p.B) {
-                if (blockIdx.x == 0) p.unit_steps[b] = at;
-                if (at <= mine && mine < at + w) {
-                    found_b = b;
-                    found_at = at;
-                }
-            }
-        }
-        total = sum;
-    }
-    if (blockIdx.x == 0 && tid == 0) p.unit_steps[p.B] = total;
-    __syncthreads();
-    const Deal deal(total, p.blocks);
-    if ((int)blockIdx.x >= deal.blocks || total == 0) return;
-    const int64_t begin = deal.begin(blockIdx.x), end = deal.begin(blockIdx.x + 1);
-
-    int b = found_b;
-    int64_t at = found_at;
+    Mine mine;
+    if (!find_steps<kRows>(p, search, mine)) return;
+    const int64_t begin = mine.begin, end = mine.end;
+    int b = mine.b;
+    int64_t at = mine.at;
     Request r = request_of<kRows>(p, b);
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * C::kStages * C::kStageBytes;
     float* join_vec = reinterpret_cast<float*>(smem);  // in the ring's place once it is empty
@@ -168,34 +102,11 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                 raw[4 * c][0] = lo.x, raw[4 * c][1] = lo.y, raw[4 * c + 1][0] = lo.z, raw[4 * c + 1][1] = lo.w;
                 raw[4 * c + 2][0] = hi.x, raw[4 * c + 2][1] = hi.y, raw[4 * c + 3][0] = hi.z, raw[4 * c + 3][1] = hi.w;
             }
-            if constexpr (kBf16) {
-                float m = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kSteps16; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float2 f = Half<true>::unpack(raw[i][j]);
-                        m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
-                    }
-                m = fmaxf(m, __shfl_xor_sync(~0u, m, 1));
-                m = fmaxf(m, __shfl_xor_sync(~0u, m, 2));
-                const int e = query_exponent((int)(__float_as_uint(m) >> 23));
-                const float down = power_of_2(15 - e);
-                factor *= power_of_2(e - 15);
-#pragma unroll
-                for (int i = 0; i < kSteps16; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float2 f = Half<true>::unpack(raw[i][j]);
-                        raw[i][j] = Half<false>::pack(f.x * down, f.y * down);
-                    }
-            }
+            query_to_fp16<kBf16>(raw, factor);
 #pragma unroll
             for (int i = 0; i < kSteps16; ++i) qf[nt][i][0] = raw[i][0], qf[nt][i][1] = raw[i][1];
-            const int64_t place = (int64_t)p.ctx_len[b] - r.n + query;  // of the query among its request's tokens
-            int hi_tok = p.causal ? (int)min((int64_t)r.ctx, place + 1) : r.ctx;
-            int lo_tok = p.window > 0 && place + 1 > p.window ? (int)min(place + 1 - p.window, (int64_t)r.ctx) : 0;
-            if (!live || hi_tok < 0) hi_tok = 0;
+            int lo_tok, hi_tok;
+            visible(p, r, b, query, live, lo_tok, hi_tok);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {  // from the thread that loaded row 2t + j
                 cq[nt][j] = __shfl_sync(~0u, factor, (2 * t + j) * 4);
@@ -204,24 +115,8 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
             }
         }
 
-        // tokens [all_lo, all_hi) that every row of the unit sees
-        int all_lo = 0, all_hi = 0x7FFFFFFF;
-#pragma unroll
-        for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (8 * nt + 2 * t + j < n_rows) all_lo = max(all_lo, see_lo[nt][j]), all_hi = min(all_hi, see_hi[nt][j]);
-        all_lo = __reduce_max_sync(~0u, all_lo);
-        all_hi = __reduce_min_sync(~0u, all_hi);
-        // tokens [any_lo, any_hi) that some row sees: the pages of others are not followed, which a window may have given up
-        int any_lo = 0x7FFFFFFF, any_hi = 0;
-#pragma unroll
-        for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (see_lo[nt][j] < see_hi[nt][j]) any_lo = min(any_lo, see_lo[nt][j]), any_hi = max(any_hi, see_hi[nt][j]);
-        any_lo = __reduce_min_sync(~0u, any_lo);
-        any_hi = __reduce_max_sync(~0u, any_hi);
+        const Sees sees = sees_of<kNT>(see_lo, see_hi, n_rows, t);
+        const int all_lo = sees.all_lo, all_hi = sees.all_hi, any_lo = sees.any_lo, any_hi = sees.any_hi;
 
         float o[kSteps16][kNT][4];
         float m_ref[kNT][2], sum[kNT][2], sum_lse[kNT][2];
@@ -431,113 +326,9 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                 }
             }
         __syncthreads();
-        const bool whole = step0 == 0 && step1 == r.steps;
-        const int slot = 2 * blockIdx.x + (step0 == 0);
-        for (int row = warp; row < n_rows; row += kWarps) {
-            float4 st[kWarps];
-            float m = -INFINITY, total_sum = 0.0f, total_lse = 0.0f, a[kWarps];
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                st[w] = join_stat[w * kRows + row];
-                m = fmaxf(m, st[w].x);
-            }
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                a[w] = st[w].x == -INFINITY ? (st[w].y == 0.0f ? 0.0f : 1.0f) : exp2_approx(st[w].x - m);
-                total_sum = fmaf(st[w].y, a[w], total_sum);
-                total_lse = fmaf(st[w].z, a[w], total_lse);
-            }
-            const int query = (row0 + row) / p.group, qh = head * p.group + (row0 + row) % p.group;
-            const int64_t token = r.q0 + query;
-            const float inv = total_sum == 0.0f ? 0.0f : 1.0f / total_sum;
-            T16* dst = reinterpret_cast<T16*>(p.out) + token * p.ldo + (int64_t)qh * kD;
-            for (int d = 4 * lane; d < kD; d += 128) {
-                float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float4 y = *reinterpret_cast<const float4*>(join_vec + (w * kRows + row) * C::kVecPitch + d);
-                    x.x = fmaf(y.x, a[w], x.x), x.y = fmaf(y.y, a[w], x.y), x.z = fmaf(y.z, a[w], x.z), x.w = fmaf(y.w, a[w], x.w);
-                }
-                if (whole)
-                    *reinterpret_cast<uint2*>(dst + d) =
-                        make_uint2(Half<kBf16>::pack(x.x * inv, x.y * inv), Half<kBf16>::pack(x.z * inv, x.w * inv));
-                else
-                    *reinterpret_cast<float4*>(p.part_vec + ((int64_t)slot * kRows + row) * kD + d) = x;
-            }
-            if (lane == 0) {
-                if (!whole) p.part_stat[(int64_t)slot * kRows + row] = make_float4(m, total_sum, total_lse, 0.0f);
-                else if (p.lse) p.lse[token * p.heads * p.group + qh] = total_lse == 0.0f ? -INFINITY : (m + log2f(total_lse)) * 0.69314718056f;
-            }
-        }
+        finish_unit<kD, kRows, kBf16>(p, r, join_vec, join_stat, step0, step1, head, row0, n_rows);
         __syncthreads();
     }
-}
-
-// Joins the parts of the units that were cut: one warp per (token, query head).
-template <int kD, int kNT, bool kBf16>
-__global__ void __launch_bounds__(kThreads) kv_attention_join_kernel(const AttnParams p) {
-    constexpr int kRows = 8 * kNT;
-    using T16 = typename Half<kBf16>::type;
-    const int lane = threadIdx.x & 31, q_heads = p.heads * p.group;
-    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    grid_wait();
-    if (item >= p.T * q_heads) return;
-    const int token = (int)(item / q_heads), qh = (int)(item % q_heads);
-    // the request of the token: last b with q_start[b] <= token
-    int b = 0;
-    for (int n = p.B; n > 1;) {
-        const int half = n >> 1;
-        if (p.q_start[b + half] <= token) b += half;
-        n -= half;
-    }
-    const Request r = request_of<kRows>(p, b);
-    if (token < r.q0 || token >= r.q0 + r.n) return;
-    const int64_t total = p.unit_steps[p.B];
-    const int row_all = (token - r.q0) * p.group + qh % p.group, row = row_all % kRows;
-    const int unit = row_all / kRows * p.heads + qh / p.group;
-    const int64_t w0 = p.unit_steps[b] + (int64_t)unit * r.steps, w1 = w0 + r.steps;
-    const Deal deal(total, p.blocks);
-    const int first = deal.block_of(w0), last = deal.block_of(w1 - 1);
-    if (first == last) return;  // one block had all of it
-    float m = -INFINITY, sum = 0.0f, sum_lse = 0.0f;
-    float4 x[kD / 128 + (kD < 128)];
-#pragma unroll
-    for (auto& v : x) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = first; i <= last; ++i) {
-        const int64_t part = ((int64_t)2 * i + (i == first)) * kRows + row;  // the first part is the one that begins the unit
-        const float4 st = p.part_stat[part];
-        const float m_new = fmaxf(m, st.x);
-        const float a = m == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_approx(m - m_new);
-        const float c = st.x == -INFINITY ? (st.y == 0.0f ? 0.0f : 1.0f) : exp2_approx(st.x - m_new);
-        sum = fmaf(sum, a, st.y * c);
-        sum_lse = fmaf(sum_lse, a, st.z * c);
-        m = m_new;
-#pragma unroll
-        for (int k = 0; k < (int)(sizeof(x) / sizeof(x[0])); ++k) {
-            const int d = 4 * lane + 128 * k;
-            if (d < kD) {
-                const float4 y = *reinterpret_cast<const float4*>(p.part_vec + part * kD + d);
-                x[k].x = fmaf(x[k].x, a, y.x * c), x[k].y = fmaf(x[k].y, a, y.y * c);
-                x[k].z = fmaf(x[k].z, a, y.z * c), x[k].w = fmaf(x[k].w, a, y.w * c);
-            }
-        }
-    }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T16* dst = reinterpret_cast<T16*>(p.out) + (int64_t)token * p.ldo + (int64_t)qh * kD;
-#pragma unroll
-    for (int k = 0; k < (int)(sizeof(x) / sizeof(x[0])); ++k) {
-        const int d = 4 * lane + 128 * k;
-        if (d < kD)
-            *reinterpret_cast<uint2*>(dst + d) =
-                make_uint2(Half<kBf16>::pack(x[k].x * inv, x[k].y * inv), Half<kBf16>::pack(x[k].z * inv, x[k].w * inv));
-    }
-    if (lane == 0 && p.lse) p.lse[(int64_t)token * q_heads + qh] = sum_lse == 0.0f ? -INFINITY : (m + log2f(sum_lse)) * 0.69314718056f;
-}
-
-// Query rows a unit holds: 16 where a request has more than 8 on average (their cache bytes are then read once),
-// else 8; head dimension 256 leaves no registers for 16.
-int row_tiles(int64_t T, int64_t B, int64_t group, int64_t head_dim) {
-    return head_dim < 256 && T * group > 8 * B ? 2 : 1;
 }
 
 // tcgen05 pays from about 64 query rows per request and head on, where the work fills its units of 256 rows x 128
@@ -552,17 +343,6 @@ bool use_tc(const awe_kv_cache& cache, int64_t T, int64_t B, int64_t n_q_heads, 
     if (cache.n_pages * cache.n_heads * cache.page_size * head_dim >= (int64_t)15 << 32) return false;  // its offsets are 32 bits of 16-byte units
     if (window > 0) tokens = std::min(tokens, window + T / B + 128);
     return (double)T * n_q_heads * head_dim * tokens >= (double)(1 << 29);
-}
-
-struct Workspace {
-    size_t vec, stat, total;
-};
-Workspace workspace_of(int blocks, int rows, int64_t head_dim, int64_t B) {
-    Workspace w;
-    w.vec = (size_t)round_up((B + 1) * 8, 256);
-    w.stat = w.vec + (size_t)2 * blocks * rows * head_dim * 4;
-    w.total = w.stat + (size_t)2 * blocks * rows * 16;
-    return w;
 }
 
 template <int kD, int kNT>
@@ -583,12 +363,38 @@ cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
     cudaError_t e = allow_smem(kv_attention_kernel<kD, kNT, kBf16>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
-    if (p.whole) return cudaSuccess;
-    const int64_t items = p.T * p.heads * p.group;
-    return launch_early(kv_attention_join_kernel<kD, kNT, kBf16>, dim3((unsigned)((items + kWarps - 1) / kWarps)), kThreads, 0, st, p);
+    return p.whole ? cudaSuccess : launch_join<kD, kNT, kBf16>(p, st);
 }
 
 }  // namespace
+
+awe_status_t attention_params(AttnParams& p, bool& empty, const void* q_dev, awe_float_t type, int64_t T, int64_t n_q_heads, int64_t ldq,
+                              const int32_t* q_start_dev, const int32_t* ctx_len_dev, int64_t B, const int32_t* block_table_dev,
+                              int64_t max_pages, int64_t ld_table, float scale, int causal, int64_t window, void* out_dev, int64_t ldo,
+                              float* lse_dev, void* workspace_dev, int64_t n_pages, int64_t n_heads, int64_t page_size, int64_t head_dim) {
+    if ((int)type < AWE_F16 || (int)type > AWE_F32 || window < 0 || (window > 0 && !causal)) return AWE_ERR_INVALID_ARG;
+    if (!is_half_type(type)) return AWE_ERR_UNSUPPORTED;
+    empty = T == 0 || B == 0;
+    if (empty) return AWE_OK;
+    const int64_t width = n_q_heads * head_dim;
+    if (!q_dev || !q_start_dev || !ctx_len_dev || !block_table_dev || !out_dev || !workspace_dev || n_q_heads <= 0 || n_q_heads % n_heads ||
+        max_pages <= 0 || ld_table < max_pages || (T > 1 && (ldq < width || ldo < width)))
+        return AWE_ERR_INVALID_ARG;
+    if (B > AWE_KV_MAX_REQUESTS || n_q_heads > 65535 || T * n_q_heads > INT32_MAX || max_pages > INT32_MAX / page_size) return AWE_ERR_UNSUPPORTED;
+    if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || ldq % 8 || ldo % 8 || (uintptr_t)workspace_dev % 256 ||
+        (uintptr_t)q_start_dev % 4 || (uintptr_t)ctx_len_dev % 4 || (uintptr_t)block_table_dev % 4 || (uintptr_t)lse_dev % 4)
+        return AWE_ERR_ALIGNMENT;
+    int page_log2 = 4;
+    while ((1 << page_log2) < page_size) ++page_log2;
+    p.q = q_dev, p.out = out_dev, p.lse = lse_dev;
+    p.q_start = q_start_dev, p.ctx_len = ctx_len_dev, p.table = block_table_dev;
+    p.ldq = ldq, p.ldo = ldo, p.ld_table = ld_table, p.T = T;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.B = (int)B, p.heads = (int)n_heads, p.group = (int)(n_q_heads / n_heads), p.page_log2 = page_log2;
+    p.n_pages = (int)n_pages, p.max_pages = (int)max_pages, p.causal = causal != 0;
+    p.window = window;
+    return AWE_OK;
+}
 }  // namespace awe
 
 using namespace awe;
@@ -599,7 +405,7 @@ extern "C" size_t awe_kv_attention_workspace_bytes(awe_handle_t h, const awe_kv_
     size_t most = 0;
     for (int nt = 1; nt <= (cache->head_dim < 256 ? 2 : 1); ++nt)
         most = std::max(most, workspace_of(blocks_of(h->sm_count, cache->head_dim, nt), 8 * nt, cache->head_dim, B).total);
-    return std::max(most, kv_attention_tc_workspace_bytes(h, T, n_q_heads, B, cache->head_dim));
+    return std::max(most, kv_attention_tc_workspace_bytes(h, T, n_q_heads / cache->n_heads, B, cache->head_dim));
 }
 
 extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cache, const void* q_dev, awe_float_t type,
@@ -611,47 +417,17 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     if (!h || T < 0 || B < 0) return AWE_ERR_INVALID_ARG;
     awe_status_t s = check_kv_cache(cache);
     if (s != AWE_OK) return s;
-    if ((int)type < AWE_F16 || (int)type > AWE_F32 || window < 0 || (window > 0 && !causal)) return AWE_ERR_INVALID_ARG;
-    if (!is_half_type(type)) return AWE_ERR_UNSUPPORTED;
-    if (T == 0 || B == 0) return AWE_OK;
-    const int64_t width = n_q_heads * cache->head_dim;
-    if (!q_dev || !q_start_dev || !ctx_len_dev || !block_table_dev || !out_dev || !workspace_dev || n_q_heads <= 0 ||
-        n_q_heads % cache->n_heads || max_pages <= 0 || ld_table < max_pages || (T > 1 && (ldq < width || ldo < width)))
-        return AWE_ERR_INVALID_ARG;
-    if (B > AWE_KV_MAX_REQUESTS || n_q_heads > 65535 || T * n_q_heads > INT32_MAX || max_pages > INT32_MAX / cache->page_size)
-        return AWE_ERR_UNSUPPORTED;
-    if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || ldq % 8 || ldo % 8 || (uintptr_t)workspace_dev % 256 ||
-        (uintptr_t)q_start_dev % 4 || (uintptr_t)ctx_len_dev % 4 || (uintptr_t)block_table_dev % 4 || (uintptr_t)lse_dev % 4)
-        return AWE_ERR_ALIGNMENT;
-    if (workspace_bytes < awe_kv_attention_workspace_bytes(h, cache, T, n_q_heads, B)) return AWE_ERR_WORKSPACE;
-    const int64_t group = n_q_heads / cache->n_heads;
-    const int nt = row_tiles(T, B, group, cache->head_dim);
-    int page_log2 = 4;
-    while ((1 << page_log2) < cache->page_size) ++page_log2;
     AttnParams p = {};
+    bool empty = false;
+    s = attention_params(p, empty, q_dev, type, T, n_q_heads, ldq, q_start_dev, ctx_len_dev, B, block_table_dev, max_pages, ld_table, scale, causal, window,
+                         out_dev, ldo, lse_dev, workspace_dev, cache->n_pages, cache->n_heads, cache->page_size, cache->head_dim);
+    if (s != AWE_OK || empty) return s;
+    if (workspace_bytes < awe_kv_attention_workspace_bytes(h, cache, T, n_q_heads, B)) return AWE_ERR_WORKSPACE;
     p.k = cache->k_dev, p.v = cache->v_dev, p.k_scale = cache->k_scale_dev, p.v_scale = cache->v_scale_dev;
-    p.q = q_dev, p.out = out_dev, p.lse = lse_dev;
-    p.q_start = q_start_dev, p.ctx_len = ctx_len_dev, p.table = block_table_dev;
-    p.ldq = ldq, p.ldo = ldo, p.ld_table = ld_table, p.T = T;
-    p.scale_log2 = scale * 1.4426950408889634f;
-    p.B = (int)B, p.heads = (int)cache->n_heads, p.group = (int)group, p.page_log2 = page_log2;
-    p.n_pages = (int)cache->n_pages, p.max_pages = (int)max_pages, p.causal = causal != 0;
-    p.window = window;
-    if (use_tc(*cache, T, B, n_q_heads, group, max_pages * cache->page_size, window))
-        return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, workspace_dev, (cudaStream_t)stream);
-    p.blocks = blocks_of(h->sm_count, cache->head_dim, nt);
-    // Short contexts: a block per unit and no second launch.  Each block scans all requests, so it pays while the units times the
-    // requests are few: up to 256 tokens for one query, 8 heads of 4 queries each, us whole / in parts with the join: 1 request
-    // 7.0 / 7.6, 64 16.2 / 17.6, 128 25.2 / 26.6, 256 50 / 47, 2,048 902 / 337; 1 head of 8: 128 7.6 / 11.1, 512 20.7 / 22.3, 1,024 47 / 38.
-    int64_t tokens = max_pages * cache->page_size;
-    if (window > 0) tokens = std::min(tokens, window + T / B + kStepTokens);
-    const int64_t units = (T * group / (8 * nt) + B) * cache->n_heads;
-    p.whole = tokens <= kWholeTokens && units * B <= kWholeScans;
-    const Workspace w = workspace_of(p.blocks, 8 * nt, cache->head_dim, B);
-    p.unit_steps = (int64_t*)workspace_dev;
-    p.part_vec = (float*)((uint8_t*)workspace_dev + w.vec);
-    p.part_stat = (float4*)((uint8_t*)workspace_dev + w.stat);
-    if (p.whole) p.blocks = (int)units;
+    if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, window))
+        return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, false, workspace_dev, (cudaStream_t)stream);
+    const int nt = row_tiles(T, B, p.group, cache->head_dim);
+    place_few(p, blocks_of(h->sm_count, cache->head_dim, nt), nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);
     auto run = [&](auto dim, auto tiles) {
         constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
         return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)

@@ -1,4 +1,5 @@
-// Attention over the paged 8-bit cache for prompts, on tcgen05.  The formula is that of awe_kv_attention.cu.
+// Attention over the paged cache of 8 or of 4 bits for prompts, on tcgen05.  The formulas are those of awe_kv_attention.cu and
+// awe_kv4_attention.cu.
 //
 // A unit of work is (request, cache head, 256 query rows), two tiles of 128 rows that share every key and value.  Per step
 // of 128 tokens four warps unpack the keys and values to FP16 (exact) in shared memory, one thread issues
@@ -15,11 +16,17 @@
 // they neither add to O nor move m, and their exponentials are summed apart, against a maximum of their own, in a pass that only
 // steps with such pages take; the two sums meet at the end.
 //
+// The cache of 4 bits has a scale for every token.  Its values, scale times (code - zero), are exact in FP16, so they are unpacked whole
+// and the softmax knows no scales.  A word's eight codes come apart in the order 0 4 1 5 2 6 3 7, in which the operands keep them: queries are
+// brought into it, results back.
+//
 // All steps of all units in a row are dealt out evenly to one block per SM; units that were cut are joined by a second
 // kernel in the order of the tokens.  A small kernel before lists the units' steps, which causality makes uneven.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_common.cuh"
+#include "kv4.cuh"
 #include "kv_attention.cuh"
 #include "ptx_serve.cuh"
 
@@ -149,7 +156,7 @@ struct Shared {
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
     float4 constants[4][kStep / 16];  // of 16 tokens: key scale, log2 of the value scale, kDivisorUnit over it
-    uint32_t unvalued[4];             // of a step: which 16 tokens have value scale 0
+    uint32_t unvalued[4];             // of a step: which 16 tokens have value scale 0; 4 bits: which have no page
     float2 unvalued_sum[kRows];       // of a query row over those: reference, sum of the exponentials
 };
 static_assert(sizeof(Shared) <= kSharedBytes, "shared memory behind the tiles");
@@ -202,7 +209,7 @@ __device__ __forceinline__ void add_unvalued(Shared* sh, uint32_t groups, int sl
     sh->unvalued_sum[row] = own;
 }
 
-template <int kD, bool kBf16>
+template <int kD, bool kBf16, bool kFour>
 __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
     using C = Config<kD>;
     using T16 = typename Half<kBf16>::type;
@@ -312,7 +319,95 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 return true;
             });
         }
-    } else if (warp >= kSoftWarps) {  // ---- unpack keys and values
+    } else if (kFour && warp >= kSoftWarps) {  // ---- unpack keys and values of 4 bits
+        constexpr int kPieces = kD / 32;          // 16-byte pieces per token, and passes per step
+        constexpr int kPassRows = 128 / kPieces;  // tokens per pass
+        const int thread = tid - 32 * kSoftWarps, c = thread % kPieces, r = thread / kPieces;
+        uint32_t step = 0;
+        for_parts([&](const Unit& u, int head, int s0, int s1) {
+            const int32_t* table = p.table + (int64_t)u.b * p.ld_table;
+            auto page_of = [&](int j) {  // lanes below 8: page of their 16 tokens of step j, -1 where there is none
+                const int tok = u.lo + j * kStep + 16 * lane;
+                int page = -1;
+                if (j < s1 && lane < kStep / 16 && tok < u.end && tok + 16 > u.first) {
+                    page = table[tok >> p.page_log2];
+                    if (page < 0 || page >= p.n_pages) page = -1;
+                }
+                return page;
+            };
+            uint4 kr[kPieces], vr[kPieces];
+            uint32_t kw[kPieces], vw[kPieces];  // parameter words
+            uint32_t at[kPieces];               // rows of the pieces of a step; ~0 where there is nothing
+            auto places = [&](int pages, int j) {
+                const int place = (u.lo + j * kStep) & ((1 << p.page_log2) - 1);
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const int row = i * kPassRows + r, page = __shfl_sync(~0u, pages, row >> 4);
+                    const uint32_t block = (uint32_t)(page * p.heads + head) << p.page_log2;
+                    at[i] = page < 0 ? ~0u : block + ((place + row) & ((1 << p.page_log2) - 1));
+                }
+            };
+            auto load = [&](const int8_t* pool, const uint16_t* params, uint4 (&x)[kPieces], uint32_t (&words)[kPieces]) {
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    x[i] = make_uint4(0, 0, 0, 0), words[i] = 0;  // become zeros, under a weight of 0
+                    if (at[i] != ~0u) {
+                        x[i] = __ldg(reinterpret_cast<const uint4*>(pool) + ((uint64_t)at[i] * kPieces + c));
+                        words[i] = __ldg(params + at[i]);
+                    }
+                }
+            };
+            auto store = [&](uint32_t to, uint4 (&x)[kPieces], const uint32_t (&words)[kPieces]) {
+                const int swap = kPieces == 4 ? c >> 1 : 0;  // the two blocks' threads write opposite halves first: no bank twice
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const int row = i * kPassRows + r;
+                    if (swap) x[i] = make_uint4(x[i].z, x[i].w, x[i].x, x[i].y);
+                    const __half2 scale = __float2half2_rn(kv4_scale(words[i]));
+                    const Kv4Zeros zero(__byte_perm(words[i], 0, 0x1010));
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t x0 = (&x[i].x)[w], x1 = x0 >> 8;
+                        const uint32_t h0 = mul2(kv4_low_codes(x0, zero), scale), h1 = mul2(kv4_high_codes(x0, zero), scale);
+                        const uint32_t h2 = mul2(kv4_low_codes(x1, zero), scale), h3 = mul2(kv4_high_codes(x1, zero), scale);
+                        const uint32_t at = to + (c >> 1) * kStep * 128 + row * 128 + ((((4 * c + (w ^ (2 * swap))) & 7) ^ (row & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(h0), "r"(h1), "r"(h2), "r"(h3) : "memory");
+                    }
+                }
+            };
+            int page = page_of(s0), next_page = page_of(s0 + 1);
+            places(page, s0);
+            load(p.k, p.k_param, kr, kw);
+            load(p.v, p.v_param, vr, vw);
+            for (int j = s0; j < s1; ++j, ++step) {
+                if (!__all_sync(~0u, wait(sh->k_empty[step & 1], ((step >> 1) & 1) ^ 1, 34))) return false;
+                store(base + C::kKAt + (step & 1) * C::kKBytes, kr, kw);
+                if (warp == kSoftWarps) {
+                    const uint32_t hidden = __ballot_sync(~0u, lane < kStep / 16 && page < 0);
+                    if (lane == 0) {
+                        sh->unvalued[step & 3] = hidden;
+                        ptx::mbar_arrive(ptx::smem_u32(&sh->c_full[step & 3]));
+                    }
+                }
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh->k_full[step & 1]));
+                const int after = page_of(j + 2);
+                if (j + 1 < s1) {
+                    places(next_page, j + 1);
+                    load(p.k, p.k_param, kr, kw);
+                }
+                if (!__all_sync(~0u, wait(sh->v_empty[step & 1], ((step >> 1) & 1) ^ 1, 35))) return false;
+                store(base + C::kVAt + (step & 1) * C::kKBytes, vr, vw);
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh->v_full[step & 1]));
+                if (j + 1 < s1) load(p.v, p.v_param, vr, vw);
+                page = next_page, next_page = after;
+            }
+            return true;
+        });
+    } else if (warp >= kSoftWarps) {  // ---- unpack keys and values of 8 bits
         constexpr int kPieces = kD / 16;            // 16-byte pieces per token, and passes per step
         constexpr int kPassRows = 128 / kPieces;    // tokens per pass
         const int thread = tid - 32 * kSoftWarps, c = thread % kPieces, r = thread / kPieces;
@@ -448,6 +543,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                         }
                     }
                     x.x ^= flip, x.y ^= flip, x.z ^= flip, x.w ^= flip;
+                    if constexpr (kFour)  // in the codes' order
+                        x = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
                     *reinterpret_cast<uint4*>(smem + C::kQAt + t * C::kQBytes + (i >> 3) * 128 * 128 + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = x;
                 }
                 ptx::fence_proxy_async();
@@ -460,13 +557,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             if (!live || see_hi < 0) see_hi = 0;
             const int all_lo = __reduce_max_sync(~0u, live ? see_lo : 0), all_hi = __reduce_min_sync(~0u, live ? see_hi : 0x7FFFFFFF);
             float m_ref = -INFINITY, sum = 0.0f;
-            sh->unvalued_sum[128 * t + row] = make_float2(-INFINITY, 0.0f);  // this thread's alone
+            if constexpr (kFour) cq = factor_of(1.0f, cq);
+            else sh->unvalued_sum[128 * t + row] = make_float2(-INFINITY, 0.0f);  // this thread's alone
             for (int j = s0; j < s1; ++j, ++step, ++done) {
                 const int tok0 = u.lo + j * kStep;
-                const bool cut = tok0 < all_lo || tok0 + kStep > all_hi;
                 // the unpacking warps' constants, and S
                 if (!__all_sync(~0u, wait(sh->c_full[step & 3], (step >> 2) & 1, 36) && wait(sh->s_full[t], done & 1, 37))) return false;
                 ptx::tc_fence_after();
+                const uint32_t no_page = kFour ? sh->unvalued[step & 3] : 0;  // of 8 bits the constants hide such tokens
+                const bool cut = tok0 < all_lo || tok0 + kStep > all_hi || no_page;
                 // Both passes read S in pieces of 32 tokens, the next on its way meanwhile; 16 tokens share their scales.
                 auto for_pieces = [&](auto f) {
                     uint32_t v[2][32];
@@ -485,24 +584,30 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                     const int lo = see_lo - tok0 - 16 * g, hi = see_hi - tok0 - 16 * g;
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (e < lo || e >= hi) v[e] = 0xFF800000u;
+                        if (e < lo || e >= hi || (kFour && (no_page >> (g + e / 16) & 1))) v[e] = 0xFF800000u;
                 };
                 auto factor = [&](const float4& k) { return factor_of(k.x, cq); };
                 float top = -INFINITY;  // the largest exponent: of each piece the largest score decides
                 for_pieces([&](int g, uint32_t (&v)[32]) {
                     if (cut) hide(g, v);
+                    if constexpr (kFour) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 k = sh->constants[step & 3][g + h];
-                        float m = __uint_as_float(v[16 * h]);
+                        for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(v[e]));
+                    } else {
 #pragma unroll
-                        for (int e = 1; e < 16; ++e) m = fmaxf(m, __uint_as_float(v[16 * h + e]));
-                        top = fmaxf(top, fmaf(m, factor(k), k.y));
+                        for (int h = 0; h < 2; ++h) {
+                            const float4 k = sh->constants[step & 3][g + h];
+                            float m = __uint_as_float(v[16 * h]);
+#pragma unroll
+                            for (int e = 1; e < 16; ++e) m = fmaxf(m, __uint_as_float(v[16 * h + e]));
+                            top = fmaxf(top, fmaf(m, factor(k), k.y));
+                        }
                     }
                 });
+                if constexpr (kFour) top *= cq;
                 const bool first = m_ref == -INFINITY;
                 const bool grows = top > (first ? -INFINITY : m_ref + kMostAbove);
-                const uint32_t unvalued = sh->unvalued[step & 3];
+                const uint32_t unvalued = kFour ? 0 : sh->unvalued[step & 3];
                 if (__any_sync(~0u, grows || unvalued)) {  // one branch on the way of most steps: with two they take 0.6 % longer
                     if (unvalued) add_unvalued(sh, unvalued, step & 3, s_at[t] + lanes, 128 * t + row, see_lo - tok0, see_hi - tok0, cq);
                     const float before = m_ref;
@@ -523,25 +628,41 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                         }
                     }
                 }
-                // P, over the pieces of S that have been read, and the sum of P / vs
+                // P, over the pieces of S that have been read, and its sum (8 bits: the sum of P / vs)
                 const float m = m_ref == -INFINITY ? 0.0f : m_ref;
                 float part = 0.0f;
                 for_pieces([&](int g, uint32_t (&v)[32]) {
                     if (cut) hide(g, v);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 k = sh->constants[step & 3][g + h];
-                        const float a = factor(k), b = k.y - m;
+                    if constexpr (kFour) {
                         float s0 = 0.0f, s1 = 0.0f;
-                        uint32_t pk[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float x = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e]), a, b)), y = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e + 1]), a, b));
-                            s0 += x, s1 += y;
-                            pk[e] = Half<false>::pack(x, y);
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t pk[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float x = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e]), cq, -m)), y = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e + 1]), cq, -m));
+                                s0 += x, s1 += y;
+                                pk[e] = Half<false>::pack(x, y);
+                            }
+                            ptx::tmem_st_32x8(s_at[t] + lanes + 8 * (g + h), pk);
                         }
-                        part = fmaf(s0 + s1, k.z, part);
-                        ptx::tmem_st_32x8(s_at[t] + lanes + 8 * (g + h), pk);
+                        part += s0 + s1;
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float4 k = sh->constants[step & 3][g + h];
+                            const float a = factor(k), b = k.y - m;
+                            float s0 = 0.0f, s1 = 0.0f;
+                            uint32_t pk[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float x = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e]), a, b)), y = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e + 1]), a, b));
+                                s0 += x, s1 += y;
+                                pk[e] = Half<false>::pack(x, y);
+                            }
+                            part = fmaf(s0 + s1, k.z, part);
+                            ptx::tmem_st_32x8(s_at[t] + lanes + 8 * (g + h), pk);
+                        }
                     }
                 });
                 sum += part;
@@ -554,8 +675,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             const bool whole = s0 == 0 && s1 == u.steps;
             const int64_t token = u.q0 + query, part_row = ((int64_t)2 * blockIdx.x + (s0 == 0)) * kRows + 128 * t + row;
             // sum is relative to m_ref + kDivisorLog2; with the other tokens' sum relative to the larger reference
-            float m_all = m_ref + kDivisorLog2, keep = kDivisorUnit;  // keep: what brings O to that reference
-            if (const float2 own = sh->unvalued_sum[128 * t + row]; own.y != 0.0f) {
+            float m_all = kFour ? m_ref : m_ref + kDivisorLog2, keep = kFour ? 1.0f : kDivisorUnit;  // keep: what brings O to that reference
+            if (const float2 own = kFour ? make_float2(0.0f, 0.0f) : sh->unvalued_sum[128 * t + row]; own.y != 0.0f) {
                 const float m = fmaxf(m_all, own.x), a = exp2_approx(m_all - m);
                 sum = fmaf(sum, a, own.y * exp2_approx(own.x - m));
                 keep *= a;
@@ -573,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 for (int e = 0; e < 32; e += 8) {
                     float f[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[e + i]);
+                    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[e + (kFour ? 2 * (i & 3) + (i >> 2) : i)]);
                     if (whole) {
                         *reinterpret_cast<uint4*>(dst + c + e) = make_uint4(Half<kBf16>::pack(f[0] * inv, f[1] * inv), Half<kBf16>::pack(f[2] * inv, f[3] * inv),
                                                                             Half<kBf16>::pack(f[4] * inv, f[5] * inv), Half<kBf16>::pack(f[6] * inv, f[7] * inv));
@@ -674,32 +795,38 @@ Workspace workspace_of(int blocks, int64_t T, int64_t group, int64_t B, int64_t 
     return w;
 }
 
-template <int kD, bool kBf16>
+template <int kD, bool kBf16, bool kFour>
 cudaError_t launch(const TcAttnParams& p, int device, cudaStream_t st) {
     using C = Config<kD>;
     static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(kv_attention_tc_kernel<kD, kBf16>, C::kSmemBytes, device, done);
+    cudaError_t e = allow_smem(kv_attention_tc_kernel<kD, kBf16, kFour>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_units_kernel, dim3(1), kPlanThreads, 0, st, p)) != cudaSuccess) return e;
-    if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16>, dim3(p.a.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
+    if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16, kFour>, dim3(p.a.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     const int64_t items = p.a.T * p.a.heads * p.a.group;
     return launch_early(kv_attention_tc_join_kernel<kD, kBf16>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
 }
 
 }  // namespace
 
-size_t kv_attention_tc_workspace_bytes(awe_ctx* h, int64_t T, int64_t n_q_heads, int64_t B, int64_t head_dim) {
-    return workspace_of(h->sm_count, T, n_q_heads, B, head_dim).total;
+size_t kv_attention_tc_workspace_bytes(awe_ctx* h, int64_t T, int64_t group, int64_t B, int64_t head_dim) {
+    return workspace_of(h->sm_count, T, group, B, head_dim).total;
 }
 
-awe_status_t kv_attention_tc(awe_ctx* h, AttnParams a, int64_t head_dim, bool bf16, void* workspace, cudaStream_t st) {
+awe_status_t kv_attention_tc(awe_ctx* h, AttnParams a, int64_t head_dim, bool bf16, bool four, void* workspace, cudaStream_t st) {
     a.blocks = h->sm_count;
     const Workspace w = workspace_of(a.blocks, a.T, a.group, a.B, head_dim);
     uint8_t* at = (uint8_t*)workspace;
     a.part_vec = (float*)(at + w.vec), a.part_stat = (float4*)(at + w.stat);
     TcAttnParams p = {a, (int64_t*)(at + w.steps), (int2*)(at + w.of), (int32_t*)(at + w.base), (int)(a.T * a.group / kRows + a.B), h->status_dev};
-    const cudaError_t e = head_dim == 64 ? (bf16 ? launch<64, true>(p, h->device, st) : launch<64, false>(p, h->device, st))
-                                         : (bf16 ? launch<128, true>(p, h->device, st) : launch<128, false>(p, h->device, st));
+    auto run = [&](auto dim, auto is_four) {
+        constexpr int kD = decltype(dim)::value;
+        constexpr bool kFour = decltype(is_four)::value;
+        return bf16 ? launch<kD, true, kFour>(p, h->device, st) : launch<kD, false, kFour>(p, h->device, st);
+    };
+    using std::integral_constant;
+    const cudaError_t e = head_dim == 64 ? (four ? run(integral_constant<int, 64>(), std::true_type()) : run(integral_constant<int, 64>(), std::false_type()))
+                                         : (four ? run(integral_constant<int, 128>(), std::true_type()) : run(integral_constant<int, 128>(), std::false_type()));
     if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 3;
     return AWE_OK;

@@ -8,7 +8,8 @@ namespace awe {
 
 struct AttnParams {
     const int8_t *k, *v;
-    const float *k_scale, *v_scale;
+    const float *k_scale, *v_scale;      // 8 bits: of pages and heads
+    const uint16_t *k_param, *v_param;  // 4 bits: of tokens and heads
     const void* q;
     void* out;
     float* lse;
@@ -59,8 +60,14 @@ __device__ __forceinline__ uint32_t bytes_to_half2(uint32_t flipped, uint32_t se
 }
 __device__ __forceinline__ uint32_t flip_signs(uint32_t w) { return w ^ 0x80808080u; }  // of four bytes
 
-// Prompts: the tcgen05 kernel; the arguments have been checked, p's pointers into the workspace are not set.
-size_t kv_attention_tc_workspace_bytes(awe_ctx* h, int64_t T, int64_t n_q_heads, int64_t B, int64_t head_dim);
-awe_status_t kv_attention_tc(awe_ctx* h, AttnParams p, int64_t head_dim, bool bf16, void* workspace, cudaStream_t st);
+// Checks the arguments that the two attention entry points share and fills in what they say; `empty`: there is nothing to do.
+awe_status_t attention_params(AttnParams& p, bool& empty, const void* q_dev, awe_float_t type, int64_t T, int64_t n_q_heads, int64_t ldq,
+                              const int32_t* q_start_dev, const int32_t* ctx_len_dev, int64_t B, const int32_t* block_table_dev,
+                              int64_t max_pages, int64_t ld_table, float scale, int causal, int64_t window, void* out_dev, int64_t ldo,
+                              float* lse_dev, void* workspace_dev, int64_t n_pages, int64_t n_heads, int64_t page_size, int64_t head_dim);
+
+// Prompts: the tcgen05 kernel, over the cache of 8 bits or of 4; the arguments have been checked, p's pointers into the workspace are not set.
+size_t kv_attention_tc_workspace_bytes(awe_ctx* h, int64_t T, int64_t group, int64_t B, int64_t head_dim);
+awe_status_t kv_attention_tc(awe_ctx* h, AttnParams p, int64_t head_dim, bool bf16, bool four, void* workspace, cudaStream_t st);
 
 }  // namespace awe
