@@ -7,7 +7,8 @@
 // warps.  Both products run on the 16-bit matrix instruction with FP32 sums.  The bytes of x, base, y and the adapters bound many
 // tokens, latency few; no operand is read by more than a few flops a byte, so operands go from global memory to registers directly:
 // the order of k (and of the rank) inside an instruction is free, and a thread takes eight (four) neighbours of a row.
-// u enters the second product as two 16-bit values, the rounded u and the rounded rest.
+// u enters the second product as several 16-bit values, the rounded u, the rounded rest of it, and so on: two hold 22 bits in FP16 and 16 in
+// BF16, whose third (24 bits) is taken where y is FP32.
 //
 // Units are numbered without a scan: request b's first is q_start[b] / kTokens + b, which leaves room for all of its units before
 // those of request b + 1.  Some numbers have no unit; their clusters end at once.
@@ -62,13 +63,20 @@ __device__ __forceinline__ Unit unit_of(const AdapterParams& p, int number) {
     return {(int)min(token, (int64_t)p.T), (int)max(min((int64_t)kTokens, q1 - token), (int64_t)0), adapter};
 }
 
-// A value as two of 16 bits.  FP16's range is narrow, so the values of a token are brought to [-2^15, 2^15] first (`down`).
+// A pair of values as kParts pairs of 16 bits: the rounded value, the rounded rest, and so on.  FP16's range is narrow, so the values of a
+// token are brought below 2^15 first (`down`).
+constexpr int kParts = 3;
 template <bool kBf16>
-__device__ __forceinline__ void split2(float x, float y, float down, uint32_t& hi, uint32_t& lo) {
+__device__ __forceinline__ void split(float x, float y, float down, uint32_t& first, uint32_t& second, uint32_t& third) {
     if constexpr (!kBf16) x *= down, y *= down;
-    hi = Half<kBf16>::pack(x, y);
-    const float2 f = Half<kBf16>::unpack(hi);
-    lo = Half<kBf16>::pack(x - f.x, y - f.y);
+    first = Half<kBf16>::pack(x, y);
+    float2 f = Half<kBf16>::unpack(first);
+    x -= f.x, y -= f.y;
+    second = Half<kBf16>::pack(x, y);
+    if constexpr (kBf16) {
+        f = Half<kBf16>::unpack(second);
+        third = Half<kBf16>::pack(x - f.x, y - f.y);
+    }
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 // Exponent that brings magnitudes up to `largest` below 2^15; both powers of it stay normal.
@@ -199,7 +207,8 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
     __syncthreads();
 
     // ---- y = base + B u: thread (g, t) holds of token g the ranks 4 t .. 4 t + 3 of each tile
-    uint32_t vh[kRT][2], vl[kRT][2];
+    uint32_t vs[kParts][kRT][2];
+    const bool third = kBf16 && p.y_f32;
     float back[2] = {1.0f, 1.0f};  // of the tokens 2 t, 2 t + 1
     {
         float v[kRT][4], most = 0.0f;
@@ -218,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
 #pragma unroll
         for (int r = 0; r < kRT; ++r)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) split2<kBf16>(v[r][2 * i], v[r][2 * i + 1], down, vh[r][i], vl[r][i]);
+            for (int i = 0; i < 2; ++i) split<kBf16>(v[r][2 * i], v[r][2 * i + 1], down, vs[0][r][i], vs[1][r][i], vs[2][r][i]);
     }
     for (int tile0 = me; tile0 < tiles; tile0 += all * kAhead) {
         if (tile0 != me) fetch(tile0);
@@ -230,8 +239,9 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
 #pragma unroll
             for (int r = 0; r < kRT; ++r) {
                 const uint32_t f[4] = {bw[i][r][0].x, bw[i][r][1].x, bw[i][r][0].y, bw[i][r][1].y};
-                mma_16816<kBf16>(d, f, vl[r][0], vl[r][1]);
-                mma_16816<kBf16>(d, f, vh[r][0], vh[r][1]);
+                if (third) mma_16816<kBf16>(d, f, vs[2][r][0], vs[2][r][1]);
+                mma_16816<kBf16>(d, f, vs[1][r][0], vs[1][r][1]);
+                mma_16816<kBf16>(d, f, vs[0][r][0], vs[0][r][1]);
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -348,7 +358,8 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
     // ---- y = base + B u: a warp has one tile of 16 tokens and 64 columns of y at a time
     constexpr int kRT = kRN / 2;
     const int m = warp & 1;
-    uint32_t vh[kRT][4], vl[kRT][4];
+    uint32_t vs[kParts][kRT][4];
+    const bool third = kBf16 && p.y_f32;
     float back[2] = {1.0f, 1.0f};  // of the tokens g, g + 8
     {
         const float* from[2] = {low + (16 * m + g) * M::kPitch + 4 * t, low + (16 * m + 8 + g) * M::kPitch + 4 * t};
@@ -373,8 +384,8 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float4 v = *reinterpret_cast<const float4*>(from[j] + 16 * r);
-                split2<kBf16>(v.x, v.y, down[j], vh[r][j], vl[r][j]);
-                split2<kBf16>(v.z, v.w, down[j], vh[r][2 + j], vl[r][2 + j]);
+                split<kBf16>(v.x, v.y, down[j], vs[0][r][j], vs[1][r][j], vs[2][r][j]);
+                split<kBf16>(v.z, v.w, down[j], vs[0][r][2 + j], vs[1][r][2 + j], vs[2][r][2 + j]);
             }
     }
     const T16* b = reinterpret_cast<const T16*>(p.b) + (int64_t)u.adapter * p.N * p.rank;
@@ -383,19 +394,53 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
     if (live_tokens > 0) {
         for (int block = part * (kWarps / 2) + (warp >> 1); block < blocks; block += parts * (kWarps / 2)) {
             const int n0 = 64 * block;
+            const bool vec = p.vec && n0 + 64 <= p.N;
+            // base's tile is on its way meanwhile: pieces of 16 bytes, or elements
+            uint32_t raw[32];
+            if (vec && p.base) {
+                if (p.y_f32) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = min(2 * i + (lane >> 4), live_tokens - 1), c = 4 * (lane & 15);
+                        *reinterpret_cast<uint4*>(raw + 4 * i) = *reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int row = min(4 * i + (lane >> 3), live_tokens - 1), c = 8 * (lane & 7);
+                        *reinterpret_cast<uint4*>(raw + 4 * i) = *reinterpret_cast<const uint4*>(reinterpret_cast<const T16*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int row = i >> 1, c = lane + 32 * (i & 1);
+                    raw[i] = 0;
+                    if (p.base && row < live_tokens && n0 + c < p.N) raw[i] = __float_as_uint(load_base<kBf16>(p, token0 + row, n0 + c));
+                }
+            }
             float d[8][4];
+            constexpr int kAtOnce = kRT <= 2 ? 8 : (kRT == 4 ? 4 : 2);  // tiles of 8 columns whose rows of B are on their way together
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i0 = 0; i0 < 8; i0 += kAtOnce) {
+                uint2 w[kAtOnce][kRT];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) d[i][j] = 0.0f;
-                uint2 w[kRT];
-                const int n = n0 + 8 * i + g;
+                for (int i = 0; i < kAtOnce; ++i) {
+                    const int n = n0 + 8 * (i0 + i) + g;
 #pragma unroll
-                for (int r = 0; r < kRT; ++r) w[r] = load8_if(b + (int64_t)n * p.rank + 16 * r + 4 * t, n < p.N && 16 * r + 4 * t < p.rank);
+                    for (int r = 0; r < kRT; ++r) w[i][r] = load8_if(b + (int64_t)n * p.rank + 16 * r + 4 * t, n < p.N && 16 * r + 4 * t < p.rank);
+                }
 #pragma unroll
-                for (int r = 0; r < kRT; ++r) {
-                    mma_16816<kBf16>(d[i], vl[r], w[r].x, w[r].y);
-                    mma_16816<kBf16>(d[i], vh[r], w[r].x, w[r].y);
+                for (int i = 0; i < kAtOnce; ++i) {
+                    float(&to)[4] = d[i0 + i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[j] = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < kRT; ++r) {
+                        if (third) mma_16816<kBf16>(to, vs[2][r], w[i][r].x, w[i][r].y);
+                        mma_16816<kBf16>(to, vs[1][r], w[i][r].x, w[i][r].y);
+                        mma_16816<kBf16>(to, vs[0][r], w[i][r].x, w[i][r].y);
+                    }
                 }
             }
             // through shared memory, so that a warp reads base and writes y along the rows
@@ -405,38 +450,33 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
                 for (int j = 0; j < 2; ++j)
                     *reinterpret_cast<float2*>(out + (8 * j + g) * M::kOutPitch + 8 * i + 2 * t) = make_float2(d[i][2 * j] * back[j], d[i][2 * j + 1] * back[j]);
             __syncwarp();
-            if (p.vec && n0 + 64 <= p.N) {
-                if (p.y_f32) {
+            if (vec && p.y_f32) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int row = 2 * i + (lane >> 4), c = 4 * (lane & 15);
-                        if (row >= live_tokens) continue;
-                        float4 s = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c);
-                        if (p.base) {
-                            const float4 o = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
-                            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
-                        }
-                        *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) = s;
-                    }
-                } else {
+                for (int i = 0; i < 8; ++i) {
+                    const int row = 2 * i + (lane >> 4), c = 4 * (lane & 15);
+                    if (row >= live_tokens) continue;
+                    float4 s = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c);
+                    s.x += __uint_as_float(raw[4 * i]), s.y += __uint_as_float(raw[4 * i + 1]);
+                    s.z += __uint_as_float(raw[4 * i + 2]), s.w += __uint_as_float(raw[4 * i + 3]);
+                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) = s;
+                }
+            } else if (vec) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int row = 4 * i + (lane >> 3), c = 8 * (lane & 7);
-                        if (row >= live_tokens) continue;
-                        const float4 s0 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c), s1 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c + 4);
-                        uint4 o = make_uint4(0, 0, 0, 0);  // base may be y, so not by the read-only path
-                        if (p.base) o = *reinterpret_cast<const uint4*>(reinterpret_cast<const T16*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
-                        const float2 o0 = Half<kBf16>::unpack(o.x), o1 = Half<kBf16>::unpack(o.y), o2 = Half<kBf16>::unpack(o.z), o3 = Half<kBf16>::unpack(o.w);
-                        *reinterpret_cast<uint4*>(reinterpret_cast<T16*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) =
-                            make_uint4(Half<kBf16>::pack(s0.x + o0.x, s0.y + o0.y), Half<kBf16>::pack(s0.z + o1.x, s0.w + o1.y),
-                                       Half<kBf16>::pack(s1.x + o2.x, s1.y + o2.y), Half<kBf16>::pack(s1.z + o3.x, s1.w + o3.y));
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 4 * i + (lane >> 3), c = 8 * (lane & 7);
+                    if (row >= live_tokens) continue;
+                    const float4 s0 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c), s1 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c + 4);
+                    const float2 o0 = Half<kBf16>::unpack(raw[4 * i]), o1 = Half<kBf16>::unpack(raw[4 * i + 1]);
+                    const float2 o2 = Half<kBf16>::unpack(raw[4 * i + 2]), o3 = Half<kBf16>::unpack(raw[4 * i + 3]);
+                    *reinterpret_cast<uint4*>(reinterpret_cast<T16*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) =
+                        make_uint4(Half<kBf16>::pack(s0.x + o0.x, s0.y + o0.y), Half<kBf16>::pack(s0.z + o1.x, s0.w + o1.y),
+                                   Half<kBf16>::pack(s1.x + o2.x, s1.y + o2.y), Half<kBf16>::pack(s1.z + o3.x, s1.w + o3.y));
                 }
             } else {
-#pragma unroll 8
+#pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     const int row = i >> 1, c = lane + 32 * (i & 1);
-                    if (row < live_tokens && n0 + c < p.N) store_y<kBf16>(p, token0 + row, n0 + c, out[row * M::kOutPitch + c] + load_base<kBf16>(p, token0 + row, n0 + c));
+                    if (row < live_tokens && n0 + c < p.N) store_y<kBf16>(p, token0 + row, n0 + c, out[row * M::kOutPitch + c] + __uint_as_float(raw[i]));
                 }
             }
             __syncwarp();

@@ -5,10 +5,11 @@
 // M is subtracted first: a product x c could pass FP32 where logits are a type's lowest value.
 // One pass: every thread keeps a maximum of its own and rescales its two sums when it grows.
 //
-// The most likely tokens.  A warp keeps the best so far in order, one a lane, and looks at a batch's elements one by one only if the
-// batch's maximum reaches the least of the best top_k of any warp of the block, which after a few batches is rare.  That bound
-// comes first from the top_k-th largest of the lanes' maxima of the first batch, then from the full lists.  Lists are joined in
-// pairs: of two lists in order, the larger of a[i] and b[31 - i] are the best 32, in an order that five exchanges sort.
+// The most likely tokens.  The top_k-th largest of a block's 256 thread maxima is a bound that top_k elements reach, and few others do:
+// the threads whose maximum reaches it look at their elements again (from the cache) and gather those that do, some 22 for 20.  They are sorted,
+// 32 a warp, and lists are joined in pairs: of two lists in order, the larger of a[i] and b[31 - i] are the best 32, in an order that
+// five exchanges sort.  Where more are gathered than there is room for (many equal logits), all warps look at all elements again: each keeps its best so
+// far in order, one a lane, and inserts what reaches the bound, which its own list and the others' raise.
 //
 // HBM bounds many rows; a single row is spread over a cluster of blocks that join in shared memory, which bounds it by latency.
 #include <cooperative_groups.h>
@@ -80,6 +81,15 @@ struct Piece {  // 16 bytes of logits
             return i & 1 ? f.y : f.x;
         }
     }
+    // Masked tokens alone, and a first element with nothing behind it.
+    static __device__ __forceinline__ uint4 nothing() {
+        constexpr uint32_t kMasked = kType == AWE_F32 ? 0xFF800000u : (kType == AWE_BF16 ? 0xFF80FF80u : 0xFC00FC00u);
+        return make_uint4(kMasked, kMasked, kMasked, kMasked);
+    }
+    static __device__ __forceinline__ uint4 single(float x) {
+        if constexpr (kType == AWE_F32) return make_uint4(__float_as_uint(x), 0, 0, 0);
+        else return make_uint4(Half<kType == AWE_BF16>::pack(x, 0.0f), 0, 0, 0);
+    }
     // The largest; NaN if one is.
     static __device__ __forceinline__ float largest(const uint4& w) {
         if constexpr (kType == AWE_F32)
@@ -115,9 +125,12 @@ __device__ __forceinline__ Sums join_sums(Sums a, Sums b, float c) {
     return {m, a.s0 + b.s0, a.s1 + b.s1};
 }
 
+constexpr int kRoom = 32 * kWarps;  // for gathered elements
 struct Shared {
     Sums sums[kWarps];
-    Entry list[kWarps][32];
+    Entry list[kWarps][32];  // also the gathered elements, one behind the other
+    float maxima[kWarps][32];
+    int gathered;
     Sums block_sums;
     Entry block_list[32];
     int bound;  // least of a full list's best top_k, as an ordered whole number
@@ -158,31 +171,8 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
     }
 
     Sums own = {-INFINITY, 0.0f, 0.0f};
+    bool one_list = false;  // whether the first warp has all of the block's
     Entry best = {-INFINITY, kNoToken};  // this lane's of the warp's list
-    float bound = -INFINITY;
-    // Elements first + i, i < count, of this thread's piece w.
-    auto look = [&](const uint4& w, int first, int count, float most) {
-        const unsigned any = __ballot_sync(~0u, most >= bound);
-        if (!any) return;
-#pragma unroll
-        for (int i = 0; i < P::kCount; ++i) {
-            const Entry mine = {P::at(w, i), first + i};
-            const Entry least = from_lane(best, p.top - 1);
-            unsigned ask = __ballot_sync(~0u, i < count && mine.x >= bound && before(mine, least));
-            for (; ask; ask &= ask - 1) {
-                const Entry e = from_lane(mine, __ffs(ask) - 1);
-                const bool stays = before(best, e);
-                const Entry above = {__shfl_up_sync(~0u, best.x, 1), __shfl_up_sync(~0u, best.id, 1)};
-                const unsigned keep = __ballot_sync(~0u, stays);  // lanes 0 .. n - 1
-                if (!stays) best = lane == __popc(keep) ? e : above;
-            }
-        }
-    };
-    auto raise_bound = [&] {  // to the least of this warp's best, if there are as many
-        const Entry least = from_lane(best, p.top - 1);
-        if (lane == 0 && least.id != kNoToken) atomicMax(&sh.bound, ordered(least.x));
-        bound = fmaxf(bound, from_ordered(*(volatile int*)&sh.bound));
-    };
     auto add = [&](const uint4& w, int count) {
         const float m = own.m == -INFINITY ? 0.0f : own.m;
 #pragma unroll
@@ -194,65 +184,119 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
             own.s1 = fmaf(e, t, own.s1);
         }
     };
-    // the ends of the row, an element a thread, by the first warp of the first block and of the last
-    auto end_of_row = [&](int first, int count) {
-        const bool live = lane < count;
-        const float one = live ? P::one(x + first + lane) : -INFINITY;
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if constexpr (kType == AWE_F32) w.x = __float_as_uint(one);
-        else w.x = Half<kType == AWE_BF16>::pack(one, 0.0f);
-        const float m = max_nan(own.m, one);
-        if (m != own.m) raise(own, m, c);
-        add(w, live);
-        if constexpr (kTop) look(w, first + lane, live, live ? one : -INFINITY);
+    // the ends of the row, an element a thread, by the first warp of the first block and the last of the last: f(element, its place)
+    auto at_ends = [&](auto f) {
+        if (rank == 0 && warp == 0 && lane < head) f(P::one(x + lane), lane);
+        if (rank == parts - 1 && warp == kWarps - 1 && lane < p.V - tail_at) f(P::one(x + tail_at + lane), tail_at + lane);
     };
-
-    uint4 w[kPieces] = {};
-    bool is_first = true;
-    for (int i0 = begin + warp * 32; i0 < end; i0 += kThreads * kPieces) {
+    for (int i0 = begin + tid; i0 < end; i0 += kThreads * kPieces) {
+        uint4 w[kPieces];
         float most = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kPieces; ++u) {
-            const int i = i0 + lane + u * kThreads;
-            if (i < end) w[u] = __ldcs(from + i);
+            const int i = i0 + u * kThreads;
+            w[u] = P::nothing();
+            if (i < end) w[u] = __ldg(from + i);
         }
-        float of_piece[kPieces];
 #pragma unroll
-        for (int u = 0; u < kPieces; ++u) {
-            of_piece[u] = i0 + lane + u * kThreads < end ? P::largest(w[u]) : -INFINITY;
-            most = max_nan(most, of_piece[u]);
-        }
+        for (int u = 0; u < kPieces; ++u) most = max_nan(most, P::largest(w[u]));
         if (!(most <= own.m)) raise(own, max_nan(own.m, most), c);
 #pragma unroll
-        for (int u = 0; u < kPieces; ++u)
-            if (i0 + lane + u * kThreads < end) add(w[u], P::kCount);
-        if constexpr (kTop) {
-            if (is_first) {
-                // as many lanes as top_k have a maximum that is not below the top_k-th largest of them
-                float m = most == most ? most : -INFINITY;
+        for (int u = 0; u < kPieces; ++u) add(w[u], P::kCount);
+    }
+    at_ends([&](float one, int) {
+        const float m = max_nan(own.m, one);
+        if (m != own.m) raise(own, m, c);
+        add(P::single(one), 1);
+    });
+
+    if constexpr (kTop) {
+        // ---- the bound: the top_k-th largest of the thread maxima (of threads without a NaN, whose maximum is not known)
+        float m = own.m == own.m ? own.m : -INFINITY;
 #pragma unroll
-                for (int k = 2; k <= 32; k <<= 1)
+        for (int k = 2; k <= 32; k <<= 1)
 #pragma unroll
-                    for (int d = k >> 1; d > 0; d >>= 1) {
-                        const float o = __shfl_xor_sync(~0u, m, d);
-                        m = ((lane & d) == 0) == ((lane & k) == 0) ? fmaxf(m, o) : fminf(m, o);
-                    }
-                bound = fmaxf(bound, __shfl_sync(~0u, m, p.top - 1));
-                is_first = false;
+            for (int d = k >> 1; d > 0; d >>= 1) {
+                const float o = __shfl_xor_sync(~0u, m, d);
+                m = ((lane & d) == 0) == ((lane & k) == 0) ? fmaxf(m, o) : fminf(m, o);
             }
-            if (__any_sync(~0u, !(most < bound))) {
+        sh.maxima[warp][lane] = m;
+        if (tid == 0) sh.gathered = 0;
+        __syncthreads();
+        for (int step = 1; step < kWarps; step <<= 1) {
+            if (warp % (2 * step) == 0) {
+                m = fmaxf(m, sh.maxima[warp + step][31 - lane]);
 #pragma unroll
-                for (int u = 0; u < kPieces; ++u) {
-                    const int i = i0 + lane + u * kThreads;
-                    // a NaN hides what else its piece has, so such a piece is looked at
-                    look(w[u], head + i * P::kCount, i < end ? P::kCount : 0, of_piece[u] == of_piece[u] ? of_piece[u] : INFINITY);
+                for (int d = 16; d > 0; d >>= 1) {
+                    const float o = __shfl_xor_sync(~0u, m, d);
+                    m = lane & d ? fminf(m, o) : fmaxf(m, o);
                 }
-                raise_bound();
+                sh.maxima[warp][lane] = m;
+            }
+            __syncthreads();
+        }
+        float bound = sh.maxima[0][p.top - 1];
+        // ---- what reaches it
+        auto gather = [&](float logit, int id) {
+            if (!(logit >= bound)) return;
+            const int at = atomicAdd(&sh.gathered, 1);
+            if (at < kRoom) sh.list[at >> 5][at & 31] = {logit, id};
+        };
+        if (!(own.m < bound)) {
+            for (int i = begin + tid; i < end; i += kThreads) {
+                const uint4 w = __ldg(from + i);
+                if (P::largest(w) < bound) continue;
+#pragma unroll
+                for (int e = 0; e < P::kCount; ++e) gather(P::at(w, e), head + i * P::kCount + e);
+            }
+            at_ends(gather);
+        }
+        __syncthreads();
+        const int gathered = sh.gathered;
+        one_list = gathered <= 32;
+        if (gathered <= kRoom) {
+            best = 32 * warp + lane < gathered ? sh.list[warp][lane] : Entry{-INFINITY, kNoToken};
+#pragma unroll
+            for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+                for (int d = k >> 1; d > 0; d >>= 1) {
+                    const Entry o = {__shfl_xor_sync(~0u, best.x, d), __shfl_xor_sync(~0u, best.id, d)};
+                    if (before(o, best) == (((lane & d) == 0) == ((lane & k) == 0))) best = o;
+                }
+        } else {
+            // Too many: every warp inserts what it finds among its elements into a list of its own.
+            auto look = [&](float logit, int id, bool live) {
+                const Entry mine = {logit, id};
+                const bool reaches = live && logit >= bound;
+                if (!__any_sync(~0u, reaches)) return;
+                const Entry least = from_lane(best, p.top - 1);  // by all lanes
+                unsigned ask = __ballot_sync(~0u, reaches && before(mine, least));
+                for (; ask; ask &= ask - 1) {
+                    const Entry e = from_lane(mine, __ffs(ask) - 1);
+                    const bool stays = before(best, e);
+                    const Entry above = {__shfl_up_sync(~0u, best.x, 1), __shfl_up_sync(~0u, best.id, 1)};
+                    const unsigned keep = __ballot_sync(~0u, stays);  // lanes 0 .. n - 1
+                    if (!stays) best = lane == __popc(keep) ? e : above;
+                }
+            };
+            for (int i0 = begin + 32 * warp; i0 < end; i0 += kThreads) {
+                const int i = i0 + lane;
+                const uint4 w = i < end ? __ldg(from + i) : P::nothing();
+#pragma unroll
+                for (int e = 0; e < P::kCount; ++e) look(P::at(w, e), head + i * P::kCount + e, i < end);
+                const Entry least = from_lane(best, p.top - 1);
+                if (lane == 0 && least.id != kNoToken) atomicMax(&sh.bound, ordered(least.x));
+                bound = fmaxf(bound, from_ordered(*(volatile int*)&sh.bound));
+            }
+            if (rank == 0 && warp == 0) look(lane < head ? P::one(x + lane) : 0.0f, lane, lane < head);
+            if (rank == parts - 1 && warp == kWarps - 1) {
+                const bool live = lane < p.V - tail_at;
+                look(live ? P::one(x + tail_at + lane) : 0.0f, tail_at + lane, live);
             }
         }
+        __syncthreads();
+        sh.list[warp][lane] = best;
     }
-    if (rank == 0 && warp == 0 && head > 0) end_of_row(0, head);
-    if (rank == parts - 1 && warp == kWarps - 1 && tail_at < p.V) end_of_row(tail_at, p.V - tail_at);
 
     // ---- the warp, the block, the cluster
 #pragma unroll
@@ -261,7 +305,6 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         own = lane & d ? join_sums(o, own, c) : join_sums(own, o, c);  // the same order on both sides
     }
     if (lane == 0) sh.sums[warp] = own;
-    if constexpr (kTop) sh.list[warp][lane] = best;
     __syncthreads();
     auto join_all = [&](int n, auto list_of) {  // lists list_of(0 .. n - 1), n a power of two: into the first
         for (int step = 1; step < n; step <<= 1) {
@@ -272,7 +315,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
             __syncthreads();
         }
     };
-    if constexpr (kTop) join_all(kWarps, [&](int i) { return sh.list[i]; });
+    if (kTop && !one_list) join_all(kWarps, [&](int i) { return sh.list[i]; });
     if (tid == 0) {
         for (int i = 1; i < kWarps; ++i) own = join_sums(own, sh.sums[i], c);
         sh.block_sums = own;
