@@ -15,6 +15,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "awe_internal.h"
 #include "serve_common.cuh"
@@ -27,7 +28,7 @@ namespace {
 using namespace serve;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMostCluster = 8;
+constexpr int kMostCluster = 16;
 constexpr int kFew = 8, kMany = 32;  // tokens of a unit
 
 struct AdapterParams {
@@ -37,7 +38,7 @@ struct AdapterParams {
     const int32_t *q_start, *adapter;
     int64_t ldx, ldb, ldy, n_adapters;
     int T, B, N, K, rank;
-    int y_f32, vec;  // vec: rows of base and y lie on 16 bytes
+    int vec;  // vec: rows of base and y lie on 16 bytes
 };
 
 struct Unit {
@@ -46,38 +47,44 @@ struct Unit {
 template <int kTokens>
 __device__ __forceinline__ Unit unit_of(const AdapterParams& p, int number) {
     const int lane = threadIdx.x & 31;
-    // last request whose first unit is not behind `number`: 32 requests are asked at a time
-    int b = 0, first = -1, q0 = 0;
+    // last request whose first unit is not behind `number`: 32 requests are asked at a time, and the last time all that is wanted of them
+    int b = 0;
     for (int n = p.B;;) {
         const int stride = (n + 31) / 32, i = lane * stride;
-        const int start = i < n ? min(max(p.q_start[b + i], 0), p.T) : 0, unit = start / kTokens + b + i;
+        int start = 0, next = 0, adapter = -1;
+        if (i < n) {
+            start = min(max(p.q_start[b + i], 0), p.T);
+            if (stride == 1) next = p.q_start[b + i + 1], adapter = p.adapter[b + i];
+        }
+        const int unit = start / kTokens + b + i;
         const unsigned fits = __ballot_sync(~0u, i < n && unit <= number);
         if (!fits) return {0, 0, -1};
         const int last = 31 - __clz(fits);
-        first = __shfl_sync(~0u, unit, last), q0 = __shfl_sync(~0u, start, last);
+        if (stride == 1) {
+            const int first = __shfl_sync(~0u, unit, last), q1 = min(__shfl_sync(~0u, next, last), p.T);
+            const int64_t token = __shfl_sync(~0u, start, last) + (int64_t)(number - first) * kTokens;
+            return {(int)min(token, (int64_t)p.T), (int)max(min((int64_t)kTokens, q1 - token), (int64_t)0), __shfl_sync(~0u, adapter, last)};
+        }
         b += last * stride, n = min(stride, n - last * stride);
-        if (n == 1) break;
     }
-    const int q1 = min(p.q_start[b + 1], p.T), adapter = p.adapter[b];
-    const int64_t token = q0 + (int64_t)(number - first) * kTokens;
-    return {(int)min(token, (int64_t)p.T), (int)max(min((int64_t)kTokens, q1 - token), (int64_t)0), adapter};
 }
 
 // A pair of values as kParts pairs of 16 bits: the rounded value, the rounded rest, and so on.  FP16's range is narrow, so the values of a
 // token are brought below 2^15 first (`down`).
-constexpr int kParts = 3;
-template <bool kBf16>
-__device__ __forceinline__ void split(float x, float y, float down, uint32_t& first, uint32_t& second, uint32_t& third) {
-    if constexpr (!kBf16) x *= down, y *= down;
-    first = Half<kBf16>::pack(x, y);
-    float2 f = Half<kBf16>::unpack(first);
-    x -= f.x, y -= f.y;
-    second = Half<kBf16>::pack(x, y);
-    if constexpr (kBf16) {
-        f = Half<kBf16>::unpack(second);
-        third = Half<kBf16>::pack(x - f.x, y - f.y);
+template <bool kBf16, int kParts>
+struct Split {
+    uint32_t part[kParts];
+    __device__ __forceinline__ Split() {}
+    __device__ __forceinline__ Split(float x, float y, float down) {
+        if constexpr (!kBf16) x *= down, y *= down;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            part[i] = Half<kBf16>::pack(x, y);
+            const float2 f = Half<kBf16>::unpack(part[i]);
+            x -= f.x, y -= f.y;
+        }
     }
-}
+};
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 // Exponent that brings magnitudes up to `largest` below 2^15; both powers of it stay normal.
 __device__ __forceinline__ int down_exponent(float largest) { return min(max((int)(__float_as_uint(largest) >> 23) - 127 - 14, -120), 120); }
@@ -88,31 +95,65 @@ __device__ __forceinline__ uint4 load16_if(const void* from, bool live) {
 __device__ __forceinline__ uint2 load8_if(const void* from, bool live) {
     return live ? __ldg(reinterpret_cast<const uint2*>(from)) : make_uint2(0, 0);
 }
-template <bool kBf16>
-__device__ __forceinline__ float load_base(const AdapterParams& p, int64_t token, int n) {
-    if (!p.base) return 0.0f;
-    const int64_t at = token * p.ldb + n;
-    return p.y_f32 ? reinterpret_cast<const float*>(p.base)[at] : Half<kBf16>::to_float(reinterpret_cast<const typename Half<kBf16>::type*>(p.base)[at]);
-}
-template <bool kBf16>
-__device__ __forceinline__ void store_y(const AdapterParams& p, int64_t token, int n, float y) {
-    const int64_t at = token * p.ldy + n;
-    if (p.y_f32) reinterpret_cast<float*>(p.y)[at] = y;
-    else reinterpret_cast<typename Half<kBf16>::type*>(p.y)[at] = Half<kBf16>::from_float(y);
-}
+// Elements of base and y: FP32, or of the adapters' type.
+template <bool kBf16, bool kF32>
+struct Out {
+    using T = typename std::conditional<kF32, float, typename Half<kBf16>::type>::type;
+    static __device__ __forceinline__ float load(const T* at) {
+        if constexpr (kF32) return *at;
+        else return Half<kBf16>::to_float(*at);
+    }
+    static __device__ __forceinline__ void store(T* at, float y) {
+        if constexpr (kF32) *at = y;
+        else *at = Half<kBf16>::from_float(y);
+    }
+};
 
-// A unit without an adapter: y = base, by all threads of the cluster.
-template <bool kBf16>
+// A unit without an adapter: y = base, a row a warp, kAhead pieces on their way together (base and y may be one, so the compiler moves no
+// load before a store).
+template <class O, int kAhead>
 __device__ __forceinline__ void copy_base(const AdapterParams& p, const Unit& u, int part, int parts) {
+    using T = typename O::T;
     if (p.base == p.y) return;
-    for (int i = 0; i < u.n; ++i)
-        for (int n = part * kThreads + threadIdx.x; n < p.N; n += parts * kThreads) store_y<kBf16>(p, u.token + i, n, load_base<kBf16>(p, u.token + i, n));
+    constexpr int kPiece = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31;
+    // few tokens: a row goes to several warps
+    const int warps = parts * kWarps, each = max(warps / u.n, 1), warp = part * kWarps + (threadIdx.x >> 5);
+    if (warp >= each * u.n && each > 1) return;
+    for (int i = warp / each; i < u.n; i += max(warps / each, 1)) {
+        const T* from = reinterpret_cast<const T*>(p.base) + (int64_t)(u.token + i) * p.ldb;
+        T* to = reinterpret_cast<T*>(p.y) + (int64_t)(u.token + i) * p.ldy;
+        const int first = (warp % each) * 32 + lane, stride = 32 * each;
+        int done = 0;
+        if (p.vec) {
+            const int pieces = p.N / kPiece;
+            for (int c = first; c < pieces; c += kAhead * stride) {
+                uint4 x[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) x[k] = p.base && c + k * stride < pieces ? reinterpret_cast<const uint4*>(from)[c + k * stride] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (c + k * stride < pieces) reinterpret_cast<uint4*>(to)[c + k * stride] = x[k];
+            }
+            done = pieces * kPiece;
+        }
+        for (int n = done + first; n < p.N; n += 2 * kAhead * stride) {
+            float x[2 * kAhead];
+#pragma unroll
+            for (int k = 0; k < 2 * kAhead; ++k) x[k] = p.base && n + k * stride < p.N ? O::load(from + n + k * stride) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 2 * kAhead; ++k)
+                if (n + k * stride < p.N) O::store(to + n + k * stride, x[k]);
+        }
+    }
 }
 
 // Few tokens: they are the instruction's 8 columns, ranks (then n) its 16 rows.  kRT tiles of 16 ranks.
-template <bool kBf16, int kRT>
-__global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterParams p) {
+template <bool kBf16, bool kF32, int kRT>
+__global__ void __launch_bounds__(kThreads, kRT == 1 ? 3 : 2) adapters_few_kernel(const AdapterParams p) {
     using T16 = typename Half<kBf16>::type;
+    using O = Out<kBf16, kF32>;
+    constexpr int kParts = kBf16 && kF32 ? 3 : 2;
     constexpr int kValues = kRT * 16 * kFew;
     constexpr int kAhead = kRT <= 2 ? 4 : (kRT == 4 ? 2 : 1);  // steps of k, and tiles of n, that are on their way together
     __shared__ float sums[kWarps][kValues];
@@ -124,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
     grid_wait();
     const Unit u = unit_of<kFew>(p, blockIdx.x / parts);
     if (u.n == 0) return;  // the whole cluster
-    if (u.adapter < 0 || u.adapter >= p.n_adapters) return copy_base<kBf16>(p, u, part, parts);
+    if (u.adapter < 0 || u.adapter >= p.n_adapters) return copy_base<O, 4>(p, u, part, parts);
     const int me = part * kWarps + warp, all = parts * kWarps;
 
     // ---- u = A x
@@ -166,6 +207,13 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
     const int tiles = (p.N + 15) / 16;
     uint2 bw[kAhead][kRT][2];
     float base[kAhead][4];
+    const typename O::T* base_row[2];  // of the tokens 2 t, 2 t + 1
+    typename O::T* y_row[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        base_row[c] = reinterpret_cast<const typename O::T*>(p.base) + (int64_t)(u.token + 2 * t + c) * p.ldb;
+        y_row[c] = reinterpret_cast<typename O::T*>(p.y) + (int64_t)(u.token + 2 * t + c) * p.ldy;
+    }
     auto fetch = [&](int tile0) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -176,7 +224,7 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
 #pragma unroll
                 for (int r = 0; r < kRT; ++r) bw[i][r][j] = load8_if(b + (int64_t)n * p.rank + 16 * r + 4 * t, tile < tiles && n < p.N && 16 * r + 4 * t < p.rank);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) base[i][2 * j + c] = tile < tiles && n < p.N && 2 * t + c < u.n ? load_base<kBf16>(p, u.token + 2 * t + c, n) : 0.0f;
+                for (int c = 0; c < 2; ++c) base[i][2 * j + c] = p.base && tile < tiles && n < p.N && 2 * t + c < u.n ? O::load(base_row[c] + n) : 0.0f;
             }
         }
     };
@@ -207,8 +255,7 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
     __syncthreads();
 
     // ---- y = base + B u: thread (g, t) holds of token g the ranks 4 t .. 4 t + 3 of each tile
-    uint32_t vs[kParts][kRT][2];
-    const bool third = kBf16 && p.y_f32;
+    Split<kBf16, kParts> vs[kRT][2];
     float back[2] = {1.0f, 1.0f};  // of the tokens 2 t, 2 t + 1
     {
         float v[kRT][4], most = 0.0f;
@@ -227,7 +274,7 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
 #pragma unroll
         for (int r = 0; r < kRT; ++r)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) split<kBf16>(v[r][2 * i], v[r][2 * i + 1], down, vs[0][r][i], vs[1][r][i], vs[2][r][i]);
+            for (int i = 0; i < 2; ++i) vs[r][i] = Split<kBf16, kParts>(v[r][2 * i], v[r][2 * i + 1], down);
     }
     for (int tile0 = me; tile0 < tiles; tile0 += all * kAhead) {
         if (tile0 != me) fetch(tile0);
@@ -239,16 +286,15 @@ __global__ void __launch_bounds__(kThreads) adapters_few_kernel(const AdapterPar
 #pragma unroll
             for (int r = 0; r < kRT; ++r) {
                 const uint32_t f[4] = {bw[i][r][0].x, bw[i][r][1].x, bw[i][r][0].y, bw[i][r][1].y};
-                if (third) mma_16816<kBf16>(d, f, vs[2][r][0], vs[2][r][1]);
-                mma_16816<kBf16>(d, f, vs[1][r][0], vs[1][r][1]);
-                mma_16816<kBf16>(d, f, vs[0][r][0], vs[0][r][1]);
+#pragma unroll
+                for (int k = kParts - 1; k >= 0; --k) mma_16816<kBf16>(d, f, vs[r][0].part[k], vs[r][1].part[k]);
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
                     if (const int n = 16 * tile + 8 * j + g; n < p.N && 2 * t + c < u.n)
-                        store_y<kBf16>(p, u.token + 2 * t + c, n, fmaf(d[2 * j + c], back[c], base[i][2 * j + c]));
+                        O::store(y_row[c] + n, fmaf(d[2 * j + c], back[c], base[i][2 * j + c]));
         }
     }
     cluster.barrier_wait();  // no block leaves while its sums are read
@@ -266,10 +312,12 @@ struct Many {
     static constexpr int kSmemBytes = kLowAt + kMany * kPitch * 4;
 };
 
-template <bool kBf16, int kRN>
-__global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterParams p) {
+template <bool kBf16, bool kF32, int kRN>
+__global__ void __launch_bounds__(kThreads, kRN <= 8 ? 2 : 1) adapters_many_kernel(const AdapterParams p) {
     using M = Many<kRN>;
     using T16 = typename Half<kBf16>::type;
+    using O = Out<kBf16, kF32>;
+    constexpr int kParts = kBf16 && kF32 ? 3 : 2;
     extern __shared__ __align__(16) uint8_t smem[];
     float* sums = reinterpret_cast<float*>(smem);
     float* part_sums = reinterpret_cast<float*>(smem + M::kPartAt);
@@ -280,7 +328,7 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
     grid_wait();
     const Unit u = unit_of<kMany>(p, blockIdx.x / parts);
     if (u.n == 0) return;  // the whole cluster
-    if (u.adapter < 0 || u.adapter >= p.n_adapters) return copy_base<kBf16>(p, u, part, parts);
+    if (u.adapter < 0 || u.adapter >= p.n_adapters) return copy_base<O, 8>(p, u, part, parts);
     const int me = part * kWarps + warp, all = parts * kWarps;
 
     // ---- u = A x: every warp has all tokens and ranks and its own steps of k
@@ -359,7 +407,6 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
     constexpr int kRT = kRN / 2;
     const int m = warp & 1;
     uint32_t vs[kParts][kRT][4];
-    const bool third = kBf16 && p.y_f32;
     float back[2] = {1.0f, 1.0f};  // of the tokens g, g + 8
     {
         const float* from[2] = {low + (16 * m + g) * M::kPitch + 4 * t, low + (16 * m + 8 + g) * M::kPitch + 4 * t};
@@ -384,51 +431,50 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float4 v = *reinterpret_cast<const float4*>(from[j] + 16 * r);
-                split<kBf16>(v.x, v.y, down[j], vs[0][r][j], vs[1][r][j], vs[2][r][j]);
-                split<kBf16>(v.z, v.w, down[j], vs[0][r][2 + j], vs[1][r][2 + j], vs[2][r][2 + j]);
+                const Split<kBf16, kParts> x(v.x, v.y, down[j]), z(v.z, v.w, down[j]);
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) vs[k][r][j] = x.part[k], vs[k][r][2 + j] = z.part[k];
             }
     }
     const T16* b = reinterpret_cast<const T16*>(p.b) + (int64_t)u.adapter * p.N * p.rank;
     float* out = reinterpret_cast<float*>(smem) + warp * 16 * M::kOutPitch;
     const int blocks = (p.N + 63) / 64, token0 = u.token + 16 * m, live_tokens = min(16, u.n - 16 * m);
+    const typename O::T* base = reinterpret_cast<const typename O::T*>(p.base) + (int64_t)token0 * p.ldb;
+    typename O::T* y = reinterpret_cast<typename O::T*>(p.y) + (int64_t)token0 * p.ldy;
     if (live_tokens > 0) {
         for (int block = part * (kWarps / 2) + (warp >> 1); block < blocks; block += parts * (kWarps / 2)) {
             const int n0 = 64 * block;
             const bool vec = p.vec && n0 + 64 <= p.N;
-            // base's tile is on its way meanwhile: pieces of 16 bytes, or elements
+            // base's tile is on its way meanwhile: kRowsAtOnce rows in pieces of 16 bytes, or two elements a row
+            constexpr int kPiece = 16 / sizeof(typename O::T), kLanes = 64 / kPiece, kRowsAtOnce = 32 / kLanes, kPieces = 16 / kRowsAtOnce;
             uint32_t raw[32];
-            if (vec && p.base) {
-                if (p.y_f32) {
+            if (vec) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int row = min(2 * i + (lane >> 4), live_tokens - 1), c = 4 * (lane & 15);
-                        *reinterpret_cast<uint4*>(raw + 4 * i) = *reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int row = min(4 * i + (lane >> 3), live_tokens - 1), c = 8 * (lane & 7);
-                        *reinterpret_cast<uint4*>(raw + 4 * i) = *reinterpret_cast<const uint4*>(reinterpret_cast<const T16*>(p.base) + (int64_t)(token0 + row) * p.ldb + n0 + c);
-                    }
+                for (int i = 0; i < kPieces; ++i) {
+                    const int row = min(kRowsAtOnce * i + lane / kLanes, live_tokens - 1);
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (p.base) x = *reinterpret_cast<const uint4*>(base + (int64_t)row * p.ldb + n0 + kPiece * (lane % kLanes));
+                    raw[4 * i] = x.x, raw[4 * i + 1] = x.y, raw[4 * i + 2] = x.z, raw[4 * i + 3] = x.w;
                 }
             } else {
+                const typename O::T* from = base + n0 + lane;
+                const bool in[2] = {p.base && n0 + lane < p.N, p.base && n0 + lane + 32 < p.N};
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int row = i >> 1, c = lane + 32 * (i & 1);
-                    raw[i] = 0;
-                    if (p.base && row < live_tokens && n0 + c < p.N) raw[i] = __float_as_uint(load_base<kBf16>(p, token0 + row, n0 + c));
-                }
+                for (int row = 0; row < 16; ++row, from += p.ldb)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) raw[2 * row + c] = in[c] && row < live_tokens ? __float_as_uint(O::load(from + 32 * c)) : 0;
             }
             float d[8][4];
-            constexpr int kAtOnce = kRT <= 2 ? 8 : (kRT == 4 ? 4 : 2);  // tiles of 8 columns whose rows of B are on their way together
+            constexpr int kAtOnce = kRT <= 2 ? 4 : 2;  // tiles of 8 columns whose rows of B are on their way together
 #pragma unroll
             for (int i0 = 0; i0 < 8; i0 += kAtOnce) {
                 uint2 w[kAtOnce][kRT];
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
                     const int n = n0 + 8 * (i0 + i) + g;
+                    const T16* from = b + (int64_t)n * p.rank + 4 * t;
 #pragma unroll
-                    for (int r = 0; r < kRT; ++r) w[i][r] = load8_if(b + (int64_t)n * p.rank + 16 * r + 4 * t, n < p.N && 16 * r + 4 * t < p.rank);
+                    for (int r = 0; r < kRT; ++r) w[i][r] = load8_if(from + 16 * r, n < p.N && 16 * r + 4 * t < p.rank);
                 }
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
@@ -436,11 +482,9 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
 #pragma unroll
                     for (int j = 0; j < 4; ++j) to[j] = 0.0f;
 #pragma unroll
-                    for (int r = 0; r < kRT; ++r) {
-                        if (third) mma_16816<kBf16>(to, vs[2][r], w[i][r].x, w[i][r].y);
-                        mma_16816<kBf16>(to, vs[1][r], w[i][r].x, w[i][r].y);
-                        mma_16816<kBf16>(to, vs[0][r], w[i][r].x, w[i][r].y);
-                    }
+                    for (int r = 0; r < kRT; ++r)
+#pragma unroll
+                        for (int k = kParts - 1; k >= 0; --k) mma_16816<kBf16>(to, vs[k][r], w[i][r].x, w[i][r].y);
                 }
             }
             // through shared memory, so that a warp reads base and writes y along the rows
@@ -450,34 +494,32 @@ __global__ void __launch_bounds__(kThreads) adapters_many_kernel(const AdapterPa
                 for (int j = 0; j < 2; ++j)
                     *reinterpret_cast<float2*>(out + (8 * j + g) * M::kOutPitch + 8 * i + 2 * t) = make_float2(d[i][2 * j] * back[j], d[i][2 * j + 1] * back[j]);
             __syncwarp();
-            if (vec && p.y_f32) {
+            if (vec) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = 2 * i + (lane >> 4), c = 4 * (lane & 15);
-                    if (row >= live_tokens) continue;
-                    float4 s = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c);
-                    s.x += __uint_as_float(raw[4 * i]), s.y += __uint_as_float(raw[4 * i + 1]);
-                    s.z += __uint_as_float(raw[4 * i + 2]), s.w += __uint_as_float(raw[4 * i + 3]);
-                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) = s;
-                }
-            } else if (vec) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 4 * i + (lane >> 3), c = 8 * (lane & 7);
-                    if (row >= live_tokens) continue;
-                    const float4 s0 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c), s1 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c + 4);
-                    const float2 o0 = Half<kBf16>::unpack(raw[4 * i]), o1 = Half<kBf16>::unpack(raw[4 * i + 1]);
-                    const float2 o2 = Half<kBf16>::unpack(raw[4 * i + 2]), o3 = Half<kBf16>::unpack(raw[4 * i + 3]);
-                    *reinterpret_cast<uint4*>(reinterpret_cast<T16*>(p.y) + (int64_t)(token0 + row) * p.ldy + n0 + c) =
-                        make_uint4(Half<kBf16>::pack(s0.x + o0.x, s0.y + o0.y), Half<kBf16>::pack(s0.z + o1.x, s0.w + o1.y),
-                                   Half<kBf16>::pack(s1.x + o2.x, s1.y + o2.y), Half<kBf16>::pack(s1.z + o3.x, s1.w + o3.y));
+                for (int i = 0; i < kPieces; ++i) {
+                    const int row = kRowsAtOnce * i + lane / kLanes, c = kPiece * (lane % kLanes);
+                    const float4 s0 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c);
+                    uint4 x;
+                    if constexpr (kF32) {
+                        x = make_uint4(__float_as_uint(s0.x + __uint_as_float(raw[4 * i])), __float_as_uint(s0.y + __uint_as_float(raw[4 * i + 1])),
+                                       __float_as_uint(s0.z + __uint_as_float(raw[4 * i + 2])), __float_as_uint(s0.w + __uint_as_float(raw[4 * i + 3])));
+                    } else {
+                        const float4 s1 = *reinterpret_cast<const float4*>(out + row * M::kOutPitch + c + 4);
+                        const float2 o0 = Half<kBf16>::unpack(raw[4 * i]), o1 = Half<kBf16>::unpack(raw[4 * i + 1]);
+                        const float2 o2 = Half<kBf16>::unpack(raw[4 * i + 2]), o3 = Half<kBf16>::unpack(raw[4 * i + 3]);
+                        x = make_uint4(Half<kBf16>::pack(s0.x + o0.x, s0.y + o0.y), Half<kBf16>::pack(s0.z + o1.x, s0.w + o1.y),
+                                       Half<kBf16>::pack(s1.x + o2.x, s1.y + o2.y), Half<kBf16>::pack(s1.z + o3.x, s1.w + o3.y));
+                    }
+                    if (row < live_tokens) *reinterpret_cast<uint4*>(y + (int64_t)row * p.ldy + n0 + c) = x;
                 }
             } else {
+                typename O::T* to = y + n0 + lane;
+                const bool in[2] = {n0 + lane < p.N, n0 + lane + 32 < p.N};
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int row = i >> 1, c = lane + 32 * (i & 1);
-                    if (row < live_tokens && n0 + c < p.N) store_y<kBf16>(p, token0 + row, n0 + c, out[row * M::kOutPitch + c] + __uint_as_float(raw[i]));
-                }
+                for (int row = 0; row < 16; ++row, to += p.ldy)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        if (in[c] && row < live_tokens) O::store(to + 32 * c, out[row * M::kOutPitch + lane + 32 * c] + __uint_as_float(raw[2 * row + c]));
             }
             __syncwarp();
         }
@@ -498,21 +540,35 @@ cudaError_t launch(Kernel kernel, const AdapterParams& p, int64_t units, int par
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
-template <bool kBf16, int kRT>
-cudaError_t launch_rank(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
-    if (few) return launch(adapters_few_kernel<kBf16, kRT>, p, units, parts, 0, st);
-    using M = Many<2 * kRT>;
-    static std::atomic<uint64_t> done{0};
-    const cudaError_t e = allow_smem(adapters_many_kernel<kBf16, 2 * kRT>, M::kSmemBytes, device, done);
-    if (e != cudaSuccess) return e;
-    return launch(adapters_many_kernel<kBf16, 2 * kRT>, p, units, parts, M::kSmemBytes, st);
+// Lets a kernel have clusters of 16, which not every GPU can: asked once per device, as allow_smem is.
+template <class Kernel>
+cudaError_t allow_large_cluster(Kernel kernel, int device, std::atomic<uint64_t>& done) {
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
-template <bool kBf16>
+template <bool kBf16, bool kF32, int kRT>
+cudaError_t launch_rank(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
+    static std::atomic<uint64_t> done_few{0}, done_many{0}, done{0};
+    if (parts > 8) {
+        const cudaError_t e = few ? allow_large_cluster(adapters_few_kernel<kBf16, kF32, kRT>, device, done_few)
+                                  : allow_large_cluster(adapters_many_kernel<kBf16, kF32, 2 * kRT>, device, done_many);
+        if (e != cudaSuccess) return e;
+    }
+    if (few) return launch(adapters_few_kernel<kBf16, kF32, kRT>, p, units, parts, 0, st);
+    using M = Many<2 * kRT>;
+    const cudaError_t e = allow_smem(adapters_many_kernel<kBf16, kF32, 2 * kRT>, M::kSmemBytes, device, done);
+    if (e != cudaSuccess) return e;
+    return launch(adapters_many_kernel<kBf16, kF32, 2 * kRT>, p, units, parts, M::kSmemBytes, st);
+}
+template <bool kBf16, bool kF32>
 cudaError_t launch_type(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
-    return p.rank <= 16   ? launch_rank<kBf16, 1>(p, few, units, parts, device, st)
-           : p.rank <= 32 ? launch_rank<kBf16, 2>(p, few, units, parts, device, st)
-           : p.rank <= 64 ? launch_rank<kBf16, 4>(p, few, units, parts, device, st)
-                          : launch_rank<kBf16, 8>(p, few, units, parts, device, st);
+    return p.rank <= 16   ? launch_rank<kBf16, kF32, 1>(p, few, units, parts, device, st)
+           : p.rank <= 32 ? launch_rank<kBf16, kF32, 2>(p, few, units, parts, device, st)
+           : p.rank <= 64 ? launch_rank<kBf16, kF32, 4>(p, few, units, parts, device, st)
+                          : launch_rank<kBf16, kF32, 8>(p, few, units, parts, device, st);
 }
 
 }  // namespace
@@ -538,16 +594,20 @@ extern "C" awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* 
     AdapterParams p = {};
     p.a = L->a_dev, p.b = L->b_dev, p.x = x_dev, p.base = base_dev, p.y = y_dev, p.scale = L->scale_dev;
     p.q_start = q_start_dev, p.adapter = adapter_dev, p.ldx = ldx, p.ldb = ldb, p.ldy = ldy, p.n_adapters = L->n_adapters;
-    p.T = (int)T, p.B = (int)B, p.N = (int)L->N, p.K = (int)L->K, p.rank = (int)L->rank, p.y_f32 = y_type == AWE_F32;
+    p.T = (int)T, p.B = (int)B, p.N = (int)L->N, p.K = (int)L->K, p.rank = (int)L->rank;
     p.vec = (uintptr_t)base_dev % 16 == 0 && (uintptr_t)y_dev % 16 == 0 && (!base_dev || ldb * out % 16 == 0) && ldy * out % 16 == 0;
     const bool few = T <= kFew * B;
     const int64_t units = T / (few ? kFew : kMany) + B;
     if (units > INT32_MAX / kMostCluster) return AWE_ERR_UNSUPPORTED;
-    // As large a cluster as leaves every SM two blocks, and every warp a step of k.
+    // The largest cluster with which all blocks are resident at once, and every warp has a step of k.
+    const int64_t live = std::min(units, T);  // units that are not empty, at most
+    const int resident = h->sm_count * (few ? (L->rank <= 16 ? 3 : 2) : (L->rank <= 64 ? 2 : 1));
     int parts = 1;
-    while (parts < kMostCluster && units * parts * 2 <= 4 * h->sm_count && (L->K + 31) / 32 >= 2 * kWarps * parts) parts *= 2;
-    const cudaError_t e = L->type == AWE_BF16 ? launch_type<true>(p, few, units, parts, h->device, (cudaStream_t)stream)
-                                              : launch_type<false>(p, few, units, parts, h->device, (cudaStream_t)stream);
+    while (parts < (few ? kMostCluster : 8) && live * parts * 2 <= resident && (L->K + 31) / 32 >= 2 * kWarps * parts) parts *= 2;
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool f32 = y_type == AWE_F32;
+    const cudaError_t e = L->type == AWE_BF16 ? (f32 ? launch_type<true, true>(p, few, units, parts, h->device, st) : launch_type<true, false>(p, few, units, parts, h->device, st))
+                                              : (f32 ? launch_type<false, true>(p, few, units, parts, h->device, st) : launch_type<false, false>(p, few, units, parts, h->device, st));
     if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;

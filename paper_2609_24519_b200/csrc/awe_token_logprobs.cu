@@ -131,6 +131,7 @@ struct Shared {
     Entry list[kWarps][32];  // also the gathered elements, one behind the other
     float maxima[kWarps][32];
     int gathered;
+    int most[kWarps];
     Sums block_sums;
     Entry block_list[32];
     int bound;  // least of a full list's best top_k, as an ordered whole number
@@ -210,59 +211,80 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         add(P::single(one), 1);
     });
 
+    // ---- sums against the block's maximum, as whole numbers in order (NaN above all)
+    const int warp_most = __reduce_max_sync(~0u, own.m == own.m ? ordered(own.m) : 0x7FFFFFFF);
+    if (lane == 0) sh.most[warp] = warp_most;
+    if (tid == 0) sh.gathered = 0;
+    __syncthreads();
+    int most_of_block = sh.most[0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) most_of_block = max(most_of_block, sh.most[i]);
+    const float thread_most = own.m == own.m ? own.m : -INFINITY;  // of a thread with a NaN it is not known
+    const bool looks_again = own.m != own.m;
+    raise(own, from_ordered(most_of_block), c);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) own.s0 += __shfl_xor_sync(~0u, own.s0, d), own.s1 += __shfl_xor_sync(~0u, own.s1, d);
+    if (lane == 0) sh.sums[warp] = own;
+
     if constexpr (kTop) {
-        // ---- the bound: the top_k-th largest of the thread maxima (of threads without a NaN, whose maximum is not known)
-        float m = own.m == own.m ? own.m : -INFINITY;
+        // ---- the bound: the top_k-th largest of the thread maxima
+        float m = thread_most;
+        if (p.top > 1) {
 #pragma unroll
-        for (int k = 2; k <= 32; k <<= 1)
+            for (int k = 2; k <= 32; k <<= 1)
 #pragma unroll
-            for (int d = k >> 1; d > 0; d >>= 1) {
-                const float o = __shfl_xor_sync(~0u, m, d);
-                m = ((lane & d) == 0) == ((lane & k) == 0) ? fmaxf(m, o) : fminf(m, o);
-            }
-        sh.maxima[warp][lane] = m;
-        if (tid == 0) sh.gathered = 0;
-        __syncthreads();
-        for (int step = 1; step < kWarps; step <<= 1) {
-            if (warp % (2 * step) == 0) {
-                m = fmaxf(m, sh.maxima[warp + step][31 - lane]);
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) {
+                for (int d = k >> 1; d > 0; d >>= 1) {
                     const float o = __shfl_xor_sync(~0u, m, d);
-                    m = lane & d ? fminf(m, o) : fmaxf(m, o);
+                    m = ((lane & d) == 0) == ((lane & k) == 0) ? fmaxf(m, o) : fminf(m, o);
                 }
-                sh.maxima[warp][lane] = m;
-            }
+            sh.maxima[warp][lane] = m;
             __syncthreads();
+            for (int step = 1; step < kWarps; step <<= 1) {
+                if (warp % (2 * step) == 0) {
+                    m = fmaxf(m, sh.maxima[warp + step][31 - lane]);
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) {
+                        const float o = __shfl_xor_sync(~0u, m, d);
+                        m = lane & d ? fminf(m, o) : fmaxf(m, o);
+                    }
+                    sh.maxima[warp][lane] = m;
+                }
+                __syncthreads();
+            }
         }
-        float bound = sh.maxima[0][p.top - 1];
+        // of one alternative it is the block's maximum, of a row with a NaN anything that is reached
+        float bound = p.top > 1 ? sh.maxima[0][p.top - 1] : (most_of_block == 0x7FFFFFFF ? -INFINITY : from_ordered(most_of_block));
         // ---- what reaches it
         auto gather = [&](float logit, int id) {
             if (!(logit >= bound)) return;
             const int at = atomicAdd(&sh.gathered, 1);
             if (at < kRoom) sh.list[at >> 5][at & 31] = {logit, id};
         };
-        if (!(own.m < bound)) {
-            for (int i = begin + tid; i < end; i += kThreads) {
+        // a thread's pieces are looked at by its whole warp, one each
+        for (unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound); ask; ask &= ask - 1) {
+            const int first = begin + 32 * warp + __ffs(ask) - 1;
+            for (int i = first + kThreads * lane; i < end; i += kThreads * 32) {
                 const uint4 w = __ldg(from + i);
                 if (P::largest(w) < bound) continue;
 #pragma unroll
                 for (int e = 0; e < P::kCount; ++e) gather(P::at(w, e), head + i * P::kCount + e);
             }
-            at_ends(gather);
         }
+        at_ends(gather);
         __syncthreads();
         const int gathered = sh.gathered;
         one_list = gathered <= 32;
         if (gathered <= kRoom) {
-            best = 32 * warp + lane < gathered ? sh.list[warp][lane] : Entry{-INFINITY, kNoToken};
+            if (32 * warp < gathered) {
+                if (32 * warp + lane < gathered) best = sh.list[warp][lane];
 #pragma unroll
-            for (int k = 2; k <= 32; k <<= 1)
+                for (int k = 2; k <= 32; k <<= 1)
 #pragma unroll
-                for (int d = k >> 1; d > 0; d >>= 1) {
-                    const Entry o = {__shfl_xor_sync(~0u, best.x, d), __shfl_xor_sync(~0u, best.id, d)};
-                    if (before(o, best) == (((lane & d) == 0) == ((lane & k) == 0))) best = o;
-                }
+                    for (int d = k >> 1; d > 0; d >>= 1) {
+                        const Entry o = {__shfl_xor_sync(~0u, best.x, d), __shfl_xor_sync(~0u, best.id, d)};
+                        if (before(o, best) == (((lane & d) == 0) == ((lane & k) == 0))) best = o;
+                    }
+            }
         } else {
             // Too many: every warp inserts what it finds among its elements into a list of its own.
             auto look = [&](float logit, int id, bool live) {
@@ -298,13 +320,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         sh.list[warp][lane] = best;
     }
 
-    // ---- the warp, the block, the cluster
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const Sums o = {__shfl_xor_sync(~0u, own.m, d), __shfl_xor_sync(~0u, own.s0, d), __shfl_xor_sync(~0u, own.s1, d)};
-        own = lane & d ? join_sums(o, own, c) : join_sums(own, o, c);  // the same order on both sides
-    }
-    if (lane == 0) sh.sums[warp] = own;
+    // ---- the block, the cluster
     __syncthreads();
     auto join_all = [&](int n, auto list_of) {  // lists list_of(0 .. n - 1), n a power of two: into the first
         for (int step = 1; step < n; step <<= 1) {
@@ -317,7 +333,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
     };
     if (kTop && !one_list) join_all(kWarps, [&](int i) { return sh.list[i]; });
     if (tid == 0) {
-        for (int i = 1; i < kWarps; ++i) own = join_sums(own, sh.sums[i], c);
+        for (int i = 1; i < kWarps; ++i) own.s0 += sh.sums[i].s0, own.s1 += sh.sums[i].s1;
         sh.block_sums = own;
     }
     if (parts > 1) {
