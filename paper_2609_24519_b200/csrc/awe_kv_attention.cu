@@ -28,6 +28,8 @@ namespace {
 using namespace serve;
 using namespace attn_few;
 
+constexpr int kStepTokens = 16 * kWarps;
+
 template <int kD, int kNT>
 struct Config {
     static constexpr int kRows = 8 * kNT;
@@ -58,11 +60,11 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
 
     grid_wait();
     Mine mine;
-    if (!find_steps<kRows>(p, search, mine)) return;
+    if (!find_steps<kRows, kStepTokens>(p, search, mine)) return;
     const int64_t begin = mine.begin, end = mine.end;
     int b = mine.b;
     int64_t at = mine.at;
-    Request r = request_of<kRows>(p, b);
+    Request r = request_of<kRows, kStepTokens>(p, b);
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * C::kStages * C::kStageBytes;
     float* join_vec = reinterpret_cast<float*>(smem);  // in the ring's place once it is empty
     float4* join_stat = reinterpret_cast<float4*>(join_vec + kWarps * kRows * C::kVecPitch);
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     for (int64_t pos = begin; pos < end;) {
         while (pos >= at + (p.whole ? r.units : (int64_t)r.units * r.steps)) {
             at += p.whole ? r.units : (int64_t)r.units * r.steps;
-            r = request_of<kRows>(p, ++b);
+            r = request_of<kRows, kStepTokens>(p, ++b);
         }
         const int unit = p.whole ? (int)(pos - at) : (int)((pos - at) / r.steps), step0 = p.whole ? 0 : (int)((pos - at) % r.steps);
         const int step1 = p.whole ? r.steps : (int)min((int64_t)r.steps, step0 + end - pos);
@@ -102,7 +104,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
                 raw[4 * c][0] = lo.x, raw[4 * c][1] = lo.y, raw[4 * c + 1][0] = lo.z, raw[4 * c + 1][1] = lo.w;
                 raw[4 * c + 2][0] = hi.x, raw[4 * c + 2][1] = hi.y, raw[4 * c + 3][0] = hi.z, raw[4 * c + 3][1] = hi.w;
             }
-            query_to_fp16<kBf16>(raw, factor);
+            query_to_fp16<kBf16, false>(raw, factor);
 #pragma unroll
             for (int i = 0; i < kSteps16; ++i) qf[nt][i][0] = raw[i][0], qf[nt][i][1] = raw[i][1];
             int lo_tok, hi_tok;
@@ -331,6 +333,67 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
     }
 }
 
+// Joins the parts of the units that were cut: one warp per (token, query head).
+template <int kD, int kNT, bool kBf16>
+__global__ void __launch_bounds__(kThreads) kv_attention_join_kernel(const AttnParams p) {
+    constexpr int kRows = 8 * kNT;
+    using T16 = typename Half<kBf16>::type;
+    const int lane = threadIdx.x & 31, q_heads = p.heads * p.group;
+    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    grid_wait();
+    if (item >= p.T * q_heads) return;
+    const int token = (int)(item / q_heads), qh = (int)(item % q_heads);
+    // the request of the token: last b with q_start[b] <= token
+    int b = 0;
+    for (int n = p.B; n > 1;) {
+        const int half = n >> 1;
+        if (p.q_start[b + half] <= token) b += half;
+        n -= half;
+    }
+    const Request r = request_of<kRows, kStepTokens>(p, b);
+    if (token < r.q0 || token >= r.q0 + r.n) return;
+    const int64_t total = p.unit_steps[p.B];
+    const int row_all = (token - r.q0) * p.group + qh % p.group, row = row_all % kRows;
+    const int unit = row_all / kRows * p.heads + qh / p.group;
+    const int64_t w0 = p.unit_steps[b] + (int64_t)unit * r.steps, w1 = w0 + r.steps;
+    const Deal deal(total, p.blocks);
+    const int first = deal.block_of(w0), last = deal.block_of(w1 - 1);
+    if (first == last) return;  // one block had all of it
+    float m = -INFINITY, sum = 0.0f, sum_lse = 0.0f;
+    float4 x[kD / 128 + (kD < 128)];
+#pragma unroll
+    for (auto& v : x) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = first; i <= last; ++i) {
+        const int64_t part = ((int64_t)2 * i + (i == first)) * kRows + row;  // the first part is the one that begins the unit
+        const float4 st = p.part_stat[part];
+        const float m_new = fmaxf(m, st.x);
+        const float a = m == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_approx(m - m_new);
+        const float c = st.x == -INFINITY ? (st.y == 0.0f ? 0.0f : 1.0f) : exp2_approx(st.x - m_new);
+        sum = fmaf(sum, a, st.y * c);
+        sum_lse = fmaf(sum_lse, a, st.z * c);
+        m = m_new;
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof(x) / sizeof(x[0])); ++k) {
+            const int d = 4 * lane + 128 * k;
+            if (d < kD) {
+                const float4 y = *reinterpret_cast<const float4*>(p.part_vec + part * kD + d);
+                x[k].x = fmaf(x[k].x, a, y.x * c), x[k].y = fmaf(x[k].y, a, y.y * c);
+                x[k].z = fmaf(x[k].z, a, y.z * c), x[k].w = fmaf(x[k].w, a, y.w * c);
+            }
+        }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T16* dst = reinterpret_cast<T16*>(p.out) + (int64_t)token * p.ldo + (int64_t)qh * kD;
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(x) / sizeof(x[0])); ++k) {
+        const int d = 4 * lane + 128 * k;
+        if (d < kD)
+            *reinterpret_cast<uint2*>(dst + d) =
+                make_uint2(Half<kBf16>::pack(x[k].x * inv, x[k].y * inv), Half<kBf16>::pack(x[k].z * inv, x[k].w * inv));
+    }
+    if (lane == 0 && p.lse) p.lse[(int64_t)token * q_heads + qh] = sum_lse == 0.0f ? -INFINITY : (m + log2f(sum_lse)) * 0.69314718056f;
+}
+
 // tcgen05 pays from about 64 query rows per request and head on, where the work fills its units of 256 rows x 128
 // tokens.  us of the kernel for few rows / on tcgen05, 8 heads of 128: one request of 4,096 tokens, 64 rows 28 / 28, 128 rows 40 / 31,
 // 1,024 rows 177 / 65; of 512 tokens, 512 rows 25 / 29, 1,024 rows 43 / 32; 16 requests of 16,384 tokens, 16 rows 186 / 334, 64 rows
@@ -363,7 +426,9 @@ cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
     cudaError_t e = allow_smem(kv_attention_kernel<kD, kNT, kBf16>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
-    return p.whole ? cudaSuccess : launch_join<kD, kNT, kBf16>(p, st);
+    if (p.whole) return cudaSuccess;
+    const int64_t items = p.T * p.heads * p.group;
+    return launch_early(kv_attention_join_kernel<kD, kNT, kBf16>, dim3((unsigned)((items + kWarps - 1) / kWarps)), kThreads, 0, st, p);
 }
 
 }  // namespace
@@ -427,7 +492,7 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, false, workspace_dev, (cudaStream_t)stream);
     const int nt = row_tiles(T, B, p.group, cache->head_dim);
-    place_few(p, blocks_of(h->sm_count, cache->head_dim, nt), nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);
+    place_few(p, kStepTokens, blocks_of(h->sm_count, cache->head_dim, nt), nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);
     auto run = [&](auto dim, auto tiles) {
         constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
         return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)

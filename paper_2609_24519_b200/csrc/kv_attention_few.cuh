@@ -1,5 +1,5 @@
 // What the kernels for few query rows share, over the cache of 8 bits (awe_kv_attention.cu) and of 4 (awe_kv4_attention.cu): how the
-// steps are dealt out, which tokens rows see, how the warps of a block and the parts of a unit are joined.
+// steps are dealt out, which tokens rows see, how the warps of a block are joined.
 #pragma once
 #include <algorithm>
 
@@ -12,15 +12,14 @@ using namespace serve;
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStepTokens = 16 * kWarps;
 constexpr int kWholeTokens = 256;
 constexpr int64_t kWholeScans = 1 << 19;
 
-// The steps of one request: tokens [lo, hi) in steps of kStepTokens, for each of `units` units.
+// The steps of one request: tokens [lo, hi) in steps of kStepTokens (a tile for each warp), for each of `units` units.
 struct Request {
     int q0, n, ctx, lo, steps, units;
 };
-template <int kRows>
+template <int kRows, int kStepTokens>
 __device__ __forceinline__ Request request_of(const AttnParams& p, int b) {
     Request r;
     r.q0 = min(max(p.q_start[b], 0), (int)p.T);
@@ -45,7 +44,7 @@ struct Mine {
     int64_t begin, end, at;
     int b;
 };
-template <int kRows>
+template <int kRows, int kStepTokens>
 __device__ __forceinline__ bool find_steps(const AttnParams& p, Search& sh, Mine& mine_out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int64_t total = 0;
@@ -56,7 +55,7 @@ __device__ __forceinline__ bool find_steps(const AttnParams& p, Search& sh, Mine
             const int b = b0 + tid;
             int64_t w = 0;
             if (b < p.B) {
-                const Request r = request_of<kRows>(p, b);
+                const Request r = request_of<kRows, kStepTokens>(p, b);
                 w = p.whole ? r.units : (int64_t)r.units * r.steps;
             }
             int64_t inc = w;
@@ -93,17 +92,17 @@ __device__ __forceinline__ bool find_steps(const AttnParams& p, Search& sh, Mine
     return true;
 }
 
-// A query row's 32-bit words in FP16: BF16 ones are scaled by a power of two (query_exponent), which `factor` takes back.  The
-// row lies in the four threads of a lane group.
-template <bool kBf16, int kWords>
+// A query row's 32-bit words in FP16: BF16 ones, and if kScaled all, are scaled by a power of two (query_exponent), which `factor` takes
+// back.  The row lies in the four threads of a lane group.
+template <bool kBf16, bool kScaled, int kWords>
 __device__ __forceinline__ void query_to_fp16(uint32_t (&raw)[kWords][2], float& factor) {
-    if constexpr (kBf16) {
+    if constexpr (kBf16 || kScaled) {
         float m = 0.0f;
 #pragma unroll
         for (int i = 0; i < kWords; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float2 f = Half<true>::unpack(raw[i][j]);
+                const float2 f = Half<kBf16>::unpack(raw[i][j]);
                 m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
             }
         m = fmaxf(m, __shfl_xor_sync(~0u, m, 1));
@@ -115,7 +114,7 @@ __device__ __forceinline__ void query_to_fp16(uint32_t (&raw)[kWords][2], float&
         for (int i = 0; i < kWords; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float2 f = Half<true>::unpack(raw[i][j]);
+                const float2 f = Half<kBf16>::unpack(raw[i][j]);
                 raw[i][j] = Half<false>::pack(f.x * down, f.y * down);
             }
     }
@@ -201,67 +200,6 @@ __device__ __forceinline__ void finish_unit(const AttnParams& p, const Request& 
     }
 }
 
-// Joins the parts of the units that were cut: one warp per (token, query head).
-template <int kD, int kNT, bool kBf16>
-__global__ void __launch_bounds__(kThreads) kv_attention_join_kernel(const AttnParams p) {
-    constexpr int kRows = 8 * kNT;
-    using T16 = typename Half<kBf16>::type;
-    const int lane = threadIdx.x & 31, q_heads = p.heads * p.group;
-    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    grid_wait();
-    if (item >= p.T * q_heads) return;
-    const int token = (int)(item / q_heads), qh = (int)(item % q_heads);
-    // the request of the token: last b with q_start[b] <= token
-    int b = 0;
-    for (int n = p.B; n > 1;) {
-        const int half = n >> 1;
-        if (p.q_start[b + half] <= token) b += half;
-        n -= half;
-    }
-    const Request r = request_of<kRows>(p, b);
-    if (token < r.q0 || token >= r.q0 + r.n) return;
-    const int64_t total = p.unit_steps[p.B];
-    const int row_all = (token - r.q0) * p.group + qh % p.group, row = row_all % kRows;
-    const int unit = row_all / kRows * p.heads + qh / p.group;
-    const int64_t w0 = p.unit_steps[b] + (int64_t)unit * r.steps, w1 = w0 + r.steps;
-    const Deal deal(total, p.blocks);
-    const int first = deal.block_of(w0), last = deal.block_of(w1 - 1);
-    if (first == last) return;  // one block had all of it
-    float m = -INFINITY, sum = 0.0f, sum_lse = 0.0f;
-    float4 x[kD / 128 + (kD < 128)];
-#pragma unroll
-    for (auto& v : x) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = first; i <= last; ++i) {
-        const int64_t part = ((int64_t)2 * i + (i == first)) * kRows + row;  // the first part is the one that begins the unit
-        const float4 st = p.part_stat[part];
-        const float m_new = fmaxf(m, st.x);
-        const float a = m == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_approx(m - m_new);
-        const float c = st.x == -INFINITY ? (st.y == 0.0f ? 0.0f : 1.0f) : exp2_approx(st.x - m_new);
-        sum = fmaf(sum, a, st.y * c);
-        sum_lse = fmaf(sum_lse, a, st.z * c);
-        m = m_new;
-#pragma unroll
-        for (int k = 0; k < (int)(sizeof(x) / sizeof(x[0])); ++k) {
-            const int d = 4 * lane + 128 * k;
-            if (d < kD) {
-                const float4 y = *reinterpret_cast<const float4*>(p.part_vec + part * kD + d);
-                x[k].x = fmaf(x[k].x, a, y.x * c), x[k].y = fmaf(x[k].y, a, y.y * c);
-                x[k].z = fmaf(x[k].z, a, y.z * c), x[k].w = fmaf(x[k].w, a, y.w * c);
-            }
-        }
-    }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T16* dst = reinterpret_cast<T16*>(p.out) + (int64_t)token * p.ldo + (int64_t)qh * kD;
-#pragma unroll
-    for (int k = 0; k < (int)(sizeof(x) / sizeof(x[0])); ++k) {
-        const int d = 4 * lane + 128 * k;
-        if (d < kD)
-            *reinterpret_cast<uint2*>(dst + d) =
-                make_uint2(Half<kBf16>::pack(x[k].x * inv, x[k].y * inv), Half<kBf16>::pack(x[k].z * inv, x[k].w * inv));
-    }
-    if (lane == 0 && p.lse) p.lse[(int64_t)token * q_heads + qh] = sum_lse == 0.0f ? -INFINITY : (m + log2f(sum_lse)) * 0.69314718056f;
-}
-
 // Query rows a unit holds: 16 where a request has more than 8 on average (their cache bytes are then read once),
 // else 8; head dimension 256 leaves no registers for 16.
 inline int row_tiles(int64_t T, int64_t B, int64_t group, int64_t head_dim) {
@@ -279,18 +217,12 @@ inline Workspace workspace_of(int blocks, int rows, int64_t head_dim, int64_t B)
     return w;
 }
 
-template <int kD, int kNT, bool kBf16>
-cudaError_t launch_join(const AttnParams& p, cudaStream_t st) {
-    const int64_t items = p.T * p.heads * p.group;
-    return launch_early(kv_attention_join_kernel<kD, kNT, kBf16>, dim3((unsigned)((items + kWarps - 1) / kWarps)), kThreads, 0, st, p);
-}
-
 // Blocks of the launch and their places in the workspace.  Short contexts: a block per unit and no second launch.  Each block scans
 // all requests, so it pays while the units times the requests are few: up to 256 tokens for one query, 8 heads of 4 queries each, us
 // whole / in parts with the join (8 bits): 1 request 7.0 / 7.6, 64 16.2 / 17.6, 128 25.2 / 26.6, 256 50 / 47, 2,048 902 / 337; 1 head of
 // 8: 128 7.6 / 11.1, 512 20.7 / 22.3, 1,024 47 / 38.
-inline void place_few(AttnParams& p, int blocks, int nt, int64_t head_dim, int64_t tokens, void* workspace_dev) {
-    if (p.window > 0) tokens = std::min(tokens, p.window + p.T / p.B + kStepTokens);
+inline void place_few(AttnParams& p, int step_tokens, int blocks, int nt, int64_t head_dim, int64_t tokens, void* workspace_dev) {
+    if (p.window > 0) tokens = std::min(tokens, p.window + p.T / p.B + step_tokens);
     const int64_t units = (p.T * p.group / (8 * nt) + p.B) * p.heads;
     p.whole = tokens <= kWholeTokens && units * p.B <= kWholeScans;
     const Workspace w = workspace_of(blocks, 8 * nt, head_dim, p.B);
