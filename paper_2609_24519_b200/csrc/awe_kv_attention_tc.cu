@@ -37,9 +37,11 @@ using namespace serve;
 
 constexpr int kRows = 256;      // query rows of a unit
 constexpr int kStep = 128;      // tokens of a step
-constexpr int kSoftWarps = 8, kUnpackWarps = 4;
-constexpr int kMultiplier = kSoftWarps + kUnpackWarps;
-constexpr int kThreads = 32 * (kMultiplier + 1);
+constexpr int kSoftWarps = 8;
+template <bool kFour>
+struct Warps {
+    static constexpr int kUnpack = 4, kMultiplier = kSoftWarps + kUnpack, kThreads = 32 * (kMultiplier + 1);
+};
 constexpr int kTmemCols = 512;
 constexpr int kPlanThreads = 1024;
 
@@ -210,7 +212,8 @@ __device__ __forceinline__ void add_unvalued(Shared* sh, uint32_t groups, int sl
 }
 
 template <int kD, bool kBf16, bool kFour>
-__global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
+__global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
+    constexpr int kUnpackWarps = Warps<kFour>::kUnpack, kMultiplier = Warps<kFour>::kMultiplier;
     using C = Config<kD>;
     using T16 = typename Half<kBf16>::type;
     const AttnParams& p = tp.a;
@@ -320,8 +323,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             });
         }
     } else if (kFour && warp >= kSoftWarps) {  // ---- unpack keys and values of 4 bits
-        constexpr int kPieces = kD / 32;          // 16-byte pieces per token, and passes per step
-        constexpr int kPassRows = 128 / kPieces;  // tokens per pass
+        constexpr int kPieces = kD / 32;  // 16-byte pieces per token
+        constexpr int kPassRows = 32 * kUnpackWarps / kPieces, kPasses = (kStep + kPassRows - 1) / kPassRows;  // tokens per pass, the last not whole
         const int thread = tid - 32 * kSoftWarps, c = thread % kPieces, r = thread / kPieces;
         uint32_t step = 0;
         for_parts([&](const Unit& u, int head, int s0, int s1) {
@@ -335,21 +338,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 }
                 return page;
             };
-            uint4 kr[kPieces], vr[kPieces];
-            uint32_t kw[kPieces], vw[kPieces];  // parameter words
-            uint32_t at[kPieces];               // rows of the pieces of a step; ~0 where there is nothing
+            uint4 kr[kPasses], vr[kPasses];
+            uint32_t kw[kPasses], vw[kPasses];  // parameter words
+            uint32_t at[kPasses];               // rows of the pieces of a step; ~0 where there is nothing
             auto places = [&](int pages, int j) {
                 const int place = (u.lo + j * kStep) & ((1 << p.page_log2) - 1);
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int row = i * kPassRows + r, page = __shfl_sync(~0u, pages, row >> 4);
+                for (int i = 0; i < kPasses; ++i) {
+                    const int row = i * kPassRows + r, page = __shfl_sync(~0u, pages, row >> 4);  // a lane behind the eighth has none
                     const uint32_t block = (uint32_t)(page * p.heads + head) << p.page_log2;
                     at[i] = page < 0 ? ~0u : block + ((place + row) & ((1 << p.page_log2) - 1));
                 }
             };
-            auto load = [&](const int8_t* pool, const uint16_t* params, uint4 (&x)[kPieces], uint32_t (&words)[kPieces]) {
+            auto load = [&](const int8_t* pool, const uint16_t* params, uint4 (&x)[kPasses], uint32_t (&words)[kPasses]) {
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
+                for (int i = 0; i < kPasses; ++i) {
                     x[i] = make_uint4(0, 0, 0, 0), words[i] = 0;  // become zeros, under a weight of 0
                     if (at[i] != ~0u) {
                         x[i] = __ldg(reinterpret_cast<const uint4*>(pool) + ((uint64_t)at[i] * kPieces + c));
@@ -357,11 +360,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                     }
                 }
             };
-            auto store = [&](uint32_t to, uint4 (&x)[kPieces], const uint32_t (&words)[kPieces]) {
+            auto store = [&](uint32_t to, uint4 (&x)[kPasses], const uint32_t (&words)[kPasses]) {
                 const int swap = kPieces == 4 ? c >> 1 : 0;  // the two blocks' threads write opposite halves first: no bank twice
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
+                for (int i = 0; i < kPasses; ++i) {
                     const int row = i * kPassRows + r;
+                    if (row >= kStep) break;
                     if (swap) x[i] = make_uint4(x[i].z, x[i].w, x[i].x, x[i].y);
                     const __half2 scale = __float2half2_rn(kv4_scale(words[i]));
                     const Kv4Zeros zero(__byte_perm(words[i], 0, 0x1010));
@@ -566,34 +570,113 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 ptx::tc_fence_after();
                 const uint32_t no_page = kFour ? sh->unvalued[step & 3] : 0;  // of 8 bits the constants hide such tokens
                 const bool cut = tok0 < all_lo || tok0 + kStep > all_hi || no_page;
-                // Both passes read S in pieces of 32 tokens, the next on its way meanwhile; 16 tokens share their scales.
-                auto for_pieces = [&](auto f) {
-                    uint32_t v[2][32];
-                    ptx::tmem_ld_32x32(s_at[t] + lanes, v[0]);
+                auto rescale = [&](float shrink) {  // of O, once the products of the step before are in it
+                    if (!__all_sync(~0u, wait(sh->o_done[t], (done - 1) & 1, 38))) return false;
+                    ptx::tc_fence_after();
 #pragma unroll 1
-                    for (int g = 0; g < kStep / 16; g += 4) {
+                    for (int c = 0; c < kD; c += 32) {
+                        uint32_t o[32];
+                        ptx::tmem_ld_32x32(o_at[t] + lanes + c, o);
                         ptx::tmem_wait_ld();
-                        ptx::tmem_ld_32x32(s_at[t] + lanes + 16 * (g + 2), v[1]);
-                        f(g, v[0]);
-                        ptx::tmem_wait_ld();
-                        if (g + 4 < kStep / 16) ptx::tmem_ld_32x32(s_at[t] + lanes + 16 * (g + 4), v[0]);
-                        f(g + 2, v[1]);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                        ptx::tmem_st_32x32(o_at[t] + lanes + c, o);
                     }
+                    return true;
                 };
-                auto hide = [&](int g, uint32_t (&v)[32]) {  // what this row does not see
-                    const int lo = see_lo - tok0 - 16 * g, hi = see_hi - tok0 - 16 * g;
+                if constexpr (kFour) {
+                    // One pass: P against the reference so far, with the largest score beside it, half a step at a time.  Where a row's passes the
+                    // reference by too much (its first step, rarely a later one), the reference moves, by a whole number so that what there is of O
+                    // and P follows exactly, and the warp goes over the half once more, which P has not taken the place of yet.
+                    float part = 0.0f;
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t from = s_at[t] + lanes + 64 * half;
+                        bool again = true;
+#pragma unroll 1
+                        for (int pass = 0; again; ++pass) {
+                            const bool first = m_ref == -INFINITY;
+                            const float m = first ? 0.0f : m_ref;
+                            float top = -INFINITY, even = 0.0f, odd = 0.0f;
+                            uint32_t pk[32];
+                            auto weigh = [&](auto is_cut) {
+                                uint32_t v[2][16];
+                                ptx::tmem_ld_32x16(from, v[0]);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (e < lo || e >= hi || (kFour && (no_page >> (g + e / 16) & 1))) v[e] = 0xFF800000u;
-                };
-                auto factor = [&](const float4& k) { return factor_of(k.x, cq); };
-                float top = -INFINITY;  // the largest exponent: of each piece the largest score decides
-                for_pieces([&](int g, uint32_t (&v)[32]) {
-                    if (cut) hide(g, v);
-                    if constexpr (kFour) {
+                                for (int g = 0; g < 4; ++g) {
+                                    uint32_t(&w)[16] = v[g & 1];
+                                    ptx::tmem_wait_ld();
+                                    if (g < 3) ptx::tmem_ld_32x16(from + 16 * (g + 1), v[(g + 1) & 1]);
+                                    if constexpr (decltype(is_cut)::value) {  // what this row does not see
+                                        const int at = tok0 + 64 * half + 16 * g;
+                                        int lo = no_page >> (4 * half + g) & 1 ? 16 : see_lo - at, hi = see_hi - at;
+                                        // both change here as far as the compiler knows: else it compares them in front of the passes, for every step
+                                        asm volatile("" : "+r"(lo), "+r"(hi));
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(v[e]));
-                    } else {
+                                        for (int e = 0; e < 16; ++e)
+                                            if (e < lo || e >= hi) w[e] = 0xFF800000u;
+                                    }
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) {
+                                        const float a = __uint_as_float(w[2 * e]), b = __uint_as_float(w[2 * e + 1]);
+                                        top = fmaxf(fmaxf(top, a), b);
+                                        const float x = exp2_approx(fmaf(a, cq, -m)), y = exp2_approx(fmaf(b, cq, -m));
+                                        even += x, odd += y;
+                                        pk[8 * g + e] = Half<false>::pack(x, y);
+                                    }
+                                }
+                            };
+                            if (cut) weigh(std::true_type());
+                            else weigh(std::false_type());
+                            top *= cq;
+                            const bool grows = pass == 0 && top > (first ? -INFINITY : m_ref + kMostAbove);  // once: then top is 10 above it
+                            again = __any_sync(~0u, grows);
+                            if (again) {
+                                const float before = m_ref;
+                                if (grows) m_ref = first ? top - kBelow : m_ref + ceilf(top - kBelow - m_ref);
+                                const float shrink = first || !grows ? 1.0f : exp2_approx(before - m_ref);
+                                sum *= shrink, part *= shrink;
+                                if (j > s0 && __any_sync(~0u, shrink != 1.0f) && !rescale(shrink)) return false;
+                                if (half) {
+                                    uint32_t before_p[32];
+                                    ptx::tmem_ld_32x32(s_at[t] + lanes, before_p);
+                                    ptx::tmem_wait_ld();
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) before_p[e] = mul2(before_p[e], __float2half2_rn(shrink));
+                                    ptx::tmem_st_32x32(s_at[t] + lanes, before_p);
+                                }
+                            } else {
+                                part += even + odd;
+                                ptx::tmem_st_32x32(s_at[t] + lanes + 32 * half, pk);
+                            }
+                        }
+                    }
+                    sum += part;
+                } else {
+                    // Both passes read S in pieces of 32 tokens, the next on its way meanwhile; 16 tokens share their scales.
+                    auto for_pieces = [&](auto f) {
+                        uint32_t v[2][32];
+                        ptx::tmem_ld_32x32(s_at[t] + lanes, v[0]);
+#pragma unroll 1
+                        for (int g = 0; g < kStep / 16; g += 4) {
+                            ptx::tmem_wait_ld();
+                            ptx::tmem_ld_32x32(s_at[t] + lanes + 16 * (g + 2), v[1]);
+                            f(g, v[0]);
+                            ptx::tmem_wait_ld();
+                            if (g + 4 < kStep / 16) ptx::tmem_ld_32x32(s_at[t] + lanes + 16 * (g + 4), v[0]);
+                            f(g + 2, v[1]);
+                        }
+                    };
+                    auto hide = [&](int g, uint32_t (&v)[32]) {  // what this row does not see
+                        const int lo = see_lo - tok0 - 16 * g, hi = see_hi - tok0 - 16 * g;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (e < lo || e >= hi) v[e] = 0xFF800000u;
+                    };
+                    auto factor = [&](const float4& k) { return factor_of(k.x, cq); };
+                    float top = -INFINITY;  // the largest exponent: of each piece the largest score decides
+                    for_pieces([&](int g, uint32_t (&v)[32]) {
+                        if (cut) hide(g, v);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const float4 k = sh->constants[step & 3][g + h];
@@ -602,52 +685,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                             for (int e = 1; e < 16; ++e) m = fmaxf(m, __uint_as_float(v[16 * h + e]));
                             top = fmaxf(top, fmaf(m, factor(k), k.y));
                         }
+                    });
+                    const bool first = m_ref == -INFINITY;
+                    const bool grows = top > (first ? -INFINITY : m_ref + kMostAbove);
+                    const uint32_t unvalued = sh->unvalued[step & 3];
+                    if (__any_sync(~0u, grows || unvalued)) {  // one branch on the way of most steps: with two they take 0.6 % longer
+                        if (unvalued) add_unvalued(sh, unvalued, step & 3, s_at[t] + lanes, 128 * t + row, see_lo - tok0, see_hi - tok0, cq);
+                        const float before = m_ref;
+                        m_ref = fmaxf(m_ref, top - kBelow);
+                        const float shrink = first || m_ref == before ? 1.0f : exp2_approx(before - m_ref);
+                        sum *= shrink;
+                        if (j > s0 && __any_sync(~0u, shrink != 1.0f) && !rescale(shrink)) return false;
                     }
-                });
-                if constexpr (kFour) top *= cq;
-                const bool first = m_ref == -INFINITY;
-                const bool grows = top > (first ? -INFINITY : m_ref + kMostAbove);
-                const uint32_t unvalued = kFour ? 0 : sh->unvalued[step & 3];
-                if (__any_sync(~0u, grows || unvalued)) {  // one branch on the way of most steps: with two they take 0.6 % longer
-                    if (unvalued) add_unvalued(sh, unvalued, step & 3, s_at[t] + lanes, 128 * t + row, see_lo - tok0, see_hi - tok0, cq);
-                    const float before = m_ref;
-                    m_ref = fmaxf(m_ref, top - kBelow);
-                    const float shrink = first || m_ref == before ? 1.0f : exp2_approx(before - m_ref);
-                    sum *= shrink;
-                    if (j > s0 && __any_sync(~0u, shrink != 1.0f)) {  // O once the products of the step before are in it
-                        if (!__all_sync(~0u, wait(sh->o_done[t], (done - 1) & 1, 38))) return false;
-                        ptx::tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < kD; c += 32) {
-                            uint32_t o[32];
-                            ptx::tmem_ld_32x32(o_at[t] + lanes + c, o);
-                            ptx::tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                            ptx::tmem_st_32x32(o_at[t] + lanes + c, o);
-                        }
-                    }
-                }
-                // P, over the pieces of S that have been read, and its sum (8 bits: the sum of P / vs)
-                const float m = m_ref == -INFINITY ? 0.0f : m_ref;
-                float part = 0.0f;
-                for_pieces([&](int g, uint32_t (&v)[32]) {
-                    if (cut) hide(g, v);
-                    if constexpr (kFour) {
-                        float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t pk[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float x = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e]), cq, -m)), y = exp2_approx(fmaf(__uint_as_float(v[16 * h + 2 * e + 1]), cq, -m));
-                                s0 += x, s1 += y;
-                                pk[e] = Half<false>::pack(x, y);
-                            }
-                            ptx::tmem_st_32x8(s_at[t] + lanes + 8 * (g + h), pk);
-                        }
-                        part += s0 + s1;
-                    } else {
+                    // P, over the pieces of S that have been read, and the sum of P / vs
+                    const float m = m_ref == -INFINITY ? 0.0f : m_ref;
+                    float part = 0.0f;
+                    for_pieces([&](int g, uint32_t (&v)[32]) {
+                        if (cut) hide(g, v);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const float4 k = sh->constants[step & 3][g + h];
@@ -663,9 +717,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                             part = fmaf(s0 + s1, k.z, part);
                             ptx::tmem_st_32x8(s_at[t] + lanes + 8 * (g + h), pk);
                         }
-                    }
-                });
-                sum += part;
+                    });
+                    sum += part;
+                }
                 ptx::tmem_wait_st();
                 gemm::release(ptx::smem_u32(&sh->p_full[t]), lane, false);
             }
@@ -802,7 +856,7 @@ cudaError_t launch(const TcAttnParams& p, int device, cudaStream_t st) {
     cudaError_t e = allow_smem(kv_attention_tc_kernel<kD, kBf16, kFour>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_units_kernel, dim3(1), kPlanThreads, 0, st, p)) != cudaSuccess) return e;
-    if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16, kFour>, dim3(p.a.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
+    if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16, kFour>, dim3(p.a.blocks), Warps<kFour>::kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     const int64_t items = p.a.T * p.a.heads * p.a.group;
     return launch_early(kv_attention_tc_join_kernel<kD, kBf16>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
 }
