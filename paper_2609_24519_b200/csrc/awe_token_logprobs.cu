@@ -6,10 +6,11 @@
 // One pass: every thread keeps a maximum of its own and rescales its two sums when it grows.
 //
 // The most likely tokens.  The top_k-th largest of a block's 256 thread maxima is a bound that top_k elements reach, and few others do:
-// the threads whose maximum reaches it look at their elements again (from the cache) and gather those that do, some 22 for 20.  They are sorted,
-// 32 a warp, and lists are joined in pairs: of two lists in order, the larger of a[i] and b[31 - i] are the best 32, in an order that
-// five exchanges sort.  Where more are gathered than there is room for (many equal logits), all warps look at all elements again: each keeps its best so
-// far in order, one a lane, and inserts what reaches the bound, which its own list and the others' raise.
+// the threads whose maximum reaches it have their elements looked at again (in the cache) by their warp, which gathers those that do, some 22 for
+// 20; each of them finds its place by counting the ones before it.  Blocks' lists are joined in pairs: of two lists in order, the larger of a[i]
+// and b[31 - i] are the best 32, in an order that five exchanges sort.  Where more are gathered than there is room for (many equal logits), all
+// warps look at all elements again: each keeps its best so far in order, one a lane, and inserts what reaches the bound, which its own list and
+// the others' raise.  (A looser bound from each warp's maxima alone saves the joining of eight lists, but gathers more: 17.5 -> 23 us.)
 //
 // HBM bounds many rows; a single row is spread over a cluster of blocks that join in shared memory, which bounds it by latency.
 #include <cooperative_groups.h>
@@ -81,6 +82,13 @@ struct Piece {  // 16 bytes of logits
             return i & 1 ? f.y : f.x;
         }
     }
+    // The same of an element that is not known beforehand.
+    static __device__ __forceinline__ float pick(const uint4& w, int i) {
+        const int word = kType == AWE_F32 ? i : i >> 1;
+        const uint32_t low = word & 1 ? w.y : w.x, high = word & 1 ? w.w : w.z, x = word & 2 ? high : low;
+        if constexpr (kType == AWE_F32) return __uint_as_float(x);
+        else return Half<kType == AWE_BF16>::unpack(i & 1 ? x >> 16 : x).x;
+    }
     // Masked tokens alone, and a first element with nothing behind it.
     static __device__ __forceinline__ uint4 nothing() {
         constexpr uint32_t kMasked = kType == AWE_F32 ? 0xFF800000u : (kType == AWE_BF16 ? 0xFF80FF80u : 0xFC00FC00u);
@@ -125,12 +133,13 @@ __device__ __forceinline__ Sums join_sums(Sums a, Sums b, float c) {
     return {m, a.s0 + b.s0, a.s1 + b.s1};
 }
 
-constexpr int kRoom = 32 * kWarps;  // for gathered elements
+constexpr int kRoom = kThreads;  // for gathered elements
 struct Shared {
     Sums sums[kWarps];
-    Entry list[kWarps][32];  // also the gathered elements, one behind the other
-    float maxima[kWarps][32];
+    Entry list[kWarps][32];
+    Entry found[kRoom];  // gathered elements
     int gathered;
+    float maxima[kWarps][32];
     int most[kWarps];
     Sums block_sums;
     Entry block_list[32];
@@ -153,7 +162,10 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / parts;
     const float c = p.scale * 1.44269504088896f;
-    if (kTop && tid == 0) sh.bound = ordered(-INFINITY);
+    if constexpr (kTop) {
+        if (tid == 0) sh.bound = ordered(-INFINITY);
+        sh.found[tid] = {-INFINITY, kNoToken};
+    }
     __syncthreads();
     grid_wait();
     const T* x = reinterpret_cast<const T*>(p.logits) + row * p.ld;
@@ -172,7 +184,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
     }
 
     Sums own = {-INFINITY, 0.0f, 0.0f};
-    bool one_list = false;  // whether the first warp has all of the block's
+    bool one_list = false;  // whether every warp has all of the block's
     Entry best = {-INFINITY, kNoToken};  // this lane's of the warp's list
     auto add = [&](const uint4& w, int count) {
         const float m = own.m == -INFINITY ? 0.0f : own.m;
@@ -190,8 +202,8 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         if (rank == 0 && warp == 0 && lane < head) f(P::one(x + lane), lane);
         if (rank == parts - 1 && warp == kWarps - 1 && lane < p.V - tail_at) f(P::one(x + tail_at + lane), tail_at + lane);
     };
+    uint4 w[kPieces];
     for (int i0 = begin + tid; i0 < end; i0 += kThreads * kPieces) {
-        uint4 w[kPieces];
         float most = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kPieces; ++u) {
@@ -258,33 +270,54 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         auto gather = [&](float logit, int id) {
             if (!(logit >= bound)) return;
             const int at = atomicAdd(&sh.gathered, 1);
-            if (at < kRoom) sh.list[at >> 5][at & 31] = {logit, id};
+            if (at < kRoom) sh.found[at] = {logit, id};
         };
-        // a thread's pieces are looked at by its whole warp, one each
-        for (unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound); ask; ask &= ask - 1) {
-            const int first = begin + 32 * warp + __ffs(ask) - 1;
-            for (int i = first + kThreads * lane; i < end; i += kThreads * 32) {
-                const uint4 w = __ldg(from + i);
-                if (P::largest(w) < bound) continue;
+        // A thread's pieces are looked at by its whole warp, one each; of two threads they are on their way together.  (With four a single row
+        // takes 0.4 us less, but a block leaves less room for others: 2,048 rows of 50,257 take 52 us instead of 44.)
+        constexpr int kAhead = 2;
+        for (unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound); ask;) {
+            int first[kAhead];
 #pragma unroll
-                for (int e = 0; e < P::kCount; ++e) gather(P::at(w, e), head + i * P::kCount + e);
+            for (int k = 0; k < kAhead; ++k) first[k] = ask ? begin + 32 * warp + __ffs(ask) - 1 : end, ask &= ask - 1;
+#pragma unroll 1
+            for (int at = kThreads * lane; at < end - begin; at += kThreads * 32) {
+                uint4 w[kAhead];
+                unsigned hits[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) w[k] = first[k] + at < end ? __ldg(from + first[k] + at) : P::nothing();
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    hits[k] = 0;
+#pragma unroll
+                    for (int e = 0; e < P::kCount; ++e) hits[k] |= (unsigned)(P::at(w[k], e) >= bound) << e;
+                    if (first[k] + at >= end) hits[k] = 0;
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+#pragma unroll 1
+                    for (; hits[k]; hits[k] &= hits[k] - 1) {
+                        const int e = __ffs(hits[k]) - 1;
+                        gather(P::pick(w[k], e), head + (first[k] + at) * P::kCount + e);
+                    }
             }
         }
         at_ends(gather);
         __syncthreads();
         const int gathered = sh.gathered;
-        one_list = gathered <= 32;
-        if (gathered <= kRoom) {
-            if (32 * warp < gathered) {
-                if (32 * warp + lane < gathered) best = sh.list[warp][lane];
+        one_list = gathered <= kRoom;
+        if (one_list) {
+            if (tid < gathered) {
+                const Entry mine = sh.found[tid];
+                int place = 0;
+                for (int i = 0; i < gathered; i += 8)
 #pragma unroll
-                for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-                    for (int d = k >> 1; d > 0; d >>= 1) {
-                        const Entry o = {__shfl_xor_sync(~0u, best.x, d), __shfl_xor_sync(~0u, best.id, d)};
-                        if (before(o, best) == (((lane & d) == 0) == ((lane & k) == 0))) best = o;
-                    }
+                    for (int k = 0; k < 8; ++k) place += before(sh.found[i + k], mine);  // behind the last: nothing, which is before none
+                if (place < 32) sh.list[0][place] = mine;
+            } else if (tid < 32) {
+                sh.list[0][tid] = best;  // nothing
             }
+            __syncthreads();
+            best = sh.list[0][lane];
         } else {
             // Too many: every warp inserts what it finds among its elements into a list of its own.
             auto look = [&](float logit, int id, bool live) {
@@ -316,8 +349,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
                 look(live ? P::one(x + tail_at + lane) : 0.0f, tail_at + lane, live);
             }
         }
-        __syncthreads();
-        sh.list[warp][lane] = best;
+        if (!one_list) sh.list[warp][lane] = best;
     }
 
     // ---- the block, the cluster
@@ -340,8 +372,15 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         if (kTop && warp == 0) sh.block_list[lane] = best;
         cluster.sync();
         if (rank == 0) {
-            if (tid == 0)
-                for (int i = 1; i < parts; ++i) own = join_sums(own, *cluster.map_shared_rank(&sh.block_sums, i), c);
+            if (warp == 0) {  // a block's sums a lane
+                own = {-INFINITY, 0.0f, 0.0f};
+                if (lane < parts) own = *cluster.map_shared_rank(&sh.block_sums, lane);
+#pragma unroll
+                for (int d = kMostCluster / 2; d > 0; d >>= 1) {
+                    const Sums o = {__shfl_xor_sync(~0u, own.m, d), __shfl_xor_sync(~0u, own.s0, d), __shfl_xor_sync(~0u, own.s1, d)};
+                    own = lane & d ? join_sums(o, own, c) : join_sums(own, o, c);  // the same order on both sides
+                }
+            }
             if constexpr (kTop) {
                 if (warp < parts) best = cluster.map_shared_rank(&sh, warp)->block_list[lane];
                 sh.list[warp][lane] = best;
