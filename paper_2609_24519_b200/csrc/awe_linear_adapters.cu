@@ -606,8 +606,16 @@ extern "C" awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* 
     while (parts < (few ? kMostCluster : 8) && live * parts * 2 <= resident && (L->K + 31) / 32 >= 2 * kWarps * parts) parts *= 2;
     cudaStream_t st = (cudaStream_t)stream;
     const bool f32 = y_type == AWE_F32;
-    const cudaError_t e = L->type == AWE_BF16 ? (f32 ? launch_type<true, true>(p, few, units, parts, h->device, st) : launch_type<true, false>(p, few, units, parts, h->device, st))
-                                              : (f32 ? launch_type<false, true>(p, few, units, parts, h->device, st) : launch_type<false, false>(p, few, units, parts, h->device, st));
+    auto run = [&] {
+        return L->type == AWE_BF16 ? (f32 ? launch_type<true, true>(p, few, units, parts, h->device, st) : launch_type<true, false>(p, few, units, parts, h->device, st))
+                                   : (f32 ? launch_type<false, true>(p, few, units, parts, h->device, st) : launch_type<false, false>(p, few, units, parts, h->device, st));
+    };
+    cudaError_t e = run();
+    if (e != cudaSuccess && parts > 8) {  // a part of a GPU may have no room for clusters of 16
+        cudaGetLastError();
+        parts = 8;
+        e = run();
+    }
     if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;

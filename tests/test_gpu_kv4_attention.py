@@ -152,6 +152,15 @@ def test_long_contexts():
         check(s)
 
 
+@pytest.mark.parametrize("D,dtype", [(64, b.F16), (128, b.BF16), (256, b.F16)])
+def test_many_rows_whose_parts_are_joined(D, dtype):
+    """More rows than are joined by a block each."""
+    ctx = [1 + (997 * i) % 2500 for i in range(45)]
+    s = make([1] * 45, ctx, 32, 4, D, 16, dtype, seed=D)
+    assert call(s) == 2
+    check(s)
+
+
 @pytest.mark.parametrize("new,ctx", [([1, 1], [700, 64]), ([900, 40], [1000, 900])])
 def test_pages_that_do_not_exist(new, ctx):
     """Entries outside the pool hide their tokens; a request with no page at all sees nothing."""

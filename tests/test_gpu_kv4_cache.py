@@ -108,6 +108,27 @@ def test_append_and_read(T, Hq, H, D, page, rotary, interleaved, dtype):
     check(s)
 
 
+@pytest.mark.parametrize("D,H,rotary,interleaved", [(64, 3, 64, False), (128, 2, 32, True), (256, 1, 256, False)])
+def test_many_tokens_with_some_left_out(D, H, rotary, interleaved):
+    """So many that a block takes several tokens; their number is no multiple of that, and any of a block's may be left out."""
+    T = 2603
+    s = make(T, 5, H, D, 32, b.BF16, rotary, interleaved, seed=D)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    out = torch.rand(T, generator=g, device="cuda")
+    slots, positions = s["slots"].clone(), s["positions"].clone()
+    s["slots"][out < 0.2] = -1
+    s["positions"][(out > 0.1) & (out < 0.3)] = -1
+    append(s)
+    turned_rows = (out <= 0.1) | (out >= 0.3)
+    stored = turned_rows & (out >= 0.2)
+    q = s["q"].clone()
+    s["positions"], s["slots"] = positions, slots
+    want = turned(s, torch.float32)[0].to(torch.bfloat16).view(T, -1)
+    assert torch.equal(q[turned_rows], want[turned_rows]) and bool((q[~turned_rows] == 7.0).all())
+    s["q"] = want
+    check(s, stored)
+
+
 def test_far_positions():
     s = make(40, 2, 1, 128, 16, b.BF16, 128, n_positions=300000)
     s["positions"] += 299990 - s["positions"].max()

@@ -74,6 +74,15 @@ def test_lengths_of_many_kinds(lengths):
     check(s, call(s))
 
 
+def test_all_numbers_of_blocks_a_cluster():
+    """From one block for each of many requests to sixteen for one."""
+    for B in (1, 5, 20, 40, 100, 300):
+        s = make([1] * B, [i % 5 for i in range(B)], 8, 300, 4096, b.F16, b.F32, seed=B)
+        check(s, call(s))
+        s = make([12] * B, [i % 5 for i in range(B)], 8, 300, 4096, b.BF16, b.BF16, seed=B)
+        check(s, call(s))
+
+
 def test_long_sums_and_wide_results():
     for T in (1, 40):
         s = make([T], [2], 64, 8200, 8200, b.F16, b.F16, seed=T)
