@@ -10,6 +10,10 @@
 // u enters the second product as several 16-bit values, the rounded u, the rounded rest of it, and so on: two hold 22 bits in FP16 and 16 in
 // BF16, whose third (24 bits) is taken where y is FP32.
 //
+// One token, 8,192 x 8,192, rank 64: 7.5 us (a cluster of 16); 64 tokens with 48 adapters, 4,096 x 4,096, rank 16: 7.2 us (clusters of 4); 4,096
+// tokens of 8 requests, same sizes: 28 us for 101 MB = 3.6 TB/s.  Tried for many tokens without gain: 16 warps a block, tiles of 32 columns with the
+// next one's loads under way, results straight from the registers (27 to 30 us; unaligned rows 82 to 102 instead of 69).
+//
 // Units are numbered without a scan: request b's first is q_start[b] / kTokens + b, which leaves room for all of its units before
 // those of request b + 1.  Some numbers have no unit; their clusters end at once.
 #include <cooperative_groups.h>
