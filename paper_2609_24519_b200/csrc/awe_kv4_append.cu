@@ -318,6 +318,8 @@ extern "C" awe_status_t awe_kv4_append(awe_handle_t h, const awe_kv4_cache* cach
     const bool bf16 = type == AWE_BF16, pairs = rotary && rotary->interleaved;
     cudaStream_t st = (cudaStream_t)stream;
     // A block takes four tokens, whose rows are on their way together, where there are enough for every SM to have some blocks.
+    // One token a block and four, 32 + 2 x 8 heads of 128, us: 300 tokens 4.4 and 6.3, 600 6.2 and 7.5, 1,200 10.4 and 10.3, 2,400 20.1 and 19.9,
+    // 10,000 75.8 and 72.6.
     const bool many = T >= 16 * h->sm_count;
     auto run = [&](auto dim) {
         constexpr int kD = decltype(dim)::value;

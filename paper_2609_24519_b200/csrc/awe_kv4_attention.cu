@@ -504,12 +504,17 @@ cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
     if ((e = launch_early(kv4_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     if (p.whole) return cudaSuccess;
     // Few rows have many parts each (one token of 131,072: 74), which a block joins faster than a warp; of many rows most have one or two.
+    // Attention and its join, a warp and a block a row, us: 1 token over 131,072 (32 rows) 53.8 and 46.6, 8 over 16,000 (256) 48.0 and 47.4,
+    // 32 over 4,096 (1,024) 48.8 and 49.2, 64 over 4,096 (2,048) 82.5 and 85.5, 16 x 8 tokens over 4,096 (4,096) 88.7 and 95.5.
     const int64_t items = p.T * p.heads * p.group;
     if (items <= kSharedJoins) return launch_early(kv4_attention_join_kernel<kD, kNT, kWarps, kBf16>, dim3((unsigned)items), kThreads, 0, st, p);
     return launch_early(kv4_attention_join_kernel<kD, kNT, 1, kBf16>, dim3((unsigned)((items + kWarps - 1) / kWarps)), kThreads, 0, st, p);
 }
 
-// The kernel on tcgen05 pays from about 64 query rows per request and head on, as over the 8-bit cache.
+// The kernel on tcgen05 pays from about 64 query rows per request and head on, and 2^29 products.  32 heads over 8 of 128, few rows' kernel
+// and tcgen05's, us: 1 request of 16 tokens over 4,096 (64 rows a head) 23.1 and 26.5, of 32 31.6 and 29.6, of 256 147 and 63;
+// 128 over 512 (2^28 products) 23.4 and 27.4, 256 over 512 (2^29) 35.2 and 31.0; 16 requests of 4 tokens over 16,384 152 and 286, of 16
+// 528 and 296; 300 tokens over 2,000 with 4 heads over 1 27.3 and 29.2.
 bool use_tc(const awe_kv4_cache& cache, int64_t T, int64_t B, int64_t n_q_heads, int64_t group, int64_t tokens, int64_t window) {
     const int64_t head_dim = cache.head_dim;
     if (head_dim > 128 || T * group < 64 * B) return false;

@@ -600,7 +600,11 @@ extern "C" awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* 
     p.q_start = q_start_dev, p.adapter = adapter_dev, p.ldx = ldx, p.ldb = ldb, p.ldy = ldy, p.n_adapters = L->n_adapters;
     p.T = (int)T, p.B = (int)B, p.N = (int)L->N, p.K = (int)L->K, p.rank = (int)L->rank;
     p.vec = (uintptr_t)base_dev % 16 == 0 && (uintptr_t)y_dev % 16 == 0 && (!base_dev || ldb * out % 16 == 0) && ldy * out % 16 == 0;
-    const bool few = T <= kFew * B;
+    // Units of 8 tokens while they leave room for two blocks' clusters or hold no more than two tokens; then units of 32, which read an
+    // adapter less often.  4,096 x 4,096, rank 16, units of 8 and of 32 tokens, us: one request of 8 tokens 3.9 and 6.3, of 64 5.0 and 7.4, of
+    // 512 (65 units of 8) 8.0 and 9.8, of 1,024 (129) 17.1 and 10.9; 16 requests of 16 tokens 7.3 and 8.4, 32 of 16 (96) 10.1 and 9.6,
+    // 64 of 8 (128) 17.4 and 15.3, 128 of 4 16.2 and 15.5; 128 of 1 11.3 and 12.3, 256 of 1 19.3 and 20.7.
+    const bool few = 2 * (T / kFew + B) <= h->sm_count || T <= 2 * B;
     const int64_t units = T / (few ? kFew : kMany) + B;
     if (units > INT32_MAX / kMostCluster) return AWE_ERR_UNSUPPORTED;
     // The largest cluster with which all blocks are resident at once, and every warp has a step of k.

@@ -446,10 +446,17 @@ extern "C" awe_status_t awe_token_logprobs(awe_handle_t h, const void* logits_de
     if (!top_logprob_dev && !top_id_dev) top_k = 0;
     if (!logprob_dev && !entropy_dev && !lse_dev && !top_k) return AWE_OK;
     LogprobParams p = {logits_dev, tokens_dev, logprob_dev, entropy_dev, lse_dev, top_logprob_dev, top_id_dev, ld, scale, (int)V, (int)top_k};
-    // A row goes to a cluster while the rows alone leave SMs without work and a block would still have a batch for every thread.
-    const int64_t batch = (int64_t)kThreads * kPieces * (type == AWE_F32 ? 4 : 8);
+    // A row goes to a cluster while its blocks keep enough of it: twice as much where lists have to be joined, and twice as much again when
+    // there are blocks for half of the SMs, and for two on each.  BF16, 20 alternatives, 1, 2, 4 and 8 blocks a row, us: 1 x 32,000 8.0, 8.4,
+    // 8.4, 8.6; 16 x 65,536 10.7, 10.4, 9.6, 9.8; 64 x 131,072 17.4, 12.8, 12.3, 14.2; 148 x 65,536 11.3, 12.1, 15.3, 22.9;
+    // 300 x 131,072 29.9, 27.4, 34.6, 46.6; 600 x 131,072 45.6, 47.3, 57.6, 87.0.  Without alternatives: 1 x 32,000 4.2, 4.3, 3.6, 3.6;
+    // 64 x 65,536 6.7, 5.5, 4.8, 5.1; 300 x 131,072 23.1, 20.8, 21.6, 21.9.
+    const int64_t batch = (int64_t)kThreads * kPieces * (type == AWE_F32 ? 4 : 8) * (top_k ? 2 : 1), sms = h->sm_count;
     int parts = 1;
-    while (parts < kMostCluster && T * parts * 2 <= 4 * h->sm_count && V >= batch * parts) parts *= 2;
+    for (; parts < kMostCluster; parts *= 2) {
+        const int64_t blocks = T * parts * 2;
+        if (blocks > 5 * sms || V < batch * 2 * parts * (2 * blocks <= sms ? 1 : blocks < 2 * sms ? 2 : 4)) break;
+    }
     cudaStream_t st = (cudaStream_t)stream;
     const cudaError_t e = type == AWE_F32 ? launch<AWE_F32>(p, T, parts, st) : type == AWE_BF16 ? launch<AWE_BF16>(p, T, parts, st) : launch<AWE_F16>(p, T, parts, st);
     if (e != cudaSuccess) return AWE_ERR_CUDA;

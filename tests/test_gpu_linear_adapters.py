@@ -162,3 +162,40 @@ def test_refusals():
 
 def b_alignment():
     return next(i for i in range(1, 12) if "align" in b.status_string(i))
+
+
+@pytest.mark.parametrize("rank", [8, 16, 32, 56, 128])
+@pytest.mark.parametrize("dtype,out,N", [(b.BF16, b.BF16, 640), (b.F16, b.F16, 517), (b.BF16, b.F32, 256), (b.F16, b.F32, 333)])
+def test_long_prompts(rank, dtype, out, N):
+    """As many tokens as take units of 32, of every length of the last one."""
+    s = make([33, 0, 1, 64, 300, 31, 8, 500, 207], [1, 2, 0, 4, -1, 3, 3, 0, 2], rank, N, 528, dtype, out, seed=rank + N, pad=8)
+    y = call(s).clone()
+    check(s, y)
+    assert torch.equal(y, call(s))
+
+
+@pytest.mark.parametrize("lengths", [[32] * 40, list(range(1, 65)), [2000], [0] * 9 + [641, 0, 700]])
+def test_long_prompts_of_many_lengths(lengths):
+    s = make(lengths, [(3 * i) % 6 - 1 if len(lengths) > 1 else 2 for i in range(len(lengths))], 16, 136, 4104, b.BF16, b.F32, seed=len(lengths))
+    check(s, call(s))
+    check(s, call(s, "none"), torch.zeros_like(s["base"]))
+    y = s["base"].clone()
+    check(s, call(s, "y", y))
+
+
+def test_long_prompts_outside_the_requests_and_between_the_rows():
+    s = make([400, 500], [0, 1], 16, 100, 64, b.F16, b.F16)
+    wide = torch.full((s["T"], 108), 7.0, device="cuda", dtype=torch.float16)
+    s["start"] = s["start"].clamp(max=s["T"] - 1)
+    y = call(s, y=wide)
+    s["lengths"] = [400, 499]
+    check(s, y[:, :100])
+    assert bool((y[-1] == 7.0).all()) and bool((y[:, 100:] == 7.0).all())
+
+
+def test_large_and_small_sums_of_long_prompts():
+    for factor in (2.0 ** -12, 2.0 ** 6):
+        s = make([5, 640], [0, 1], 32, 200, 512, b.F16, b.F32, seed=3)
+        s["a"] = (s["a"].float() * 512 ** 0.5 * factor).to(torch.float16)
+        s["x"] = (s["x"].float() * factor * 8).to(torch.float16)
+        check(s, call(s))

@@ -171,3 +171,11 @@ def test_refusals():
     assert status(top=33) == 2 and status(V=2 ** 30, ld=2 ** 30, T=1) == 2
     aligned = next(k for k in range(1, 12) if "align" in b.status_string(k))
     assert status(logits=x.view(torch.uint8).view(-1)[2:]) == aligned
+
+
+@pytest.mark.parametrize("dtype", [b.F16, b.F32])
+@pytest.mark.parametrize("T,V,top", [(1, 131072, 0), (3, 50257, 0), (2, 262147, 20), (70, 131075, 32), (100, 65601, 3), (160, 262144, 1), (301, 131072, 2)])
+def test_long_rows_of_few_and_many_tokens(T, V, top, dtype):
+    """Rows of one to eight blocks."""
+    x = logits(T, V, dtype, seed=T)
+    check(call(x, V, dtype, top, 0.7), x, V, float(torch.tensor(0.7)))
