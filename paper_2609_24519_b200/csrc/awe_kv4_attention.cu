@@ -9,8 +9,11 @@
 //   - The value's scale goes into the weight as an addition to its exponent, w_j = 2^(s_j / ln 2 + log2 vs_j - m), with m 10 to 15 below the
 //     largest such exponent so far, so that w_j rounds to FP16 as well as it can for what it contributes, and the products of all tokens
 //     add up in one accumulator.  The divisor is the sum of w_j 2^-log2 vs_j before that rounding.
-//   - A key's nibble with its sign bit flipped, u = code + 8, is FP16's subnormal u 2^-24 as it stands (or, four bits up, u 2^-20, which the
-//     queries make up for), so keys take one instruction a pair; the zero point goes off the score, q . K = sum q u - (zero + 8) sum q.
+//   - A key's nibble with its sign bit flipped, u = code + 8, moved to the top of a mantissa, is FP16's subnormal u 2^-18 (or, four bits
+//     down, u 2^-22, which the queries make up for), so keys take an instruction a pair and half a shift; the zero point goes off the score,
+//     q . K = sum q u - (zero + 8) sum q.  (The instruction lines products up by the exponent that subnormals have, 2^-14: with nibbles at
+//     the mantissa's bottom, which saves the shift, the logarithm over one token was off by 1.3e-6 of itself with FP16 queries, now by 3.2e-7.)
+//   - m is a whole number, so that it and the exponent of the sum add up exactly in the logarithm.
 //   - A value's becomes FP16 by inserting it into the mantissa of 1024 (or, four bits up, 16 of it) and subtracting 1024 and the zero point: taken off
 //     behind the sum, which is small where many tokens weigh alike, it would cost bits.
 //   - A 32-bit word's eight codes come apart in pairs (0, 4), (1, 5), (2, 6), (3, 7), so queries are laid out in that order once; of two
@@ -115,8 +118,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
         // ---- the query rows, as the matrix instruction's 16 x 8 operand: thread (g, t) holds of row g the dimensions t kD / 4 and
         // following, eight at a time in the order of the codes' pairs
         uint32_t qf[kNT][kSteps16][2];
-        float cq[kNT][2];                    // factor of the scores of columns 2t, 2t + 1, for scales that come 16 times and codes that come 2^-24 times
-        float q_sum[kNT][2];                 // sums of those columns' queries, 2^-24 times
+        float cq[kNT][2];                    // factor of the scores of columns 2t, 2t + 1, for scales that come 16 times and codes that come 2^-22 times
+        float q_sum[kNT][2];                 // sums of those columns' queries, 2^-22 times
         int see_lo[kNT][2], see_hi[kNT][2];  // tokens [see_lo, see_hi) are visible
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt) {
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
             const bool live = 8 * nt + g < n_rows;
             const int query = live ? row / p.group : 0, qh = head * p.group + (live ? row % p.group : 0);
             const T16* src = reinterpret_cast<const T16*>(p.q) + (int64_t)(r.q0 + query) * p.ldq + (int64_t)qh * kD + t * (kD / 4);
-            float factor = p.scale_log2 * 1048576.0f;
+            float factor = p.scale_log2 * 262144.0f;
 #pragma unroll
             for (int w = 0; w < kWords; ++w) {
                 uint4 x = make_uint4(0, 0, 0, 0);
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
             }
             total += __shfl_xor_sync(~0u, total, 1);
             total += __shfl_xor_sync(~0u, total, 2);
-            total *= 5.9604644775390625e-8f;  // 2^-24
+            total *= 2.384185791015625e-7f;  // 2^-22
             int lo_tok, hi_tok;
             visible(p, r, b, query, live, lo_tok, hi_tok);
 #pragma unroll
@@ -275,9 +278,9 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                 for (int w = 0; w < kWords; ++w) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint32_t x = k[0][w] >> (8 * h), y = k[1][w] >> (8 * h);
-                        const uint32_t f[4] = {and_xor(x, 0x000F000Fu, 0x00080008u), and_xor(y, 0x000F000Fu, 0x00080008u),
-                                               and_xor(x, 0x00F000F0u, 0x00800080u), and_xor(y, 0x00F000F0u, 0x00800080u)};
+                        const uint32_t x = h ? k[0][w] >> 6 : k[0][w] << 2, y = h ? k[1][w] >> 6 : k[1][w] << 2;
+                        const uint32_t f[4] = {and_xor(x, 0x003C003Cu, 0x00200020u), and_xor(y, 0x003C003Cu, 0x00200020u),
+                                               and_xor(x, 0x03C003C0u, 0x02000200u), and_xor(y, 0x03C003C0u, 0x02000200u)};
 #pragma unroll
                         for (int nt = 0; nt < kNT; ++nt) {
                             float(&to)[4] = h ? s_odd[nt] : s[nt];
@@ -321,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                             m = fmaxf(m, __shfl_xor_sync(~0u, m, 4));
                             m = fmaxf(m, __shfl_xor_sync(~0u, m, 8));
                             m = fmaxf(m, __shfl_xor_sync(~0u, m, 16));
-                            m = fmaxf(m - kBelow, m_ref[nt][j]);
+                            m = fmaxf(rintf(m - kBelow), m_ref[nt][j]);
                             const float a = m == m_ref[nt][j] ? 1.0f : exp2_approx(m_ref[nt][j] - m);
                             m_ref[nt][j] = m;
                             sum[nt][j] *= a;
@@ -374,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                 for (int c = 0; c < kSteps16; ++c) vec[2 * c] = o[c][nt][j], vec[2 * c + 1] = o[c][nt][j + 2];
             }
         __syncthreads();
-        finish_unit<kD, kRows, kBf16>(p, r, join_vec, join_stat, step0, step1, head, row0, n_rows);
+        finish_unit<kD, kRows, kBf16, true>(p, r, join_vec, join_stat, step0, step1, head, row0, n_rows);
         __syncthreads();
     }
 }
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(kThreads) kv4_attention_join_kernel(const Attn
     for (int k = 0; k < kVecs; ++k)
         if (const int d = 4 * lane + 128 * k; d < kD)
             *reinterpret_cast<uint2*>(dst + d) = make_uint2(Half<kBf16>::pack(x[k].x * inv, x[k].y * inv), Half<kBf16>::pack(x[k].z * inv, x[k].w * inv));
-    if (lane == 0 && p.lse) p.lse[(int64_t)token * q_heads + qh] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.69314718056f;
+    if (lane == 0 && p.lse) p.lse[(int64_t)token * q_heads + qh] = sum == 0.0f ? -INFINITY : log_sum(m, sum);
 }
 
 template <int kD, int kNT>

@@ -153,8 +153,16 @@ __device__ __forceinline__ Sees sees_of(const int (&see_lo)[kNT][2], const int (
     return {all_lo, all_hi, any_lo, any_hi};
 }
 
+// ln(2^m sum) for a whole m.
+__device__ __forceinline__ float log_sum(float m, float sum) {
+    int e;
+    const float f = frexpf(sum, &e);
+    return (m + (float)e + log2f(f)) * 0.69314718056f;
+}
+
 // The result of a unit, or its part, from the warps' vectors and (reference, sum of the weights, sum for the logarithm).
-template <int kD, int kRows, bool kBf16>
+// kWholeRef: references are whole numbers.
+template <int kD, int kRows, bool kBf16, bool kWholeRef = false>
 __device__ __forceinline__ void finish_unit(const AttnParams& p, const Request& r, const float* join_vec, const float4* join_stat, int step0, int step1,
                                             int head, int row0, int n_rows) {
     using T16 = typename Half<kBf16>::type;
@@ -195,7 +203,8 @@ __device__ __forceinline__ void finish_unit(const AttnParams& p, const Request& 
         }
         if (lane == 0) {
             if (!whole) p.part_stat[(int64_t)slot * kRows + row] = make_float4(m, total_sum, total_lse, 0.0f);
-            else if (p.lse) p.lse[token * p.heads * p.group + qh] = total_lse == 0.0f ? -INFINITY : (m + log2f(total_lse)) * 0.69314718056f;
+            else if (p.lse)
+                p.lse[token * p.heads * p.group + qh] = total_lse == 0.0f ? -INFINITY : kWholeRef ? log_sum(m, total_lse) : (m + log2f(total_lse)) * 0.69314718056f;
         }
     }
 }

@@ -268,3 +268,22 @@ def test_refusals():
     for bad in (dict(q=s["q"].view(-1)[1:]), dict(ldq=260), dict(ldo=260), dict(ws=ws[1:]), dict(cache=b.kv4_cache(s["k"].view(-1)[1:], s["v"], s["kp"], s["vp"], 2, 2, 16, 64))):
         assert status(**bad) == 4, bad
     assert b.awe_kv4_attention_workspace_bytes(handle(), cache, 2, 5, 2) == 0
+
+
+@pytest.mark.parametrize("dtype", [b.F16, b.BF16])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("ctx,window", [(1, 0), (2, 0), (1000, 1), (33, 3)])
+def test_logarithms_of_few_tokens(ctx, window, D, dtype):
+    """Where no sum evens errors out.  s / ln 2 - m lies between 8 and 16, where half an ulp is 2^-21; the exponential and the logarithm add
+    2^-22 each, factor and score some 2^-23 of the score: together, as a root mean square, below ln 2 (2^-21 + 2^-21 of the score)."""
+    s = make([1] * 24, [ctx] * 24, 10, 2, D, 16, dtype, window=window, seed=ctx + D)
+    call(s)
+    check(s)
+    want = torch.empty((24, 10), dtype=torch.float64, device="cuda")
+    for i in range(24):
+        pages = s["table"][i, :-(-ctx // 16)].long()
+        for h in range(2):
+            k = values(s["k"][pages, h], s["kp"][pages, h]).reshape(-1, D)[:ctx][-window:]
+            want[i, 5 * h:5 * h + 5] = torch.logsumexp(s["q"][i].double().view(10, D)[5 * h:5 * h + 5] @ k.t() * s["scale"], 1)
+    size = lambda x: float(x.square().mean().sqrt())  # noqa: E731
+    assert size(s["lse"][:24].double() - want) <= math.log(2) * 2.0 ** -21 * (1 + size(want) / math.log(2))
