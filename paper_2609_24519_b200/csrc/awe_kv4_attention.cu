@@ -23,11 +23,15 @@
 // warp and 16 tokens, half of them on the ALU pipe (53 % of its rate), 60 % of the issue slots.  64 requests of up to 8,192 tokens, 8 heads of 128: 97 us for
 // 282 MB = 2.9 TB/s (tiles of 16 tokens, keys unpacked like values: 110); 2 of 131,072: 80 us (join by a warp a row: 92).  Four blocks of three
 // stages on an SM (123 registers).
+#include <cooperative_groups.h>
+
 #include <algorithm>
 #include <type_traits>
 
 #include "kv4.cuh"
 #include "kv_attention_few.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace awe {
 namespace {
@@ -40,6 +44,7 @@ constexpr int kTile = 32;  // tokens of a warp's tile: two pieces of 16, which m
 constexpr int kStepTokens = kTile * kWarps;
 
 constexpr int64_t kSharedJoins = 1024;
+constexpr int kMostCluster = 8;
 
 template <int kD, int kNT>
 struct Config {
@@ -85,7 +90,57 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr) {
     return v;
 }
 
-template <int kD, int kNT, bool kBf16>
+// The result of a unit from the warps of a cluster, in whose blocks' shared memory they have left what finish_unit takes.  A block writes some
+// of the rows, each warp a quarter of their dimensions: kLanes threads with four each, so that 32 / kLanes of the vectors are read side by
+// side, and all of a thread's on their way together.
+template <int kD, int kRows, bool kBf16>
+__device__ __forceinline__ void finish_cluster(const AttnParams& p, const Request& r, const cg::cluster_group& cluster, float* join_vec, float4* join_stat, int head,
+                                               int row0, int n_rows) {
+    using T16 = typename Half<kBf16>::type;
+    constexpr int kVecPitch = kD + 4, kLanes = kD / (4 * kWarps), kGroups = 32 / kLanes, kEach = kMostCluster * kWarps / kGroups;
+    static_assert(kMostCluster * kWarps == 32);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = (int)cluster.num_blocks(), n = parts * kWarps;
+    const int d = warp * (kD / kWarps) + 4 * (lane % kLanes), group = lane / kLanes;
+    for (int row = (int)cluster.block_rank(); row < n_rows; row += parts) {
+        float4 st = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);  // of the cluster's warp `lane`
+        if (lane < n) st = cluster.map_shared_rank(join_stat, lane / kWarps)[lane % kWarps * kRows + row];
+        float4 y[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int w = group + kGroups * i;
+            y[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (w < n) y[i] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(join_vec, w / kWarps) + (w % kWarps * kRows + row) * kVecPitch + d);
+        }
+        float m = st.x;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, k));
+        const float c = st.x == -INFINITY ? (st.y == 0.0f ? 0.0f : 1.0f) : exp2_approx(st.x - m);
+        float sum = st.y * c;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const float weight = __shfl_sync(~0u, c, group + kGroups * i);
+            x.x = fmaf(y[i].x, weight, x.x), x.y = fmaf(y[i].y, weight, x.y), x.z = fmaf(y[i].z, weight, x.z), x.w = fmaf(y[i].w, weight, x.w);
+        }
+#pragma unroll
+        for (int k = 16; k >= kLanes; k >>= 1) {
+            x.x += __shfl_xor_sync(~0u, x.x, k), x.y += __shfl_xor_sync(~0u, x.y, k);
+            x.z += __shfl_xor_sync(~0u, x.z, k), x.w += __shfl_xor_sync(~0u, x.w, k);
+        }
+        const int64_t token = r.q0 + (row0 + row) / p.group;
+        const int qh = head * p.group + (row0 + row) % p.group;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (group == 0)
+            *reinterpret_cast<uint2*>(reinterpret_cast<T16*>(p.out) + token * p.ldo + (int64_t)qh * kD + d) =
+                make_uint2(Half<kBf16>::pack(x.x * inv, x.y * inv), Half<kBf16>::pack(x.z * inv, x.w * inv));
+        if (threadIdx.x == 0 && p.lse) p.lse[token * p.heads * p.group + qh] = sum == 0.0f ? -INFINITY : log_sum(m, sum);
+    }
+}
+
+// kCluster: a cluster of blocks per unit (p.whole), each with a part of its steps; else a block has some steps of some units.
+template <int kD, int kNT, bool kBf16, bool kCluster>
 __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_attention_kernel(const AttnParams p) {
     using C = Config<kD, kNT>;
     using T16 = typename Half<kBf16>::type;
@@ -96,7 +151,9 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
 
     grid_wait();
     Mine mine;
-    if (!find_steps<kRows, kStepTokens>(p, search, mine)) return;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int parts = kCluster ? (int)cluster.num_blocks() : 1;
+    if (!find_steps<kRows, kStepTokens>(p, search, mine, kCluster ? (int)blockIdx.x / parts : (int)blockIdx.x)) return;  // the whole cluster
     int b = mine.b;
     int64_t at = mine.at;
     Request r = request_of<kRows, kStepTokens>(p, b);
@@ -109,11 +166,15 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
             at += p.whole ? r.units : (int64_t)r.units * r.steps;
             r = request_of<kRows, kStepTokens>(p, ++b);
         }
-        const int unit = p.whole ? (int)(pos - at) : (int)((pos - at) / r.steps), step0 = p.whole ? 0 : (int)((pos - at) % r.steps);
-        const int step1 = p.whole ? r.steps : (int)min((int64_t)r.steps, step0 + mine.end - pos);
+        const int unit = p.whole ? (int)(pos - at) : (int)((pos - at) / r.steps);
+        int step0 = p.whole ? 0 : (int)((pos - at) % r.steps), step1 = p.whole ? r.steps : (int)min((int64_t)r.steps, step0 + mine.end - pos);
         const int head = unit % p.heads, row0 = unit / p.heads * kRows, n_rows = min(kRows, r.n * p.group - row0);
         const int32_t* table = p.table + (int64_t)b * p.ld_table;
         pos += p.whole ? 1 : step1 - step0;
+        if constexpr (kCluster) {
+            const int rank = (int)cluster.block_rank();
+            step0 = (int)((int64_t)r.steps * rank / parts), step1 = (int)((int64_t)r.steps * (rank + 1) / parts);
+        }
 
         // ---- the query rows, as the matrix instruction's 16 x 8 operand: thread (g, t) holds of row g the dimensions t kD / 4 and
         // following, eight at a time in the order of the codes' pairs
@@ -376,9 +437,15 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
 #pragma unroll
                 for (int c = 0; c < kSteps16; ++c) vec[2 * c] = o[c][nt][j], vec[2 * c + 1] = o[c][nt][j + 2];
             }
-        __syncthreads();
-        finish_unit<kD, kRows, kBf16, true>(p, r, join_vec, join_stat, step0, step1, head, row0, n_rows);
-        __syncthreads();
+        if constexpr (kCluster) {
+            cluster.sync();
+            finish_cluster<kD, kRows, kBf16>(p, r, cluster, join_vec, join_stat, head, row0, n_rows);
+            cluster.sync();  // no block goes on, or leaves, while it is read
+        } else {
+            __syncthreads();
+            finish_unit<kD, kRows, kBf16, true>(p, r, join_vec, join_stat, step0, step1, head, row0, n_rows);
+            __syncthreads();
+        }
     }
 }
 
@@ -498,13 +565,38 @@ int blocks_of(int sm_count, int64_t head_dim, int nt) {
     return sm_count * std::min(per_sm, nt == 1 && head_dim <= 128 ? 4 : 3);
 }
 
+// Contexts of a few steps a block: a cluster of blocks for each unit joins its parts without a second launch.  More blocks a unit while
+// there are two of them an SM at most, two a unit as long as all are resident; at most five steps a block, three where parts would have one
+// each.  Returns the blocks of a cluster, 1 for none, and the units.
+// 8 heads of 128, one query of 4 heads each, us in parts with a join / in clusters of 2, 4, 8: 1 request of 777 tokens 9.0 / 10.3, 8.2, 7.5; of
+// 4,000 10.8 / 23, 14.4, 10.6; of 8,000 12.8 / 40, 23, 14.9; 4 of 2,000 11.9 / 15.0, 10.8, 10.1; 8 of 1,000 12.0 / 11.1, 10.1, 11.7; 16 of 1,000 14.5 /
+// 12.8, 13.1, 21; 32 of 1,000 22.8 / 19.4, 24.7, 40; 64 of 500 22.8 / 25.8, 38, 77; 2 of 2,000 with 8 queries 19.8 / 20.8, 14.5, 14.8.
+int cluster_parts(const AttnParams& p, int nt, int64_t tokens, int blocks, int sm_count, int64_t& units) {
+    if (p.window > 0) tokens = std::min(tokens, p.window + p.T / p.B + kStepTokens);
+    const int64_t rows = 8 * nt, steps = (tokens + kStepTokens - 1) / kStepTokens;
+    units = std::min(p.T * ((p.group + rows - 1) / rows), (p.T * p.group + p.B * (rows - 1)) / rows) * p.heads;  // at most
+    int parts = 1;
+    while (parts < kMostCluster && parts < steps && units * parts * 2 <= (parts == 1 ? blocks : 2 * sm_count)) parts *= 2;
+    return !p.whole && units * p.B <= kWholeScans && steps <= (units * steps <= blocks ? 3 : 5) * parts ? parts : 1;
+}
+
 template <int kD, int kNT, bool kBf16>
-cudaError_t launch_attention(const AttnParams& p, int device, cudaStream_t st) {
+cudaError_t launch_attention(const AttnParams& p, int parts, int device, cudaStream_t st) {
     using C = Config<kD, kNT>;
-    static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(kv4_attention_kernel<kD, kNT, kBf16>, C::kSmemBytes, device, done);
+    static std::atomic<uint64_t> done{0}, done_cluster{0};
+    if (parts > 1) {
+        const cudaError_t e = allow_smem(kv4_attention_kernel<kD, kNT, kBf16, true>, C::kSmemBytes, device, done_cluster);
+        if (e != cudaSuccess) return e;
+        cudaLaunchAttribute attr[2] = {early_launch_attribute(), cluster_attribute(1)};
+        attr[1].val.clusterDim.x = parts, attr[1].val.clusterDim.y = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(p.blocks * parts)), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = C::kSmemBytes, cfg.stream = st;
+        cfg.attrs = attr, cfg.numAttrs = 2;
+        return cudaLaunchKernelEx(&cfg, kv4_attention_kernel<kD, kNT, kBf16, true>, p);
+    }
+    cudaError_t e = allow_smem(kv4_attention_kernel<kD, kNT, kBf16, false>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
-    if ((e = launch_early(kv4_attention_kernel<kD, kNT, kBf16>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
+    if ((e = launch_early(kv4_attention_kernel<kD, kNT, kBf16, false>, dim3(p.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     if (p.whole) return cudaSuccess;
     // Few rows have many parts each (one token of 131,072: 74), which a block joins faster than a warp; of many rows most have one or two.
     // Attention and its join, a warp and a block a row, us: 1 token over 131,072 (32 rows) 53.8 and 46.6, 8 over 16,000 (256) 48.0 and 47.4,
@@ -559,11 +651,15 @@ extern "C" awe_status_t awe_kv4_attention(awe_handle_t h, const awe_kv4_cache* c
     if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, true, workspace_dev, (cudaStream_t)stream);
     const int nt = row_tiles(T, B, p.group, cache->head_dim);
-    place_few(p, kStepTokens, blocks_of(h->sm_count, cache->head_dim, nt), nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);
+    const int blocks = blocks_of(h->sm_count, cache->head_dim, nt);
+    place_few(p, kStepTokens, blocks, nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);
+    int64_t units = 0;
+    const int parts = cluster_parts(p, nt, max_pages * cache->page_size, blocks, h->sm_count, units);
+    if (parts > 1) p.whole = 1, p.blocks = (int)units;
     auto run = [&](auto dim, auto tiles) {
         constexpr int kD = decltype(dim)::value, kNT = decltype(tiles)::value;
-        return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, h->device, (cudaStream_t)stream)
-                                : launch_attention<kD, kNT, false>(p, h->device, (cudaStream_t)stream);
+        return type == AWE_BF16 ? launch_attention<kD, kNT, true>(p, parts, h->device, (cudaStream_t)stream)
+                                : launch_attention<kD, kNT, false>(p, parts, h->device, (cudaStream_t)stream);
     };
     using std::integral_constant;
     cudaError_t e;

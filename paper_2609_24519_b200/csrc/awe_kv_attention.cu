@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const AttnParams
 
     grid_wait();
     Mine mine;
-    if (!find_steps<kRows, kStepTokens>(p, search, mine)) return;
+    if (!find_steps<kRows, kStepTokens>(p, search, mine, blockIdx.x)) return;
     const int64_t begin = mine.begin, end = mine.end;
     int b = mine.b;
     int64_t at = mine.at;

@@ -33,7 +33,7 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int b) {
     return r;
 }
 
-// Which steps are this block's, by an exclusive sum of units x steps over the requests: [begin, end), the request that `begin` lies in
+// Which steps are block `number`'s, by an exclusive sum of units x steps over the requests: [begin, end), the request that `begin` lies in
 // and where its steps start.  False if there are none.
 struct Search {
     int64_t scan[kWarps];
@@ -45,11 +45,11 @@ struct Mine {
     int b;
 };
 template <int kRows, int kStepTokens>
-__device__ __forceinline__ bool find_steps(const AttnParams& p, Search& sh, Mine& mine_out) {
+__device__ __forceinline__ bool find_steps(const AttnParams& p, Search& sh, Mine& mine_out, int number) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int64_t total = 0;
     for (int pass = 0; pass < 2; ++pass) {
-        const int64_t mine = pass ? Deal(total, p.blocks).begin(blockIdx.x) : 0;
+        const int64_t mine = pass ? Deal(total, p.blocks).begin(number) : 0;
         int64_t sum = 0;
         for (int b0 = 0; b0 < p.B; b0 += kThreads) {
             const int b = b0 + tid;
@@ -87,8 +87,8 @@ __device__ __forceinline__ bool find_steps(const AttnParams& p, Search& sh, Mine
     if (blockIdx.x == 0 && tid == 0) p.unit_steps[p.B] = total;
     __syncthreads();
     const Deal deal(total, p.blocks);
-    if ((int)blockIdx.x >= deal.blocks || total == 0) return false;
-    mine_out = {deal.begin(blockIdx.x), deal.begin(blockIdx.x + 1), sh.found_at, sh.found_b};
+    if (number >= deal.blocks || total == 0) return false;
+    mine_out = {deal.begin(number), deal.begin(number + 1), sh.found_at, sh.found_b};
     return true;
 }
 

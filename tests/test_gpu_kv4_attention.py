@@ -287,3 +287,29 @@ def test_logarithms_of_few_tokens(ctx, window, D, dtype):
             want[i, 5 * h:5 * h + 5] = torch.logsumexp(s["q"][i].double().view(10, D)[5 * h:5 * h + 5] @ k.t() * s["scale"], 1)
     size = lambda x: float(x.square().mean().sqrt())  # noqa: E731
     assert size(s["lse"][:24].double() - want) <= math.log(2) * 2.0 ** -21 * (1 + size(want) / math.log(2))
+
+
+@pytest.mark.parametrize("D,dtype", [(64, b.F16), (128, b.BF16), (256, b.F16)])
+@pytest.mark.parametrize("Hq,H", [(4, 4), (16, 4), (15, 3), (32, 2)])
+@pytest.mark.parametrize("B", [1, 5, 12, 40])
+def test_contexts_of_a_few_steps(B, Hq, H, D, dtype):
+    """Clusters of two, four and eight blocks; requests that leave some of the blocks without a step, or all."""
+    ctx = [(1000, 1, 300, 129, 777, 40, 128, 999, 513)[i % 9] for i in range(B)]
+    s = make([1] * B, ctx, Hq, H, D, 32, dtype, seed=B + Hq)
+    call(s)
+    check(s)
+    first = s["out"].clone()
+    call(s)
+    assert torch.equal(first, s["out"])
+    s = make([3, 0, 1] * ((B + 2) // 3), [1000, 0, 640] * ((B + 2) // 3), Hq, H, D, 16, dtype, window=200 if B == 5 else 0, seed=B, pad=8)
+    s["table"][0, :17] = -1  # its first blocks have nothing
+    s["table"][-1] = -1
+    call(s)
+    check(s)
+
+
+def test_short_contexts_take_one_launch():
+    for B, ctx in ((1, 100), (1, 777), (4, 2000), (16, 500), (32, 1000)):
+        assert call(make([1] * B, [ctx] * B, 32, 8, 128, 32, b.BF16, width=-(-ctx // 32))) == 1
+    for B, ctx in ((1, 8000), (64, 1000)):
+        assert call(make([1] * B, [ctx] * B, 32, 8, 128, 32, b.BF16, width=-(-ctx // 32))) == 2
