@@ -505,7 +505,8 @@ typedef struct {
  * q_start[b + 1] - 1 of request b; y = base where a is outside 0 .. n_adapters - 1.  The rows outside every request are left as they
  * are.  x_dev: T x K of the adapters' type, 16-B aligned, ldx a multiple of 8.  base_dev, y_dev: T x N of y_type, the adapters' type or
  * AWE_F32, any strides; base_dev may be y_dev itself (with ldb = ldy), or NULL for zeros.  Products are exact and summed in FP32; the rank's sums
- * enter the second product as values of `type` that together hold 16 bits (BF16; 24 for FP32 y) or 21 (FP16, of the token's largest); y is rounded once. */
+ * enter the second product as values of `type` that together hold 16 bits (BF16; 24 for FP32 y) or 21 (FP16, of the token's largest); y is rounded once.
+ * A token whose sums over the rank or K are not all finite has NaN, or an infinity, in y; other tokens are not touched by it. */
 awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* L, const void* x_dev, int64_t T, int64_t ldx,
                                  const int32_t* q_start_dev, const int32_t* adapter_dev, int64_t B, const void* base_dev, int64_t ldb,
                                  void* y_dev, awe_float_t y_type, int64_t ldy, void* stream);

@@ -19,7 +19,7 @@
 //   - A 32-bit word's eight codes come apart in pairs (0, 4), (1, 5), (2, 6), (3, 7), so queries are laid out in that order once; of two
 //     tokens' values the 16-bit halves of their words are put together first, which pairs tokens.
 //
-// A token and head of dimension 128 is 132 bytes of keys and values; what bounds long contexts is not reading them but the instructions: 367 a
+// A token and head of dimension 128 is 132 bytes of keys and values; what bounds long contexts is not reading them but the instructions: some 370 a
 // warp and 16 tokens, half of them on the ALU pipe (53 % of its rate), 60 % of the issue slots.  64 requests of up to 8,192 tokens, 8 heads of 128: 97 us for
 // 282 MB = 2.9 TB/s (tiles of 16 tokens, keys unpacked like values: 110); 2 of 131,072: 80 us (join by a warp a row: 92).  Four blocks of three
 // stages on an SM (123 registers).

@@ -199,3 +199,17 @@ def test_large_and_small_sums_of_long_prompts():
         s["a"] = (s["a"].float() * 512 ** 0.5 * factor).to(torch.float16)
         s["x"] = (s["x"].float() * factor * 8).to(torch.float16)
         check(s, call(s))
+
+
+@pytest.mark.parametrize("dtype", [b.BF16, b.F16])
+@pytest.mark.parametrize("lengths", [[3, 1, 4], [300, 1, 407]])
+def test_infinities_and_nan_stay_with_their_token(lengths, dtype):
+    s = make(lengths, [0, -1, 1], 24, 200, 512, dtype, dtype, seed=7)
+    s["x"][1, 40], s["x"][-1, 511], s["x"][lengths[0], 3] = float("inf"), float("nan"), float("nan")  # the last of a token without an adapter
+    y = call(s).clone()
+    bad = torch.zeros(s["T"], dtype=torch.bool, device="cuda")
+    bad[1] = bad[-1] = True
+    assert not bool(y[bad].isfinite().any()) and bool(y[~bad].isfinite().all())
+    s["x"][bad] = 0
+    s["x"][lengths[0], 3] = 0
+    assert torch.equal(call(s)[~bad], y[~bad])

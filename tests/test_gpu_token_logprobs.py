@@ -179,3 +179,18 @@ def test_long_rows_of_few_and_many_tokens(T, V, top, dtype):
     """Rows of one to eight blocks."""
     x = logits(T, V, dtype, seed=T)
     check(call(x, V, dtype, top, 0.7), x, V, float(torch.tensor(0.7)))
+
+
+def test_two_streams_at_once():
+    rows = [logits(33, 50257, b.BF16, seed=i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in rows]
+    torch.cuda.synchronize()
+    out = [[], []]
+    for _ in range(4):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                out[i].append(call(rows[i], 50257, b.BF16, 7))
+    torch.cuda.synchronize()
+    for i in range(2):
+        check(out[i][0], rows[i], 50257)
+        assert all(torch.equal(o[k], out[i][0][k]) for o in out[i] for k in o)
