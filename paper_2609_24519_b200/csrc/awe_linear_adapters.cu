@@ -544,35 +544,52 @@ cudaError_t launch(Kernel kernel, const AdapterParams& p, int64_t units, int par
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
-// Lets a kernel have clusters of 16, which not every GPU can: asked once per device, as allow_smem is.
+// Blocks of a cluster: the most, a power of two, with which all units that may not be empty are resident at once and every warp has a step of k.
+// Fewer large clusters fit than the SMs have room for (17 units of rank 64 take 13.5 us in clusters of 16 and 8.8 in clusters of 8), so
+// the runtime is asked, once per device and size; `fit`: what it said, plus 1.
 template <class Kernel>
-cudaError_t allow_large_cluster(Kernel kernel, int device, std::atomic<uint64_t>& done) {
-    const uint64_t bit = (uint64_t)1 << (device & 63);
-    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
-    return e;
+int cluster_of(Kernel kernel, const AdapterParams& p, int64_t units, int most, int smem, std::atomic<int> (&fit)[5]) {
+    const int64_t live = std::min(units, (int64_t)p.T), steps = (p.K + 31) / 32;
+    for (int log2 = most == 16 ? 4 : 3, parts = most; log2 > 0; --log2, parts /= 2) {
+        if (steps < (int64_t)kWarps * parts) continue;
+        int n = fit[log2].load(std::memory_order_relaxed) - 1;
+        if (n < 0) {
+            cudaLaunchAttribute attr = cluster_attribute(1);
+            attr.val.clusterDim.x = parts, attr.val.clusterDim.y = 1;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(parts), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = smem, cfg.attrs = &attr, cfg.numAttrs = 1;
+            // clusters of 16 not every GPU can have
+            if ((parts > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+                cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                n = 0;
+            }
+            fit[log2].store(n + 1, std::memory_order_relaxed);
+        }
+        if (live <= n) return parts;
+    }
+    return 1;
 }
 template <bool kBf16, bool kF32, int kRT>
-cudaError_t launch_rank(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
-    static std::atomic<uint64_t> done_few{0}, done_many{0}, done{0};
-    if (parts > 8) {
-        const cudaError_t e = few ? allow_large_cluster(adapters_few_kernel<kBf16, kF32, kRT>, device, done_few)
-                                  : allow_large_cluster(adapters_many_kernel<kBf16, kF32, 2 * kRT>, device, done_many);
-        if (e != cudaSuccess) return e;
+cudaError_t launch_rank(const AdapterParams& p, bool few, int64_t units, int device, cudaStream_t st) {
+    static std::atomic<int> fit_few[64][5], fit_many[64][5];
+    static std::atomic<uint64_t> done{0};
+    if (few) {
+        const auto kernel = adapters_few_kernel<kBf16, kF32, kRT>;
+        return launch(kernel, p, units, cluster_of(kernel, p, units, kMostCluster, 0, fit_few[device & 63]), 0, st);
     }
-    if (few) return launch(adapters_few_kernel<kBf16, kF32, kRT>, p, units, parts, 0, st);
     using M = Many<2 * kRT>;
-    const cudaError_t e = allow_smem(adapters_many_kernel<kBf16, kF32, 2 * kRT>, M::kSmemBytes, device, done);
+    const auto kernel = adapters_many_kernel<kBf16, kF32, 2 * kRT>;
+    const cudaError_t e = allow_smem(kernel, M::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
-    return launch(adapters_many_kernel<kBf16, kF32, 2 * kRT>, p, units, parts, M::kSmemBytes, st);
+    return launch(kernel, p, units, cluster_of(kernel, p, units, 8, M::kSmemBytes, fit_many[device & 63]), M::kSmemBytes, st);
 }
 template <bool kBf16, bool kF32>
-cudaError_t launch_type(const AdapterParams& p, bool few, int64_t units, int parts, int device, cudaStream_t st) {
-    return p.rank <= 16   ? launch_rank<kBf16, kF32, 1>(p, few, units, parts, device, st)
-           : p.rank <= 32 ? launch_rank<kBf16, kF32, 2>(p, few, units, parts, device, st)
-           : p.rank <= 64 ? launch_rank<kBf16, kF32, 4>(p, few, units, parts, device, st)
-                          : launch_rank<kBf16, kF32, 8>(p, few, units, parts, device, st);
+cudaError_t launch_type(const AdapterParams& p, bool few, int64_t units, int device, cudaStream_t st) {
+    return p.rank <= 16   ? launch_rank<kBf16, kF32, 1>(p, few, units, device, st)
+           : p.rank <= 32 ? launch_rank<kBf16, kF32, 2>(p, few, units, device, st)
+           : p.rank <= 64 ? launch_rank<kBf16, kF32, 4>(p, few, units, device, st)
+                          : launch_rank<kBf16, kF32, 8>(p, few, units, device, st);
 }
 
 }  // namespace
@@ -607,23 +624,10 @@ extern "C" awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* 
     const bool few = 2 * (T / kFew + B) <= h->sm_count || T <= 2 * B;
     const int64_t units = T / (few ? kFew : kMany) + B;
     if (units > INT32_MAX / kMostCluster) return AWE_ERR_UNSUPPORTED;
-    // The largest cluster with which all blocks are resident at once, and every warp has a step of k.
-    const int64_t live = std::min(units, T);  // units that are not empty, at most
-    const int resident = h->sm_count * (few ? (L->rank <= 16 ? 3 : 2) : (L->rank <= 64 ? 2 : 1));
-    int parts = 1;
-    while (parts < (few ? kMostCluster : 8) && live * parts * 2 <= resident && (L->K + 31) / 32 >= 2 * kWarps * parts) parts *= 2;
     cudaStream_t st = (cudaStream_t)stream;
     const bool f32 = y_type == AWE_F32;
-    auto run = [&] {
-        return L->type == AWE_BF16 ? (f32 ? launch_type<true, true>(p, few, units, parts, h->device, st) : launch_type<true, false>(p, few, units, parts, h->device, st))
-                                   : (f32 ? launch_type<false, true>(p, few, units, parts, h->device, st) : launch_type<false, false>(p, few, units, parts, h->device, st));
-    };
-    cudaError_t e = run();
-    if (e != cudaSuccess && parts > 8) {  // a part of a GPU may have no room for clusters of 16
-        cudaGetLastError();
-        parts = 8;
-        e = run();
-    }
+    const cudaError_t e = L->type == AWE_BF16 ? (f32 ? launch_type<true, true>(p, few, units, h->device, st) : launch_type<true, false>(p, few, units, h->device, st))
+                                              : (f32 ? launch_type<false, true>(p, few, units, h->device, st) : launch_type<false, false>(p, few, units, h->device, st));
     if (e != cudaSuccess) return AWE_ERR_CUDA;
     h->launches += 1;
     return AWE_OK;
