@@ -14,7 +14,7 @@
 //
 // HBM bounds many rows; a single row is spread over a cluster of blocks that join in shared memory, which bounds it by latency.
 // 2,048 rows of 50,257 (FP16): 44 us = 4.7 TB/s, with 77 % of the issue slots and 61 % of the exponentials' rate; 128 rows of 131,072 (BF16) with 20
-// alternatives 17.5 us, without 10.7; one row of 32,000 (FP32) 6.7 us.
+// alternatives 17.5 us, without 10.7; one row of 32,000 (FP32) 7.0 us.
 #include <cooperative_groups.h>
 
 #include <algorithm>
