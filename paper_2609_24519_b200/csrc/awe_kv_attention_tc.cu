@@ -632,6 +632,7 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
                             const bool grows = pass == 0 && top > (first ? -INFINITY : m_ref + kMostAbove);  // once: then top is 10 above it
                             again = __any_sync(~0u, grows);
                             if (again) {
+                                ptx::tmem_wait_st();  // P of the first half and O may have been stored in this step, and are loaded here
                                 const float before = m_ref;
                                 if (grows) m_ref = first ? top - kBelow : m_ref + ceilf(top - kBelow - m_ref);
                                 const float shrink = first || !grows ? 1.0f : exp2_approx(before - m_ref);

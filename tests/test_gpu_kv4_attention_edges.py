@@ -1,0 +1,115 @@
+"""Attention over the 4-bit cache where it can go wrong: references of the softmax that move inside a step.
+
+The scores are built: one dimension of the keys carries them, each a value that the format holds, and the reference computes from the
+stored bytes in 64 bits.  Tolerance, with u the unit roundoff of the output type, p_j the probabilities and P the largest: a weight is rounded to
+FP16, the largest standing between 2^9 and 2^15, so by 2^-11 of itself, or by 2^-25 <= 2^-34 P where it is below 2^-14, which p_j >= 2^-23 P is not;
+FP32 sums and exponentials add less than 2^-14 for the scores here (below 2^6, so that 2^-14 is many FP32 roundings of an exponent).  So
+|out - ref| <= u |ref| + (1 + u) ((2^-11 + 2^-14) sum_j p_j |v_j| + 2^-34 P sum_small |v_j|) + 2^-25, the last for FP16's subnormals."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_24519_b200 import binding as b
+
+from .gpu_util import handle
+from .test_gpu_kv4_attention import TORCH, values
+
+pytestmark = pytest.mark.gpu
+KINDS = [(64, b.F16), (128, b.BF16)]
+
+
+def words(scale, zero):
+    """Parameter words; scales are cut to the format's 7 significant bits."""
+    bits = (scale * 16).half().view(torch.int16) & -16
+    return bits | (zero.to(torch.int16) & 15)
+
+
+def built(exponents, value_scales, rows, D, dtype, Hq=8, wide=True, seed=0):
+    """One request whose `rows` (a factor each) last tokens ask: the score of token j and row r, as a base-2 exponent, is rows[r] exponents[j]
+    (up to 7 bits), its values are random codes times value_scales[j].  wide: a table so wide that the kernel for prompts takes many rows."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n, T, page = len(exponents), len(rows), 16
+    pool = -(-n // page)
+    x = torch.tensor(exponents, dtype=torch.float64, device="cuda")
+    factor = 1.0 if dtype == b.F16 else 2.0
+    k = torch.full((pool * page, D // 2), 0x88, dtype=torch.uint8, device="cuda")  # every code its zero point, -8
+    k[:n, 0] = torch.where(x == 0, 0x88, 0x80).to(torch.uint8)  # of dimension 0: 8 scales above it
+    k_scale = torch.full((pool * page,), 1.0, dtype=torch.float64, device="cuda")
+    k_scale[:n] = torch.where(x == 0, 1.0, x.abs() / 8 / factor)
+    v = torch.randint(0, 256, (pool * page, D // 2), generator=g, device="cuda", dtype=torch.uint8)
+    v_scale = torch.full((pool * page,), 1.0, dtype=torch.float64, device="cuda")
+    v_scale[:n] = torch.tensor(value_scales, dtype=torch.float64, device="cuda")
+    minus8 = torch.full((pool * page,), -8, device="cuda")
+    q = torch.zeros((T, Hq, D), dtype=TORCH[dtype], device="cuda")
+    q[:, :, 0] = (torch.tensor(rows, device="cuda") * factor)[:, None].to(TORCH[dtype])
+    width = max(pool, 4096 // page) if wide else pool
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, :pool] = torch.randperm(pool, generator=g, device="cuda").to(torch.int32)
+    place = (table[0, :pool].long()[:, None] * page + torch.arange(page, device="cuda")).flatten()
+
+    def spread(a):
+        to = torch.empty_like(a)
+        to[place] = a
+        return to.view(pool, 1, page, *a.shape[1:])
+
+    zero = torch.randint(-4, 4, (pool * page,), generator=g, device="cuda")
+    return dict(n=n, T=T, Hq=Hq, D=D, dtype=dtype, page=page, pool=pool, width=width, table=table, q=q, k=spread(k), v=spread(v),
+                kp=spread(words(k_scale, minus8)), vp=spread(words(v_scale, zero)), place=place[:n], scale=math.log(2.0))
+
+
+def attend(s, causal=False):
+    cache = b.kv4_cache(s["k"], s["v"], s["kp"], s["vp"], s["pool"], 1, s["page"], s["D"])
+    ws = torch.empty(b.awe_kv4_attention_workspace_bytes(handle(), cache, s["T"], s["Hq"], 1), dtype=torch.uint8, device="cuda")
+    start, ctx = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, s["T"]], [s["n"]]))
+    out, lse = torch.empty_like(s["q"]), torch.empty((s["T"], s["Hq"]), device="cuda")
+    before = b.awe_launch_count(handle())
+    b.awe_kv4_attention(handle(), cache, s["q"], s["dtype"], s["T"], s["Hq"], s["Hq"] * s["D"], start, ctx, 1, s["table"], s["width"], s["width"], s["scale"],
+                        causal, 0, out, s["Hq"] * s["D"], lse, ws)
+    torch.cuda.synchronize()
+    assert b.awe_last_device_status(handle()) == (0, 0)
+    return out.double(), lse.double(), b.awe_launch_count(handle()) - before
+
+
+def reference(s):
+    """Output, lse, sum of p |v| and each row's probabilities, over all tokens."""
+    k = values(s["k"].flatten(0, 2), s["kp"].flatten())[s["place"]]
+    v = values(s["v"].flatten(0, 2), s["vp"].flatten())[s["place"]]
+    x = torch.einsum("thd,nd->thn", s["q"].double(), k) * s["scale"]
+    p = torch.softmax(x, -1)
+    return p @ v, torch.logsumexp(x, -1), p @ v.abs(), p, v
+
+
+def check(s, out, lse):
+    want, want_lse, size, p, v = reference(s)
+    u = torch.finfo(TORCH[s["dtype"]]).eps / 2
+    most = p.amax(-1, keepdim=True)
+    floor = 2.0 ** -34 * most * ((p < 2.0 ** -23 * most).double() @ v.abs())
+    slack = u * want.abs() + (1 + u) * ((2.0 ** -11 + 2.0 ** -14) * size + floor) + 2.0 ** -25
+    assert bool(((out - want).abs() <= slack).all()), float(((out - want).abs() / slack).max())
+    assert bool(((lse - want_lse).abs() <= 2.0 ** -14 + 2.0 ** -22 * want_lse.abs()).all())
+
+
+def steps_of(jumps, lead=128):
+    """Exponents of steps of 128 tokens: `lead` tokens at 0, then each pair of `jumps` raises the first and the second half of a step."""
+    e, level = [0.0] * lead, 0.0
+    for j in jumps:
+        level += j
+        e += [level] * 64
+    return e
+
+
+@pytest.mark.parametrize("D,dtype", KINDS)
+@pytest.mark.parametrize("slow", [None, 2, 31])
+@pytest.mark.parametrize("jumps", [[7, 7], [6, 6, 6, 6], [0, 7, 7, 6], [8, 0, 6, 6]])
+def test_references_that_move_in_both_halves_of_a_step(jumps, slow, D, dtype):
+    """Every token contributes alike: values shrink as the scores rise, so what was stored before a reference moved has to be brought along.
+    slow: every slow-th row's scores rise by an eighth of that, so that only some rows of a warp move theirs."""
+    e = steps_of(jumps)
+    rows = [0.125 if slow and i % slow == 0 else 1.0 for i in range(1024)]
+    s = built(e, [2.0 ** (11 - x) for x in e], rows, D, dtype)
+    out, lse, launches = attend(s)
+    assert launches == 3
+    check(s, out, lse)
+    again, lse_again, _ = attend(s)
+    assert torch.equal(out, again) and torch.equal(lse, lse_again)
