@@ -642,8 +642,10 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
                                     uint32_t before_p[32];
                                     ptx::tmem_ld_32x32(s_at[t] + lanes, before_p);
                                     ptx::tmem_wait_ld();
+                                    // by two factors: weights of up to 2^15 stay FP16 numbers under 2^-39, whose nearest FP16 number is 0
+                                    const __half2 down = __float2half2_rn(fmaxf(shrink, 1.0f / 65536)), rest = __float2half2_rn(fminf(shrink * 65536.0f, 1.0f));
 #pragma unroll
-                                    for (int e = 0; e < 32; ++e) before_p[e] = mul2(before_p[e], __float2half2_rn(shrink));
+                                    for (int e = 0; e < 32; ++e) before_p[e] = mul2(mul2(before_p[e], down), rest);
                                     ptx::tmem_st_32x32(s_at[t] + lanes, before_p);
                                 }
                             } else {

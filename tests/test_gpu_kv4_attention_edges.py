@@ -113,3 +113,18 @@ def test_references_that_move_in_both_halves_of_a_step(jumps, slow, D, dtype):
     check(s, out, lse)
     again, lse_again, _ = attend(s)
     assert torch.equal(out, again) and torch.equal(lse, lse_again)
+
+
+@pytest.mark.parametrize("D,dtype", KINDS)
+@pytest.mark.parametrize("first,second", [(4.75, 24.0), (4.75, 25.0), (4.75, 27.0), (0.0, 26.0), (4.75, 31.0), (4.75, 33.0)])
+def test_first_half_of_a_step_beside_a_jump_of_many_powers_in_the_second(first, second, D, dtype):
+    """Scores of 0, then a step whose first half passes the reference by too little to move it and whose last token moves it by 2^25 to 2^34: the
+    first half's weights stay FP16 numbers beside the new largest one.  Its values are up to 2^29 times the others'.  So many rows that most blocks
+    have whole units, whose first step comes before this one."""
+    e = [0.0] * 128 + [first] * 64 + [0.0] * 63 + [second]
+    large = [2.0 ** -17] * 128 + [4064.0] * 64 + [2.0 ** -17] * 64
+    for value_scales in (large, [1.0] * 128 + [256.0] * 64 + [1.0] * 64):
+        s = built(e, value_scales, [1.0] * 8192, D, dtype)
+        out, lse, launches = attend(s)
+        assert launches == 3
+        check(s, out, lse)
