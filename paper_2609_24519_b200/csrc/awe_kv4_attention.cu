@@ -6,7 +6,7 @@
 // warps, and that the instruction's rows are tokens (then dimensions) and its columns query rows, is as for the 8-bit cache
 // (awe_kv_attention.cu).  Different here:
 //
-//   - The value's scale goes into the weight as an addition to its exponent, w_j = 2^(s_j / ln 2 + log2 vs_j - m), with m 10 to 15 below the
+//   - The value's scale goes into the weight as an addition to its exponent, w_j = 2^(s_j / ln 2 + log2 vs_j - m), with m 9 to 15 below the
 //     largest such exponent so far, so that w_j rounds to FP16 as well as it can for what it contributes, and the products of all tokens
 //     add up in one accumulator.  The divisor is the sum of w_j 2^-log2 vs_j before that rounding.
 //   - A key's nibble with its sign bit flipped, u = code + 8, moved to the top of a mantissa, is FP16's subnormal u 2^-18 (or, four bits

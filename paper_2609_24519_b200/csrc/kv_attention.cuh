@@ -42,7 +42,8 @@ struct Deal {
 
 // Weights are rounded to FP16 as exp2(s - m).  The reference m is put kBelow below the largest s so far and moves only when an s
 // passes it by more than kMostAbove, which is rare, so the largest weight lies between 2^10 and 2^15 and FP16 holds all that
-// it can beside it: a weight keeps 11 bits down to 2^-24 of the largest, and is off by 2^-35 of that at most below.
+// it can beside it: a weight keeps 11 bits down to 2^-24 of the largest, and is off by 2^-35 of that at most below.  (Over the 4-bit cache m
+// is a whole number, or moves by whole numbers, so 2^10 is 2^9 there, and 2^-35 is 2^-34.)
 constexpr float kBelow = 10.0f, kMostAbove = 15.0f;
 
 // BF16 queries go to FP16 times 2^(15 - e), e the exponent of the row's largest magnitude, whose biased exponent is given: that

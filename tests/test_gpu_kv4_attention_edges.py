@@ -128,3 +128,30 @@ def test_first_half_of_a_step_beside_a_jump_of_many_powers_in_the_second(first, 
         out, lse, launches = attend(s)
         assert launches == 3
         check(s, out, lse)
+
+
+@pytest.mark.parametrize("D,dtype", KINDS)
+@pytest.mark.parametrize("first", [True, False])
+@pytest.mark.parametrize("below", [20, 26, 33, 36, 40])
+def test_token_of_least_scale_above_tokens_of_large_scale(below, first, D, dtype):
+    """The dominant token contributes next to nothing.  For few rows the others count by what they contribute (their weight times scale, q_j, by
+    2^-34 of the largest q: 2^-25 below 2^9); for prompts by their weight."""
+    e, scales = [float(below)] + [0.0] * 300, [2.0 ** -18] + [4064.0] * 300
+    if not first:
+        e.reverse(), scales.reverse()
+    s = built(e, scales, [1.0] * 1024, D, dtype)
+    out, lse, launches = attend(s)
+    assert launches == 3
+    check(s, out, lse)
+    for rows in ([1.0], [1.0, 0.5, 0.25]):
+        s = built(e, scales, rows, D, dtype, wide=False)
+        out, lse, launches = attend(s)
+        assert launches < 3
+        want, want_lse, size, p, v = reference(s)
+        vs = torch.tensor(scales, dtype=torch.float64, device="cuda")
+        q, u = p * vs, torch.finfo(TORCH[dtype]).eps / 2
+        most = q.amax(-1, keepdim=True)
+        floor = 2.0 ** -34 * most * ((q < 2.0 ** -23 * most).double() @ (v.abs() / vs[:, None]))
+        slack = u * want.abs() + (1 + u) * ((2.0 ** -11 + 2.0 ** -14) * size + floor) + 2.0 ** -25
+        assert bool(((out - want).abs() <= slack).all()), float(((out - want).abs() / slack).max())
+        assert bool(((lse - want_lse).abs() <= 2.0 ** -14 + 2.0 ** -22 * want_lse.abs()).all())
