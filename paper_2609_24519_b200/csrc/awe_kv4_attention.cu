@@ -13,6 +13,8 @@
 //     down, u 2^-22, which the queries make up for), so keys take an instruction a pair and half a shift; the zero point goes off the score,
 //     q . K = sum q u - (zero + 8) sum q.  (The instruction lines products up by the exponent that subnormals have, 2^-14: with nibbles at
 //     the mantissa's bottom, which saves the shift, the logarithm over one token was off by 1.3e-6 of itself with FP16 queries, now by 3.2e-7.)
+//     Both sums are FP32, so where a key's codes are its zero point but for one channel the score keeps what rounding 15 sum |q| leaves: 1e-5 for 256
+//     elements of spread 4 and a scale of 1.
 //   - m is a whole number, so that it and the exponent of the sum add up exactly in the logarithm.
 //   - A value's becomes FP16 by inserting it into the mantissa of 1024 (or, four bits up, 16 of it) and subtracting 1024 and the zero point: taken off
 //     behind the sum, which is small where many tokens weigh alike, it would cost bits.

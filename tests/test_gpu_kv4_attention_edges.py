@@ -155,3 +155,25 @@ def test_token_of_least_scale_above_tokens_of_large_scale(below, first, D, dtype
         slack = u * want.abs() + (1 + u) * ((2.0 ** -11 + 2.0 ** -14) * size + floor) + 2.0 ** -25
         assert bool(((out - want).abs() <= slack).all()), float(((out - want).abs() / slack).max())
         assert bool(((lse - want_lse).abs() <= 2.0 ** -14 + 2.0 ** -22 * want_lse.abs()).all())
+
+
+@pytest.mark.parametrize("D,dtype", [*KINDS, (256, b.F16)])
+@pytest.mark.parametrize("zero", [-8, 0, 7])
+@pytest.mark.parametrize("other", [0, 1])
+def test_keys_whose_codes_are_their_zero_point_but_for_one_channel(other, zero, D, dtype):
+    """A score of few rows is the difference of sum q (code + 8) and (zero + 8) sum q, whose terms may be large where sum |q k| is small or 0.  Each is
+    a sum of D / 16 matrix steps (D / 2 additions) of at most 15 sum |q| in all: off by D 2^-23 of that, times key scale and factor."""
+    s = built([1.0] * 40, [1.0] * 40, [1.0], D, dtype, wide=False)
+    g = torch.Generator(device="cuda").manual_seed(zero + 9)
+    code = (zero & 15) * 17
+    s["k"].fill_(code)
+    s["k"][..., 3] = code if not other else ((zero & 15) << 4) | ((zero + (1 if zero < 7 else -1)) & 15)
+    s["kp"][:] = words(torch.full_like(s["kp"], 1.0, dtype=torch.float64), torch.full_like(s["kp"], zero))
+    s["q"].normal_(0.0, 4.0, generator=g)
+    s["scale"] = D ** -0.5
+    out, lse, _ = attend(s)
+    _, want, _, _, _ = reference(s)
+    q = s["q"].double().abs()
+    small = D * 2.0 ** -23 * q[..., 6] * s["scale"] * other + 2.0 ** -20 * (1 + want.abs())
+    bound = small + D * 2.0 ** -23 * 15 * q.sum(-1) * s["scale"]
+    assert bool(((lse - want).abs() <= bound).all()), float(((lse - want).abs() / bound).max())
