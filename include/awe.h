@@ -501,7 +501,7 @@ typedef struct {
     const float* scale_dev;  /* n_adapters, or NULL: 1                                                   */
     int64_t n_adapters;
     int64_t rank;            /* a multiple of 8, at most 128; smaller adapters are filled up with zeros   */
-    int64_t N, K;            /* K a multiple of 8                                                        */
+    int64_t N, K;            /* K a multiple of 8; both below 2^31 - 65,536                              */
     int32_t type;
 } awe_adapters;
 

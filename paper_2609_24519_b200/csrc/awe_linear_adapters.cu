@@ -603,7 +603,8 @@ extern "C" awe_status_t awe_linear_adapters(awe_handle_t h, const awe_adapters* 
     if (!h || !L || !L->a_dev || !L->b_dev || L->n_adapters <= 0 || L->rank <= 0 || L->N <= 0 || L->K <= 0 || T < 0 || B < 0) return AWE_ERR_INVALID_ARG;
     if (L->type < AWE_F16 || L->type > AWE_F32 || (int)y_type < AWE_F16 || (int)y_type > AWE_F32) return AWE_ERR_INVALID_ARG;
     if (!is_half_type(L->type) || ((int)y_type != L->type && y_type != AWE_F32) || L->rank > 128 || L->rank % 8 || L->K % 8) return AWE_ERR_UNSUPPORTED;
-    if (L->N > INT32_MAX - 4096 || L->K > INT32_MAX - 65536 || T > INT32_MAX - 64 || B > AWE_KV_MAX_REQUESTS) return AWE_ERR_UNSUPPORTED;
+    // columns are counted in 32 bits, and loops look up to 32,768 of them beyond the last (copy_base: 16 blocks' threads, eight elements each)
+    if (L->N > INT32_MAX - 65536 || L->K > INT32_MAX - 65536 || T > INT32_MAX - 64 || B > AWE_KV_MAX_REQUESTS) return AWE_ERR_UNSUPPORTED;
     if (T == 0 || B == 0) return AWE_OK;
     if (!x_dev || !y_dev || !q_start_dev || !adapter_dev || (T > 1 && (ldx < L->K || ldy < L->N || (base_dev && ldb < L->N))) ||
         (base_dev == y_dev && T > 1 && ldb != ldy))
