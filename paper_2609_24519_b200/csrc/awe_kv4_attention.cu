@@ -650,7 +650,7 @@ extern "C" awe_status_t awe_kv4_attention(awe_handle_t h, const awe_kv4_cache* c
     if (workspace_bytes < awe_kv4_attention_workspace_bytes(h, cache, T, n_q_heads, B)) return AWE_ERR_WORKSPACE;
     p.k = reinterpret_cast<const int8_t*>(cache->k_dev), p.v = reinterpret_cast<const int8_t*>(cache->v_dev);
     p.k_param = cache->k_param_dev, p.v_param = cache->v_param_dev;
-    if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, window))
+    if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, p.window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, true, workspace_dev, (cudaStream_t)stream);
     const int nt = row_tiles(T, B, p.group, cache->head_dim);
     const int blocks = blocks_of(h->sm_count, cache->head_dim, nt);

@@ -457,7 +457,7 @@ awe_status_t attention_params(AttnParams& p, bool& empty, const void* q_dev, awe
     p.scale_log2 = scale * 1.4426950408889634f;
     p.B = (int)B, p.heads = (int)n_heads, p.group = (int)(n_q_heads / n_heads), p.page_log2 = page_log2;
     p.n_pages = (int)n_pages, p.max_pages = (int)max_pages, p.causal = causal != 0;
-    p.window = window;
+    p.window = std::min(window, (int64_t)INT32_MAX);  // no context is longer, and the sums that a kernel is chosen by stay in 64 bits
     return AWE_OK;
 }
 }  // namespace awe
@@ -489,7 +489,7 @@ extern "C" awe_status_t awe_kv_attention(awe_handle_t h, const awe_kv_cache* cac
     if (s != AWE_OK || empty) return s;
     if (workspace_bytes < awe_kv_attention_workspace_bytes(h, cache, T, n_q_heads, B)) return AWE_ERR_WORKSPACE;
     p.k = cache->k_dev, p.v = cache->v_dev, p.k_scale = cache->k_scale_dev, p.v_scale = cache->v_scale_dev;
-    if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, window))
+    if (use_tc(*cache, T, B, n_q_heads, p.group, max_pages * cache->page_size, p.window))
         return kv_attention_tc(h, p, cache->head_dim, type == AWE_BF16, false, workspace_dev, (cudaStream_t)stream);
     const int nt = row_tiles(T, B, p.group, cache->head_dim);
     place_few(p, kStepTokens, blocks_of(h->sm_count, cache->head_dim, nt), nt, cache->head_dim, max_pages * cache->page_size, workspace_dev);

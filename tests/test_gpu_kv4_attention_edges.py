@@ -1,19 +1,21 @@
-"""Attention over the 4-bit cache where it can go wrong: references of the softmax that move inside a step.
+"""Attention over the 4-bit cache where it can go wrong: references of the softmax that move inside a step, scales far apart, the largest sizes.
 
-The scores are built: one dimension of the keys carries them, each a value that the format holds, and the reference computes from the
+In most the scores are built: one dimension of the keys carries them, each a value that the format holds, and the reference computes from the
 stored bytes in 64 bits.  Tolerance, with u the unit roundoff of the output type, p_j the probabilities and P the largest: a weight is rounded to
 FP16, the largest standing between 2^9 and 2^15, so by 2^-11 of itself, or by 2^-25 <= 2^-34 P where it is below 2^-14, which p_j >= 2^-23 P is not;
 FP32 sums and exponentials add less than 2^-14 for the scores here (below 2^6, so that 2^-14 is many FP32 roundings of an exponent).  So
 |out - ref| <= u |ref| + (1 + u) ((2^-11 + 2^-14) sum_j p_j |v_j| + 2^-34 P sum_small |v_j|) + 2^-25, the last for FP16's subnormals."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2609_24519_b200 import binding as b
 
 from .gpu_util import handle
-from .test_gpu_kv4_attention import TORCH, values
+from .test_gpu_kv4_attention import TORCH, call, make, values
+from .test_gpu_kv_cache import make_cache, run_attention
 
 pytestmark = pytest.mark.gpu
 KINDS = [(64, b.F16), (128, b.BF16)]
@@ -177,3 +179,35 @@ def test_keys_whose_codes_are_their_zero_point_but_for_one_channel(other, zero, 
     small = D * 2.0 ** -23 * q[..., 6] * s["scale"] * other + 2.0 ** -20 * (1 + want.abs())
     bound = small + D * 2.0 ** -23 * 15 * q.sum(-1) * s["scale"]
     assert bool(((lse - want).abs() <= bound).all()), float(((lse - want).abs() / bound).max())
+
+
+LONGEST = [2 ** 31 - 1, 2 ** 31, 2 ** 62, 2 ** 63 - 129, 2 ** 63 - 1]
+
+
+@pytest.mark.parametrize("window", LONGEST)
+@pytest.mark.parametrize("new,ctx,width", [([1, 1], [9000, 8800], 563), ([1], [777], 49), ([600], [1500], 256)])
+def test_windows_longer_than_any_context(new, ctx, width, window):
+    """The same kernels and bits as without a window."""
+    s = make(new, ctx, 8, 2, 128, 16, b.BF16, width=width, seed=2)
+    launches = call(s)
+    out, lse = s["out"].clone(), s["lse"].clone()
+    s["window"] = window
+    assert call(s) == launches
+    assert torch.equal(out, s["out"]) and torch.equal(lse, s["lse"])
+
+
+@pytest.mark.parametrize("window", LONGEST)
+@pytest.mark.parametrize("rows,pages", [(1, 600), (300, 40)])
+def test_windows_longer_than_any_context_over_the_cache_of_8_bits(rows, pages, window):
+    rng = np.random.default_rng(rows)
+    cache = make_cache(rng, pages, 2, 16, 128)
+    q = torch.from_numpy(rng.standard_normal((rows, 8, 128)).astype(np.float32)).to(torch.bfloat16)
+    table = np.concatenate([rng.permutation(pages), np.full(0 if rows == 1 else 2000, -1)])[None]
+    args = (cache, q, "bf16", [0, rows], [16 * pages - 3], table, 128 ** -0.5)
+    counts = [b.awe_launch_count(handle())]
+    got = []
+    for w in (0, window):
+        got.append(run_attention(*args, window=w))
+        counts.append(b.awe_launch_count(handle()))
+    assert counts[1] - counts[0] == counts[2] - counts[1] == (3 if rows > 1 else 2)
+    assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
