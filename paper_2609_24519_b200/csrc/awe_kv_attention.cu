@@ -445,7 +445,7 @@ awe_status_t attention_params(AttnParams& p, bool& empty, const void* q_dev, awe
     if (!q_dev || !q_start_dev || !ctx_len_dev || !block_table_dev || !out_dev || !workspace_dev || n_q_heads <= 0 || n_q_heads % n_heads ||
         max_pages <= 0 || ld_table < max_pages || (T > 1 && (ldq < width || ldo < width)))
         return AWE_ERR_INVALID_ARG;
-    if (B > AWE_KV_MAX_REQUESTS || n_q_heads > 65535 || T * n_q_heads > INT32_MAX || max_pages > INT32_MAX / page_size) return AWE_ERR_UNSUPPORTED;
+    if (B > AWE_KV_MAX_REQUESTS || n_q_heads > 65535 || T > INT32_MAX / n_q_heads || max_pages > INT32_MAX / page_size) return AWE_ERR_UNSUPPORTED;
     if ((uintptr_t)q_dev % 16 || (uintptr_t)out_dev % 16 || ldq % 8 || ldo % 8 || (uintptr_t)workspace_dev % 256 ||
         (uintptr_t)q_start_dev % 4 || (uintptr_t)ctx_len_dev % 4 || (uintptr_t)block_table_dev % 4 || (uintptr_t)lse_dev % 4)
         return AWE_ERR_ALIGNMENT;

@@ -211,3 +211,14 @@ def test_windows_longer_than_any_context_over_the_cache_of_8_bits(rows, pages, w
         counts.append(b.awe_launch_count(handle()))
     assert counts[1] - counts[0] == counts[2] - counts[1] == (3 if rows > 1 else 2)
     assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("T", [2 ** 31, 2 ** 60, 2 ** 62 + 2, 2 ** 63 - 1])
+def test_more_queries_than_32_bits_count(T):
+    s = make([1], [20], 16, 2, 64, 16, b.F16)
+    s["T"] = T
+    cache = b.kv4_cache(s["k"], s["v"], s["kp"], s["vp"], s["pool"], 2, 16, 64)
+    with pytest.raises(b.AweError) as e:
+        b.awe_kv4_attention(handle(), cache, s["q"], b.F16, T, 16, 1024, s["start"], s["ctx_len"], 1, s["table"], s["width"], s["width"], 0.1, True, 0, s["out"],
+                            1024, s["lse"], s["k"], 2 ** 62)
+    assert e.value.status == 2
