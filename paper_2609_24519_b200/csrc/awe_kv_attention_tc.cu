@@ -560,7 +560,8 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
             int see_hi = p.causal ? (int)min((int64_t)u.ctx, place + 1) : u.ctx;
             const int see_lo = p.window > 0 && place + 1 > p.window ? (int)min(place + 1 - p.window, (int64_t)u.ctx) : 0;
             if (!live || see_hi < 0) see_hi = 0;
-            const int all_lo = __reduce_max_sync(~0u, live ? see_lo : 0), all_hi = __reduce_min_sync(~0u, live ? see_hi : 0x7FFFFFFF);
+            // steps that begin in [all_lo, whole_hi] are seen whole by all rows (their ends may pass 32 bits)
+            const int all_lo = __reduce_max_sync(~0u, live ? see_lo : 0), whole_hi = __reduce_min_sync(~0u, live ? see_hi : 0x7FFFFFFF) - kStep;
             float m_ref = -INFINITY, sum = 0.0f;
             if constexpr (kFour) cq = factor_of(1.0f, cq);
             else sh->unvalued_sum[128 * t + row] = make_float2(-INFINITY, 0.0f);  // this thread's alone
@@ -570,7 +571,7 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
                 if (!__all_sync(~0u, wait(sh->c_full[step & 3], (step >> 2) & 1, 36) && wait(sh->s_full[t], done & 1, 37))) return false;
                 ptx::tc_fence_after();
                 const uint32_t no_page = kFour ? sh->unvalued[step & 3] : 0;  // of 8 bits the constants hide such tokens
-                const bool cut = tok0 < all_lo || tok0 + kStep > all_hi || no_page;
+                const bool cut = tok0 < all_lo || tok0 > whole_hi || no_page;
                 auto rescale = [&](float shrink) {  // of O, once the products of the step before are in it
                     if (!__all_sync(~0u, wait(sh->o_done[t], (done - 1) & 1, 38))) return false;
                     ptx::tc_fence_after();

@@ -28,7 +28,7 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int b) {
     r.ctx = (int)min((int64_t)max(p.ctx_len[b], 0), (int64_t)p.max_pages << p.page_log2);
     const int64_t first = (int64_t)p.ctx_len[b] - r.n + 1 - p.window;  // first token that any of its queries sees
     r.lo = p.window > 0 && first > 0 ? (int)min(first, (int64_t)r.ctx) & ~(kStepTokens - 1) : 0;
-    r.steps = max((r.ctx - r.lo + kStepTokens - 1) / kStepTokens, 1);  // one at least: its rows are to be written
+    r.steps = max((int)(((unsigned)(r.ctx - r.lo) + kStepTokens - 1) / kStepTokens), 1);  // one at least: its rows are to be written
     r.units = (r.n * p.group + kRows - 1) / kRows * p.heads;
     return r;
 }

@@ -222,3 +222,53 @@ def test_more_queries_than_32_bits_count(T):
         b.awe_kv4_attention(handle(), cache, s["q"], b.F16, T, 16, 1024, s["start"], s["ctx_len"], 1, s["table"], s["width"], s["width"], 0.1, True, 0, s["out"],
                             1024, s["lse"], s["k"], 2 ** 62)
     assert e.value.status == 2
+
+
+def long_call(four, D, pool, table, q, new, ctx, window):
+    """One request over a pool of pages of 16 tokens and one head; q: new x Hq x D BF16."""
+    page, Hq = 16, q.shape[1]
+    g = torch.Generator(device="cuda").manual_seed(D)
+    if four:
+        s = make([1], [16 * pool - 32], 1, 1, D, page, b.BF16, seed=D)
+        assert s["pool"] == pool
+        cache = b.kv4_cache(s["k"], s["v"], s["kp"], s["vp"], pool, 1, page, D)
+        size, attention = b.awe_kv4_attention_workspace_bytes, b.awe_kv4_attention
+    else:
+        k, v = (torch.randint(-127, 128, (pool, 1, page, D), generator=g, device="cuda", dtype=torch.int8) for _ in range(2))
+        scales = torch.full((pool, 1), 0.02, device="cuda")
+        cache = b.kv_cache(k, v, scales, scales, pool, 1, page, D)
+        size, attention = b.awe_kv_attention_workspace_bytes, b.awe_kv_attention
+    ws = torch.empty(size(handle(), cache, new, Hq, 1), dtype=torch.uint8, device="cuda")
+    start, length = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, new], [ctx]))
+    out, lse = torch.empty_like(q), torch.empty((new, Hq), device="cuda")
+    width = table.numel()
+    before = b.awe_launch_count(handle())
+    attention(handle(), cache, q, b.BF16, new, Hq, Hq * D, start, length, 1, table, width, width, D ** -0.5, True, window, out, Hq * D, lse, ws)
+    torch.cuda.synchronize()
+    assert b.awe_last_device_status(handle()) == (0, 0)
+    return out, lse, b.awe_launch_count(handle()) - before
+
+
+@pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("new,window", [(3, 300), (700, 1000), (1, 0)])
+def test_contexts_that_end_16_tokens_below_2_to_the_31(new, window, four):
+    """With a window as a short context that ends alike; the whole of it as one page that 2^27 - 1 table entries name: its logarithm is the page's and
+    that of their number, but for the sum of so many FP32 terms."""
+    n, D = 2 ** 27 - 1, 64
+    g = torch.Generator(device="cuda").manual_seed(new)
+    q = torch.empty((new, 8, D), device="cuda").normal_(generator=g).to(torch.bfloat16)
+    if window:
+        table = torch.arange(n, dtype=torch.int32, device="cuda").remainder_(40)
+        out, lse, launches = long_call(four, D, 40, table, q, new, 16 * n, window)
+        assert (launches == 3) == (new == 700)
+        # the same steps: 2,160 tokens end as far behind a multiple of 128 as 2^31 - 16 do
+        short = table[-135:].clone()
+        want, want_lse, launches = long_call(four, D, 40, torch.cat([short, short.new_full((5000,), -1)]), q, new, 16 * 135, window)
+        assert (launches == 3) == (new == 700)
+        assert torch.equal(lse, want_lse) and torch.equal(out, want)
+    else:
+        table = torch.zeros(n, dtype=torch.int32, device="cuda")
+        out, lse, _ = long_call(four, D, 40, table, q, new, 16 * n, 0)
+        want, want_lse, _ = long_call(four, D, 40, table[:1], q, new, 16, 0)
+        assert float((lse - want_lse - math.log(n)).abs().max()) < 0.02
+        assert float((out.double() - want.double()).abs().max()) <= 0.02 * float(want.abs().max())
