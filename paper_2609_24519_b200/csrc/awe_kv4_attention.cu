@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
         // ---- the query rows, as the matrix instruction's 16 x 8 operand: thread (g, t) holds of row g the dimensions t kD / 4 and
         // following, eight at a time in the order of the codes' pairs
         uint32_t qf[kNT][kSteps16][2];
-        float cq[kNT][2];                    // factor of the scores of columns 2t, 2t + 1, for scales that come 16 times and codes that come 2^-22 times
+        float cq[kNT][2];                    // factor of the scores of columns 2t, 2t + 1
         float q_sum[kNT][2];                 // sums of those columns' queries, 2^-22 times
         int see_lo[kNT][2], see_hi[kNT][2];  // tokens [see_lo, see_hi) are visible
 #pragma unroll
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
             const bool live = 8 * nt + g < n_rows;
             const int query = live ? row / p.group : 0, qh = head * p.group + (live ? row % p.group : 0);
             const T16* src = reinterpret_cast<const T16*>(p.q) + (int64_t)(r.q0 + query) * p.ldq + (int64_t)qh * kD + t * (kD / 4);
-            float factor = p.scale_log2 * 262144.0f;
+            float factor = p.scale_log2;
 #pragma unroll
             for (int w = 0; w < kWords; ++w) {
                 uint4 x = make_uint4(0, 0, 0, 0);
@@ -293,10 +293,12 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
             next_page0 = page_of(i + C::kStages, 0), next_page1 = page_of(i + C::kStages, 1);
             const uint32_t stage = read_at;
             const uint2 pages = lds64(stage + C::kPageAt);
-            // each lane prepares a token of the 32: 16 times its key's scale, zero + 8, the exponent that is its value's scale, and that back
+            // each lane prepares a token of the 32: its key's scale, 2^22 times for codes that come 2^-22 times (here and not in the queries' factor,
+            // which may stand at the end of FP32's range: the sum is brought to its size before that), zero + 8, the exponent that is its value's scale, and that back
             const uint32_t words = lds16(stage + C::kParamAt + 2 * lane) | lds16(stage + C::kParamAt + 64 + 2 * lane) << 16;
             const float2 own_scales = scales16(words);
-            const float own_zero = kv4_zeros8(words).x, own_log2 = log2_approx(own_scales.y) - 4.0f, own_back = exp2_approx(-own_log2);
+            const float own_key = own_scales.x * 262144.0f, own_zero = kv4_zeros8(words).x, own_log2 = log2_approx(own_scales.y) - 4.0f,
+                        own_back = exp2_approx(-own_log2);
             read_at = read_at + C::kStageBytes == ring + C::kStages * C::kStageBytes ? ring : read_at + C::kStageBytes;
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
@@ -356,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int from = 16 * part + 8 * j + g;
-                    ks[j] = __shfl_sync(~0u, own_scales.x, from), kz[j] = __shfl_sync(~0u, own_zero, from);
+                    ks[j] = __shfl_sync(~0u, own_key, from), kz[j] = __shfl_sync(~0u, own_zero, from);
                     lv[j] = __shfl_sync(~0u, own_log2, from), back[j] = __shfl_sync(~0u, own_back, from);
                 }
                 const int tok = tile + g;
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                 for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        s[nt][j] = fmaf(fmaf(-kz[j >> 1], q_sum[nt][j & 1], s[nt][j] + s_odd[nt][j]), ks[j >> 1] * cq[nt][j & 1], lv[j >> 1]);
+                        s[nt][j] = fmaf(fmaf(-kz[j >> 1], q_sum[nt][j & 1], s[nt][j] + s_odd[nt][j]) * ks[j >> 1], cq[nt][j & 1], lv[j >> 1]);
                 if (tile < sees.all_lo || tile + 16 > sees.all_hi) {
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt)

@@ -272,3 +272,18 @@ def test_contexts_that_end_16_tokens_below_2_to_the_31(new, window, four):
         want, want_lse, _ = long_call(four, D, 40, table[:1], q, new, 16, 0)
         assert float((lse - want_lse - math.log(n)).abs().max()) < 0.02
         assert float((out.double() - want.double()).abs().max()) <= 0.02 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("exponent,scale", [(e, s) for e in (100, 120, 125, 126, -100, -120) for s in (1.0, 0.125, 2.0 ** -20)
+                                            if 4 * 2.0 ** e * s < 2.0 ** 128])  # the score in the kernel's unit
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_queries_at_the_ends_of_the_range(D, exponent, scale):
+    """BF16 queries of one element 2^exponent: one token's score is that times scale and the others' are 0, or all are 0 but for bits that count
+    for nothing.  Finite, and the one token's values alone where its score is large."""
+    s = built([0.0] * 9 + [8.0] + [0.0] * 30, [1.0] * 40, [1.0], D, b.BF16, wide=False)
+    s["q"][:, :, 0] = 2.0 ** exponent
+    s["scale"] = scale * math.log(2.0)
+    out, lse, _ = attend(s)
+    want, want_lse, size, _, _ = reference(s)
+    assert bool(((out - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -14) * (1 + 2.0 ** -8) * size).all())
+    assert bool(((lse - want_lse).abs() <= 2.0 ** -14 + 2.0 ** -21 * want_lse.abs()).all())
