@@ -41,7 +41,7 @@ namespace {
 using namespace serve;
 using namespace attn_few;
 
-constexpr float kNoneSeen = -3.0e38f;  // the reference of a row that has seen nothing: below every score, and not the -inf of hidden ones
+constexpr float kNoneSeen = -3.402823466e38f;  // the reference of a row that has seen nothing: the lowest number, and not the -inf of hidden scores
 constexpr int kTile = 32;  // tokens of a warp's tile: two pieces of 16, which may lie in two pages
 constexpr int kStepTokens = kTile * kWarps;
 

@@ -287,3 +287,16 @@ def test_queries_at_the_ends_of_the_range(D, exponent, scale):
     want, want_lse, size, _, _ = reference(s)
     assert bool(((out - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -14) * (1 + 2.0 ** -8) * size).all())
     assert bool(((lse - want_lse).abs() <= 2.0 ** -14 + 2.0 ** -21 * want_lse.abs()).all())
+
+
+@pytest.mark.parametrize("n", [1, 40, 300])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_scores_next_to_the_lowest_number(D, n):
+    """Every token's score is -3.75 2^126 = -3.19e38: they weigh alike."""
+    s = built([7.6] * n, [1.0] * n, [1.0], D, b.BF16, wide=False)
+    s["q"][:, :, 0] = -2.0 ** 126
+    out, lse, _ = attend(s)
+    want, want_lse, size, _, _ = reference(s)
+    assert bool((want_lse / math.log(2.0) < -3.1e38).all())
+    assert bool(((out - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -14) * (1 + 2.0 ** -8) * size).all())
+    assert bool(((lse - want_lse).abs() <= 2.0 ** -21 * want_lse.abs()).all())
