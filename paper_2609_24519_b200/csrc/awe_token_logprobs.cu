@@ -8,9 +8,12 @@
 // The most likely tokens.  The top_k-th largest of a block's 256 thread maxima is a bound that top_k elements reach, and few others do:
 // the threads whose maximum reaches it have their elements looked at again (in the cache) by their warp, which gathers those that do, some 22 for
 // 20; each of them finds its place by counting the ones before it.  Blocks' lists are joined in pairs: of two lists in order, the larger of a[i]
-// and b[31 - i] are the best 32, in an order that five exchanges sort.  Where more are gathered than there is room for (many equal logits), all
-// warps look at all elements again: each keeps its best so far in order, one a lane, and inserts what reaches the bound, which its own list and
-// the others' raise.  (A looser bound from each warp's maxima alone saves the joining of eight lists, but gathers more: 17.5 -> 23 us.)
+// and b[31 - i] are the best 32, in an order that five exchanges sort.  Where more reach the bound than there is room for (constrained rows, of
+// which few tokens are not masked, or equal logits: a warp all of whose threads reach it says so without looking), what lies above the bound is
+// gathered alone, and then the lowest tokens at the bound, found by a count in the tokens' order, which ends where there are enough.  128 rows of 131,072
+// (BF16), 10 tokens left and 20 alternatives: 21 us (each element gathered or inserted: 105).  Where even above the bound there are too many (they
+// lie with few threads), all warps look at all elements again: each keeps its best so far in order, one a lane, and inserts what reaches the
+// bound, which its own list and the others' raise.  (A looser bound from each warp's maxima alone saves the joining of eight lists, but gathers more: 17.5 -> 23 us.)
 //
 // HBM bounds many rows; a single row is spread over a cluster of blocks that join in shared memory, which bounds it by latency.
 // 2,048 rows of 50,257 (FP16): 44 us = 4.7 TB/s, with 77 % of the issue slots and 61 % of the exponentials' rate; 128 rows of 131,072 (BF16) with 20
@@ -154,8 +157,9 @@ __device__ __forceinline__ int ordered(float x) {
 __device__ __forceinline__ float from_ordered(int b) { return __int_as_float(b < 0 ? b ^ 0x7FFFFFFF : b); }
 
 // grid: a cluster for each row.
+// Six blocks on an SM: the compiler takes no more than 40 registers then (with 48, five blocks: 2,048 rows of 50,257 take 2 % longer).
 template <int kType, bool kTop>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const LogprobParams p) {
     using P = Piece<kType>;
     using T = typename P::T;
     __shared__ Shared sh;
@@ -266,8 +270,20 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
                 __syncthreads();
             }
         }
-        // of one alternative it is the block's maximum, of a row with a NaN anything that is reached
-        float bound = p.top > 1 ? sh.maxima[0][p.top - 1] : (most_of_block == 0x7FFFFFFF ? -INFINITY : from_ordered(most_of_block));
+        // of one alternative it is the block's maximum, beside a NaN that of the threads that have none
+        if (p.top == 1) {
+            m = from_ordered(most_of_block);
+            if (most_of_block == 0x7FFFFFFF) {
+                if (tid == 0) sh.bound = ordered(-INFINITY);
+                __syncthreads();
+                atomicMax(&sh.bound, ordered(thread_most));
+                __syncthreads();
+                m = from_ordered(sh.bound);
+                __syncthreads();
+                if (tid == 0) sh.bound = ordered(-INFINITY);
+            }
+        }
+        float bound = p.top > 1 ? sh.maxima[0][p.top - 1] : m;
         // ---- what reaches it
         auto gather = [&](float logit, int id) {
             if (!(logit >= bound)) return;
@@ -277,7 +293,12 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         // A thread's pieces are looked at by its whole warp, one each; of two threads they are on their way together.  (With four a single row
         // takes 0.4 us less, but a block leaves less room for others: 2,048 rows of 50,257 take 52 us instead of 44.)
         constexpr int kAhead = 2;
-        for (unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound); ask;) {
+        unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound);
+        if (ask == ~0u) {  // all of a warp's threads: a row of which few tokens are left, or all are alike (the bound is then what the others have)
+            ask = 0;
+            if (lane == 0) atomicAdd(&sh.gathered, kRoom + 1);
+        }
+        while (ask) {
             int first[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) first[k] = ask ? begin + 32 * warp + __ffs(ask) - 1 : end, ask &= ask - 1;
@@ -305,7 +326,32 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
         }
         at_ends(gather);
         __syncthreads();
-        const int gathered = sh.gathered;
+        int gathered = sh.gathered;
+        const bool crowded = gathered > kRoom;
+        if (crowded) {  // again, what lies above the bound: beside that the lowest tokens at the bound are the best
+            __syncthreads();
+            if (tid == 0) sh.gathered = 0;
+            sh.found[tid] = {-INFINITY, kNoToken};
+            __syncthreads();
+            const float at_bound = bound;
+            // the next number: of 0 the smallest above both zeros, of infinity a NaN, which nothing reaches
+            bound = from_ordered(ordered(bound + 0.0f) + 1);
+#pragma unroll 1
+            for (unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound); ask; ask &= ask - 1) {
+                const int first = begin + 32 * warp + __ffs(ask) - 1;
+#pragma unroll 1
+                for (int i = first + kThreads * lane; i < end; i += kThreads * 32) {
+                    const uint4 w = __ldg(from + i);
+#pragma unroll 1
+                    for (int e = 0; e < P::kCount; ++e) gather(P::pick(w, e), head + i * P::kCount + e);
+                }
+                if (*(volatile int*)&sh.gathered > kRoom) break;
+            }
+            at_ends(gather);
+            bound = at_bound;
+            __syncthreads();
+            gathered = sh.gathered;
+        }
         one_list = gathered <= kRoom;
         if (one_list) {
             if (tid < gathered) {
@@ -319,9 +365,42 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobP
                 sh.list[0][tid] = best;  // nothing
             }
             __syncthreads();
+            if (crowded) {
+                int have = gathered;  // places taken
+                auto add_ties = [&](unsigned hits, int first_id) {  // hits: which of this thread's elements from first_id on; threads in the tokens' order
+                    int upto = __popc(hits);
+#pragma unroll 1
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int o = __shfl_up_sync(~0u, upto, d);
+                        if (lane >= d) upto += o;
+                    }
+                    if (lane == 31) sh.most[warp] = upto;
+                    __syncthreads();
+                    int place = have + upto - __popc(hits);
+#pragma unroll 1
+                    for (int i = 0; i < kWarps; ++i) {
+                        if (i < warp) place += sh.most[i];
+                        have += sh.most[i];
+                    }
+                    for (; hits && place < p.top; hits &= hits - 1) sh.list[0][place++] = {bound, first_id + __ffs(hits) - 1};
+                    __syncthreads();
+                };
+                if (rank == 0) add_ties(tid < head && P::one(x + tid) == bound, tid);
+#pragma unroll 1
+                for (int i0 = begin; i0 < end && have < p.top; i0 += kThreads) {
+                    unsigned hits = 0;
+                    if (i0 + tid < end) {
+                        const uint4 w = __ldg(from + i0 + tid);
+#pragma unroll
+                        for (int e = 0; e < P::kCount; ++e) hits |= (unsigned)(P::at(w, e) == bound) << e;
+                    }
+                    add_ties(hits, head + (i0 + tid) * P::kCount);
+                }
+                if (rank == parts - 1) add_ties(tid < p.V - tail_at && P::one(x + tail_at + tid) == bound, tail_at + tid);
+            }
             best = sh.list[0][lane];
         } else {
-            // Too many: every warp inserts what it finds among its elements into a list of its own.
+            // Too many there, too: every warp inserts what it finds among its elements into a list of its own.
             auto look = [&](float logit, int id, bool live) {
                 const Entry mine = {logit, id};
                 const bool reaches = live && logit >= bound;
