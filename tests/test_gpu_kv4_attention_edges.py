@@ -300,3 +300,34 @@ def test_scores_next_to_the_lowest_number(D, n):
     assert bool((want_lse / math.log(2.0) < -3.1e38).all())
     assert bool(((out - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -14) * (1 + 2.0 ** -8) * size).all())
     assert bool(((lse - want_lse).abs() <= 2.0 ** -21 * want_lse.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [b.F16, b.BF16])
+@pytest.mark.parametrize("new,ctx,D", [(1, 777, 64), (1, 3000, 128), (2, 900, 256), (600, 1500, 128), (1024, 1024, 64)])
+@pytest.mark.parametrize("spread", [0.1, 1.0, 6.0])
+def test_errors_as_a_root_mean_square(spread, new, ctx, D, dtype):
+    """Weights are off by 2^-11 of themselves at most and independently of one another, so that an output's error has a root mean square below
+    2^-11 sqrt(sum (p v)^2), and its rounding one below u |out|.  A score of S in base 2 is rounded by 2^-24 S, a few times over, which with the
+    exponentials and the sums is less than 2^-16 of a weight up to S = 2^6 (ln 2 2^-18 a rounding) and in proportion above.  Two floors: weights below
+    2^-23 of the largest, P, are off by 2^-34 P (as above; for few rows of the largest product with a value's scale, and scales differ by less than
+    2^5 here), and FP16 outputs below its normal range by 2^-25."""
+    s = make([new], [ctx], 8, 2, D, 16, dtype, seed=D + new, spread=spread, width=4096 // 16 if new > 2 else None)
+    assert (call(s) == 3) == (new > 2)
+    u = torch.finfo(TORCH[dtype]).eps / 2
+    pages = s["table"][0, :-(-ctx // 16)].long()
+    hidden = torch.arange(ctx, device="cuda") > torch.arange(ctx - new, ctx, device="cuda")[:, None]
+    total = count = 0.0
+    for h in range(2):
+        k, v = (values(s[a][pages, h], s[a + "p"][pages, h]).reshape(-1, D)[:ctx] for a in "kv")
+        for i in range(4 * h, 4 * h + 4):
+            x = (s["q"][:, i * D:(i + 1) * D].double() @ k.t() * s["scale"]).masked_fill(hidden, -math.inf)
+            p = torch.softmax(x, 1)
+            want = p @ v
+            most, high = p.amax(1, keepdim=True), max(1.0, float(x.masked_fill(hidden, 0.0).abs().max()) / math.log(2.0) / 2 ** 6)
+            floor = 2.0 ** -34 * (2 ** 5 if new <= 2 else 1) * most * ((p < 2.0 ** -23 * most).double() @ v.square()).sqrt() + 2.0 ** -25
+            size = 2.0 ** -11 * (p.square() @ v.square()).sqrt() + u * want.abs() + 2.0 ** -16 * high * (p @ v.abs()) + floor
+            total += float(((s["out"][:new, i * D:(i + 1) * D].double() - want) / size).square().sum())
+            count += want.numel()
+            lse = torch.logsumexp(x, 1)
+            assert float((s["lse"][:new, i].double() - lse).square().mean().sqrt()) <= 2.0 ** -18 * high + 2.0 ** -22 * float(lse.abs().max())
+    assert math.sqrt(total / count) <= 1.0

@@ -97,3 +97,21 @@ def test_same_bits_again():
     first, again = (call(x, 50257, b.BF16, 20) for _ in range(2))
     for k in first:
         assert torch.equal(first[k], again[k]), k
+
+
+@pytest.mark.parametrize("dtype", [b.BF16, b.F32])
+@pytest.mark.parametrize("T,V", [(64, 131072), (400, 32003)])
+@pytest.mark.parametrize("spread", [0.1, 2.0])
+def test_errors_of_many_tokens_as_a_root_mean_square(spread, T, V, dtype):
+    """Of lse: its own rounding (below 16) 2^-21, the logarithm's 2^-20 (z below 12), the factor's, 2^-24 of t, whose mean is below log2 V ln 2 < 12,
+    2^-20.4, the exponentials' bias 2^-22, and the sums': 512 additions of a thread are off by sqrt(512) 2^-24 of it as a root mean square, 256
+    threads' together by 2^-23.5.  In all 2.6 2^-20.  Log probabilities (below 32) round by 2^-20 more; the entropy takes the factor's and the
+    exponentials' errors times t once more, and its quotient's (below 17, times ln 2) 2^-21: below 4 2^-20."""
+    x = logits(T, V, dtype, seed=V, spread=spread)
+    out = call(x, V, dtype, 4)
+    logp = torch.log_softmax(x.double(), 1)
+    rms = lambda e: float(e.square().mean().sqrt())  # noqa: E731
+    assert rms(out["lse"].double() - torch.logsumexp(x.double(), 1)) <= 2.6 * 2.0 ** -20
+    assert rms(out["logprob"].double() - logp.gather(1, out["tokens"].long()[:, None])[:, 0]) <= 3.6 * 2.0 ** -20
+    assert rms(out["top_logprob"].double() - logp.gather(1, out["top_id"].long())) <= 3.6 * 2.0 ** -20
+    assert rms(out["entropy"].double() + (logp.exp() * logp).sum(1)) <= 4 * 2.0 ** -20
