@@ -51,7 +51,7 @@ constexpr int kMostCluster = 8;
 template <int kD, int kNT>
 struct Config {
     static constexpr int kRows = 8 * kNT;
-    static constexpr int kStages = kD == 64 ? 5 : kD == 128 ? 3 : 3;
+    static constexpr int kStages = kD == 64 ? 5 : 3;
     static constexpr int kRowBytes = kD / 2, kHalfBytes = 16 * kRowBytes;  // of 16 tokens' keys or values
     static constexpr int kValueAt = 2 * kHalfBytes, kParamAt = 4 * kHalfBytes;  // behind the keys; behind those the words of keys, then of values
     static constexpr int kPageAt = kParamAt + 128, kStageBytes = kPageAt + 16;  // the two pages

@@ -38,11 +38,7 @@ using namespace serve;
 
 constexpr int kRows = 256;      // query rows of a unit
 constexpr int kStep = 128;      // tokens of a step
-constexpr int kSoftWarps = 8;
-template <bool kFour>
-struct Warps {
-    static constexpr int kUnpack = 4, kMultiplier = kSoftWarps + kUnpack, kThreads = 32 * (kMultiplier + 1);
-};
+constexpr int kSoftWarps = 8, kUnpackWarps = 4, kMultiplier = kSoftWarps + kUnpackWarps, kThreads = 32 * (kMultiplier + 1);
 constexpr int kTmemCols = 512;
 constexpr int kPlanThreads = 1024;
 
@@ -213,8 +209,7 @@ __device__ __forceinline__ void add_unvalued(Shared* sh, uint32_t groups, int sl
 }
 
 template <int kD, bool kBf16, bool kFour>
-__global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
-    constexpr int kUnpackWarps = Warps<kFour>::kUnpack, kMultiplier = Warps<kFour>::kMultiplier;
+__global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
     using C = Config<kD>;
     using T16 = typename Half<kBf16>::type;
     const AttnParams& p = tp.a;
@@ -325,7 +320,7 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
         }
     } else if (kFour && warp >= kSoftWarps) {  // ---- unpack keys and values of 4 bits
         constexpr int kPieces = kD / 32;  // 16-byte pieces per token
-        constexpr int kPassRows = 32 * kUnpackWarps / kPieces, kPasses = (kStep + kPassRows - 1) / kPassRows;  // tokens per pass, the last not whole
+        constexpr int kPassRows = 32 * kUnpackWarps / kPieces, kPasses = kStep / kPassRows;  // tokens per pass
         const int thread = tid - 32 * kSoftWarps, c = thread % kPieces, r = thread / kPieces;
         uint32_t step = 0;
         for_parts([&](const Unit& u, int head, int s0, int s1) {
@@ -346,7 +341,7 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
                 const int place = (u.lo + j * kStep) & ((1 << p.page_log2) - 1);
 #pragma unroll
                 for (int i = 0; i < kPasses; ++i) {
-                    const int row = i * kPassRows + r, page = __shfl_sync(~0u, pages, row >> 4);  // a lane behind the eighth has none
+                    const int row = i * kPassRows + r, page = __shfl_sync(~0u, pages, row >> 4);
                     const uint32_t block = (uint32_t)(page * p.heads + head) << p.page_log2;
                     at[i] = page < 0 ? ~0u : block + ((place + row) & ((1 << p.page_log2) - 1));
                 }
@@ -366,7 +361,6 @@ __global__ void __launch_bounds__(Warps<kFour>::kThreads, 1) kv_attention_tc_ker
 #pragma unroll
                 for (int i = 0; i < kPasses; ++i) {
                     const int row = i * kPassRows + r;
-                    if (row >= kStep) break;
                     if (swap) x[i] = make_uint4(x[i].z, x[i].w, x[i].x, x[i].y);
                     const __half2 scale = __float2half2_rn(kv4_scale(words[i]));
                     const Kv4Zeros zero(__byte_perm(words[i], 0, 0x1010));
@@ -861,7 +855,7 @@ cudaError_t launch(const TcAttnParams& p, int device, cudaStream_t st) {
     cudaError_t e = allow_smem(kv_attention_tc_kernel<kD, kBf16, kFour>, C::kSmemBytes, device, done);
     if (e != cudaSuccess) return e;
     if ((e = launch_early(kv_attention_units_kernel, dim3(1), kPlanThreads, 0, st, p)) != cudaSuccess) return e;
-    if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16, kFour>, dim3(p.a.blocks), Warps<kFour>::kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
+    if ((e = launch_early(kv_attention_tc_kernel<kD, kBf16, kFour>, dim3(p.a.blocks), kThreads, C::kSmemBytes, st, p)) != cudaSuccess) return e;
     const int64_t items = p.a.T * p.a.heads * p.a.group;
     return launch_early(kv_attention_tc_join_kernel<kD, kBf16>, dim3((unsigned)((items + 3) / 4)), 128, 0, st, p);
 }
