@@ -10,10 +10,10 @@
 // 20; each of them finds its place by counting the ones before it.  Blocks' lists are joined in pairs: of two lists in order, the larger of a[i]
 // and b[31 - i] are the best 32, in an order that five exchanges sort.  Where more reach the bound than there is room for (constrained rows, of
 // which few tokens are not masked, or equal logits: a warp all of whose threads reach it says so without looking), what lies above the bound is
-// gathered alone, and then the lowest tokens at the bound, found by a count in the tokens' order, which ends where there are enough.  128 rows of 131,072
-// (BF16), 10 tokens left and 20 alternatives: 21 us (each element gathered or inserted: 105).  Where even above the bound there are too many (they
-// lie with few threads), all warps look at all elements again: each keeps its best so far in order, one a lane, and inserts what reaches the
-// bound, which its own list and the others' raise.  (A looser bound from each warp's maxima alone saves the joining of eight lists, but gathers more: 17.5 -> 23 us.)
+// gathered, and then the lowest tokens at the bound, found by a count in the tokens' order, which ends where there are enough.  Where too many lie
+// above it (with few threads), the top_k-th largest of those that found room is a larger bound, and so on.  128 rows of 131,072 (BF16), 10
+// tokens left and 20 alternatives: 19 us (each element gathered and then inserted into a list: 105).  (A looser bound from each warp's
+// maxima alone saves the joining of eight lists, but gathers more: 17.5 -> 23 us.)
 //
 // HBM bounds many rows; a single row is spread over a cluster of blocks that join in shared memory, which bounds it by latency.
 // 2,048 rows of 50,257 (FP16): 44 us = 4.7 TB/s, with 77 % of the issue slots and 61 % of the exponentials' rate; 128 rows of 131,072 (BF16) with 20
@@ -148,7 +148,7 @@ struct Shared {
     int most[kWarps];
     Sums block_sums;
     Entry block_list[32];
-    int bound;  // least of a full list's best top_k, as an ordered whole number
+    int bound;  // as an ordered whole number
 };
 __device__ __forceinline__ int ordered(float x) {
     const int b = __float_as_int(x);
@@ -157,9 +157,8 @@ __device__ __forceinline__ int ordered(float x) {
 __device__ __forceinline__ float from_ordered(int b) { return __int_as_float(b < 0 ? b ^ 0x7FFFFFFF : b); }
 
 // grid: a cluster for each row.
-// Six blocks on an SM: the compiler takes no more than 40 registers then (with 48, five blocks: 2,048 rows of 50,257 take 2 % longer).
 template <int kType, bool kTop>
-__global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogprobParams p) {
     using P = Piece<kType>;
     using T = typename P::T;
     __shared__ Shared sh;
@@ -169,7 +168,6 @@ __global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const Logpr
     const int64_t row = blockIdx.x / parts;
     const float c = p.scale * 1.44269504088896f;
     if constexpr (kTop) {
-        if (tid == 0) sh.bound = ordered(-INFINITY);
         sh.found[tid] = {-INFINITY, kNoToken};
     }
     __syncthreads();
@@ -190,8 +188,7 @@ __global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const Logpr
     }
 
     Sums own = {-INFINITY, 0.0f, 0.0f};
-    bool one_list = false;  // whether every warp has all of the block's
-    Entry best = {-INFINITY, kNoToken};  // this lane's of the warp's list
+    Entry best = {-INFINITY, kNoToken};  // this lane's of the list
     auto add = [&](const uint4& w, int count) {
         const float m = own.m == -INFINITY ? 0.0f : own.m;
 #pragma unroll
@@ -238,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const Logpr
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) most_of_block = max(most_of_block, sh.most[i]);
     const float thread_most = own.m == own.m ? own.m : -INFINITY;  // of a thread with a NaN it is not known
-    const bool looks_again = own.m != own.m;
+    const float asked_most = own.m == own.m ? own.m : INFINITY;  // its elements are looked at
     raise(own, from_ordered(most_of_block), c);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) own.s0 += __shfl_xor_sync(~0u, own.s0, d), own.s1 += __shfl_xor_sync(~0u, own.s1, d);
@@ -279,158 +276,114 @@ __global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const Logpr
                 atomicMax(&sh.bound, ordered(thread_most));
                 __syncthreads();
                 m = from_ordered(sh.bound);
-                __syncthreads();
-                if (tid == 0) sh.bound = ordered(-INFINITY);
             }
         }
-        float bound = p.top > 1 ? sh.maxima[0][p.top - 1] : m;
-        // ---- what reaches it
-        auto gather = [&](float logit, int id) {
-            if (!(logit >= bound)) return;
-            const int at = atomicAdd(&sh.gathered, 1);
-            if (at < kRoom) sh.found[at] = {logit, id};
-        };
-        // A thread's pieces are looked at by its whole warp, one each; of two threads they are on their way together.  (With four a single row
-        // takes 0.4 us less, but a block leaves less room for others: 2,048 rows of 50,257 take 52 us instead of 44.)
-        constexpr int kAhead = 2;
-        unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound);
-        if (ask == ~0u) {  // all of a warp's threads: a row of which few tokens are left, or all are alike (the bound is then what the others have)
-            ask = 0;
-            if (lane == 0) atomicAdd(&sh.gathered, kRoom + 1);
-        }
-        while (ask) {
-            int first[kAhead];
+        float least = p.top > 1 ? sh.maxima[0][p.top - 1] : m;
+        int gathered;
+        for (bool above = false;; above = true) {
+            // ---- what is `least` or more
+            auto gather = [&](float logit, int id) {
+                if (!(logit >= least)) return;
+                const int at = atomicAdd(&sh.gathered, 1);
+                if (at < kRoom) sh.found[at] = {logit, id};
+            };
+            // A thread's pieces are looked at by its whole warp, one each; of two threads they are on their way together.  (With four a single row
+            // takes 0.4 us less, but a block leaves less room for others: 2,048 rows of 50,257 take 52 us instead of 44.)
+            constexpr int kAhead = 2;
+            unsigned ask = __ballot_sync(~0u, asked_most >= least);
+            if (ask == ~0u && !above) {  // too many
+                ask = 0;
+                if (lane == 0) atomicAdd(&sh.gathered, kRoom + 1);
+            }
+            while (ask) {
+                int first[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) first[k] = ask ? begin + 32 * warp + __ffs(ask) - 1 : end, ask &= ask - 1;
+                for (int k = 0; k < kAhead; ++k) first[k] = ask ? begin + 32 * warp + __ffs(ask) - 1 : end, ask &= ask - 1;
 #pragma unroll 1
-            for (int at = kThreads * lane; at < end - begin; at += kThreads * 32) {
-                uint4 w[kAhead];
-                unsigned hits[kAhead];
+                for (int at = kThreads * lane; at < end - begin; at += kThreads * 32) {
+                    uint4 w[kAhead];
+                    unsigned hits[kAhead];
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) w[k] = first[k] + at < end ? __ldg(from + first[k] + at) : P::nothing();
+                    for (int k = 0; k < kAhead; ++k) w[k] = first[k] + at < end ? __ldg(from + first[k] + at) : P::nothing();
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    hits[k] = 0;
+                    for (int k = 0; k < kAhead; ++k) {
+                        hits[k] = 0;
 #pragma unroll
-                    for (int e = 0; e < P::kCount; ++e) hits[k] |= (unsigned)(P::at(w[k], e) >= bound) << e;
-                    if (first[k] + at >= end) hits[k] = 0;
-                }
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k)
-#pragma unroll 1
-                    for (; hits[k]; hits[k] &= hits[k] - 1) {
-                        const int e = __ffs(hits[k]) - 1;
-                        gather(P::pick(w[k], e), head + (first[k] + at) * P::kCount + e);
+                        for (int e = 0; e < P::kCount; ++e) hits[k] |= (unsigned)(P::at(w[k], e) >= least) << e;
+                        if (first[k] + at >= end) hits[k] = 0;
                     }
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k)
+#pragma unroll 1
+                        for (; hits[k]; hits[k] &= hits[k] - 1) {
+                            const int e = __ffs(hits[k]) - 1;
+                            gather(P::pick(w[k], e), head + (first[k] + at) * P::kCount + e);
+                        }
+                }
             }
-        }
-        at_ends(gather);
-        __syncthreads();
-        int gathered = sh.gathered;
-        const bool crowded = gathered > kRoom;
-        if (crowded) {  // again, what lies above the bound: beside that the lowest tokens at the bound are the best
+            at_ends(gather);
             __syncthreads();
+            gathered = sh.gathered;
+            const bool crowded = gathered > kRoom;
+            if (!crowded || above) {
+                int place = -1;
+                if (tid < gathered) {
+                    const Entry mine = sh.found[tid];
+                    place = 0;
+                    for (int i = 0; i < min(gathered, kRoom); i += 8)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) place += before(sh.found[i + k], mine);  // behind the last: nothing, which is before none
+                    if (place < 32) sh.list[0][place] = mine;
+                } else if (tid < 32) {
+                    sh.list[0][tid] = best;  // nothing
+                }
+                if (!crowded) {
+                    if (!above) break;
+                    // ---- beside what lies above the bound, the lowest tokens at it
+                    const float bound = from_ordered(ordered(least) - 1);
+                    auto add_ties = [&](unsigned hits, int first_id) {  // hits: which of this thread's elements from first_id on; threads in the tokens' order
+                        int upto = __popc(hits);
+#pragma unroll 1
+                        for (int d = 1; d < 32; d <<= 1) {
+                            const int o = __shfl_up_sync(~0u, upto, d);
+                            if (lane >= d) upto += o;
+                        }
+                        __syncthreads();
+                        if (lane == 31) sh.most[warp] = upto;
+                        __syncthreads();
+                        int to = gathered + upto - __popc(hits);
+#pragma unroll 1
+                        for (int i = 0; i < kWarps; ++i) {
+                            if (i < warp) to += sh.most[i];
+                            gathered += sh.most[i];
+                        }
+                        for (; hits && to < p.top; hits &= hits - 1) sh.list[0][to++] = {bound, first_id + __ffs(hits) - 1};
+                    };
+                    if (rank == 0) add_ties(tid < head && P::one(x + tid) == bound, tid);
+#pragma unroll 1
+                    for (int i0 = begin; i0 < end && gathered < p.top; i0 += kThreads) {
+                        unsigned hits = 0;
+                        if (i0 + tid < end) {
+                            const uint4 w = __ldg(from + i0 + tid);
+#pragma unroll
+                            for (int e = 0; e < P::kCount; ++e) hits |= (unsigned)(P::at(w, e) == bound) << e;
+                        }
+                        add_ties(hits, head + (i0 + tid) * P::kCount);
+                    }
+                    if (rank == parts - 1) add_ties(tid < p.V - tail_at && P::one(x + tail_at + tid) == bound, tail_at + tid);
+                    break;
+                }
+                if (place == p.top - 1) sh.bound = ordered(sh.found[tid].x);
+            }
+            __syncthreads();
+            if (above) least = from_ordered(sh.bound);
+            least = from_ordered(ordered(least + 0.0f) + 1);  // the next number (of 0 the smallest above both zeros, of infinity a NaN, which nothing reaches)
             if (tid == 0) sh.gathered = 0;
             sh.found[tid] = {-INFINITY, kNoToken};
             __syncthreads();
-            const float at_bound = bound;
-            // the next number: of 0 the smallest above both zeros, of infinity a NaN, which nothing reaches
-            bound = from_ordered(ordered(bound + 0.0f) + 1);
-#pragma unroll 1
-            for (unsigned ask = __ballot_sync(~0u, looks_again || thread_most >= bound); ask; ask &= ask - 1) {
-                const int first = begin + 32 * warp + __ffs(ask) - 1;
-#pragma unroll 1
-                for (int i = first + kThreads * lane; i < end; i += kThreads * 32) {
-                    const uint4 w = __ldg(from + i);
-#pragma unroll 1
-                    for (int e = 0; e < P::kCount; ++e) gather(P::pick(w, e), head + i * P::kCount + e);
-                }
-                if (*(volatile int*)&sh.gathered > kRoom) break;
-            }
-            at_ends(gather);
-            bound = at_bound;
-            __syncthreads();
-            gathered = sh.gathered;
         }
-        one_list = gathered <= kRoom;
-        if (one_list) {
-            if (tid < gathered) {
-                const Entry mine = sh.found[tid];
-                int place = 0;
-                for (int i = 0; i < gathered; i += 8)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) place += before(sh.found[i + k], mine);  // behind the last: nothing, which is before none
-                if (place < 32) sh.list[0][place] = mine;
-            } else if (tid < 32) {
-                sh.list[0][tid] = best;  // nothing
-            }
-            __syncthreads();
-            if (crowded) {
-                int have = gathered;  // places taken
-                auto add_ties = [&](unsigned hits, int first_id) {  // hits: which of this thread's elements from first_id on; threads in the tokens' order
-                    int upto = __popc(hits);
-#pragma unroll 1
-                    for (int d = 1; d < 32; d <<= 1) {
-                        const int o = __shfl_up_sync(~0u, upto, d);
-                        if (lane >= d) upto += o;
-                    }
-                    if (lane == 31) sh.most[warp] = upto;
-                    __syncthreads();
-                    int place = have + upto - __popc(hits);
-#pragma unroll 1
-                    for (int i = 0; i < kWarps; ++i) {
-                        if (i < warp) place += sh.most[i];
-                        have += sh.most[i];
-                    }
-                    for (; hits && place < p.top; hits &= hits - 1) sh.list[0][place++] = {bound, first_id + __ffs(hits) - 1};
-                    __syncthreads();
-                };
-                if (rank == 0) add_ties(tid < head && P::one(x + tid) == bound, tid);
-#pragma unroll 1
-                for (int i0 = begin; i0 < end && have < p.top; i0 += kThreads) {
-                    unsigned hits = 0;
-                    if (i0 + tid < end) {
-                        const uint4 w = __ldg(from + i0 + tid);
-#pragma unroll
-                        for (int e = 0; e < P::kCount; ++e) hits |= (unsigned)(P::at(w, e) == bound) << e;
-                    }
-                    add_ties(hits, head + (i0 + tid) * P::kCount);
-                }
-                if (rank == parts - 1) add_ties(tid < p.V - tail_at && P::one(x + tail_at + tid) == bound, tail_at + tid);
-            }
-            best = sh.list[0][lane];
-        } else {
-            // Too many there, too: every warp inserts what it finds among its elements into a list of its own.
-            auto look = [&](float logit, int id, bool live) {
-                const Entry mine = {logit, id};
-                const bool reaches = live && logit >= bound;
-                if (!__any_sync(~0u, reaches)) return;
-                const Entry least = from_lane(best, p.top - 1);  // by all lanes
-                unsigned ask = __ballot_sync(~0u, reaches && before(mine, least));
-                for (; ask; ask &= ask - 1) {
-                    const Entry e = from_lane(mine, __ffs(ask) - 1);
-                    const bool stays = before(best, e);
-                    const Entry above = {__shfl_up_sync(~0u, best.x, 1), __shfl_up_sync(~0u, best.id, 1)};
-                    const unsigned keep = __ballot_sync(~0u, stays);  // lanes 0 .. n - 1
-                    if (!stays) best = lane == __popc(keep) ? e : above;
-                }
-            };
-            for (int i0 = begin + 32 * warp; i0 < end; i0 += kThreads) {
-                const int i = i0 + lane;
-                const uint4 w = i < end ? __ldg(from + i) : P::nothing();
-#pragma unroll
-                for (int e = 0; e < P::kCount; ++e) look(P::at(w, e), head + i * P::kCount + e, i < end);
-                const Entry least = from_lane(best, p.top - 1);
-                if (lane == 0 && least.id != kNoToken) atomicMax(&sh.bound, ordered(least.x));
-                bound = fmaxf(bound, from_ordered(*(volatile int*)&sh.bound));
-            }
-            if (rank == 0 && warp == 0) look(lane < head ? P::one(x + lane) : 0.0f, lane, lane < head);
-            if (rank == parts - 1 && warp == kWarps - 1) {
-                const bool live = lane < p.V - tail_at;
-                look(live ? P::one(x + tail_at + lane) : 0.0f, tail_at + lane, live);
-            }
-        }
-        if (!one_list) sh.list[warp][lane] = best;
+        __syncthreads();
+        best = sh.list[0][lane];
     }
 
     // ---- the block, the cluster
@@ -444,7 +397,6 @@ __global__ void __launch_bounds__(kThreads, 6) token_logprobs_kernel(const Logpr
             __syncthreads();
         }
     };
-    if (kTop && !one_list) join_all(kWarps, [&](int i) { return sh.list[i]; });
     if (tid == 0) {
         for (int i = 1; i < kWarps; ++i) own.s0 += sh.sums[i].s0, own.s1 += sh.sums[i].s1;
         sh.block_sums = own;
