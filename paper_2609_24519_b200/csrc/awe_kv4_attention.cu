@@ -8,7 +8,10 @@
 //
 //   - The value's scale goes into the weight as an addition to its exponent, w_j = 2^(s_j / ln 2 + log2 vs_j - m), with m 9 to 15 below the
 //     largest such exponent so far, so that w_j rounds to FP16 as well as it can for what it contributes, and the products of all tokens
-//     add up in one accumulator.  The divisor is the sum of w_j 2^-log2 vs_j before that rounding.
+//     add up in one accumulator.  The divisor is the sum of w_j 2^-log2 vs_j before that rounding.  Where the output is FP16, w_j enters as the sum of
+//     two FP16 numbers, itself rounded and what that left, in a second product: rounded once, it adds as much to an output's error as the
+//     output's own rounding, and a row that sees one token would not have exactly its values (64 requests of up to 8,192 tokens: 103 us for 97).
+//     BF16 outputs round eight times as much themselves.
 //   - A key's nibble with its sign bit flipped, u = code + 8, moved to the top of a mantissa, is FP16's subnormal u 2^-18 (or, four bits
 //     down, u 2^-22, which the queries make up for), so keys take an instruction a pair and half a shift; the zero point goes off the score,
 //     q . K = sum q u - (zero + 8) sum q.  (The instruction lines products up by the exponent that subnormals have, 2^-14: with nibbles at
@@ -22,9 +25,9 @@
 //     tokens' values the 16-bit halves of their words are put together first, which pairs tokens.
 //
 // A token and head of dimension 128 is 132 bytes of keys and values; what bounds long contexts is not reading them but the instructions: some 370 a
-// warp and 16 tokens, half of them on the ALU pipe (53 % of its rate), 60 % of the issue slots.  64 requests of up to 8,192 tokens, 8 heads of 128: 97 us for
+// warp and 16 tokens, half of them on the ALU pipe (52 % of its rate), 61 % of the issue slots.  64 requests of up to 8,192 tokens, 8 heads of 128, BF16: 97 us for
 // 282 MB = 2.9 TB/s (tiles of 16 tokens, keys unpacked like values: 110); 2 of 131,072: 80 us (join by a warp a row: 92).  Four blocks of three
-// stages on an SM (123 registers).
+// stages on an SM (121 registers).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -147,6 +150,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
     using C = Config<kD, kNT>;
     using T16 = typename Half<kBf16>::type;
     constexpr int kRows = C::kRows, kSteps16 = kD / 16, kWords = kD / 32;  // kWords: of keys, a thread and token
+    constexpr int kParts = kBf16 ? 1 : 2;  // FP16 values that a weight is the sum of
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ Search search;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -397,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                             for (int c = 0; c < kSteps16; ++c) o[c][nt][j] *= a, o[c][nt][j + 2] *= a;
                         }
                 }
-                uint32_t pf[kNT][2];
+                uint32_t pf[kNT][2], rest[kNT][2];
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
@@ -407,6 +411,10 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                         sum[nt][0] = fmaf(w0, back[half], sum[nt][0]);
                         sum[nt][1] = fmaf(w1, back[half], sum[nt][1]);
                         pf[nt][half] = movmatrix_trans(w);  // thread (g, t): row g, tokens 2t, 2t + 1 (+ 8 half)
+                        if constexpr (kParts > 1) {
+                            const float2 f = Half<false>::unpack(w);
+                            rest[nt][half] = movmatrix_trans(Half<false>::pack(w0 - f.x, w1 - f.y));
+                        }
                     }
 
 #pragma unroll
@@ -419,7 +427,10 @@ __global__ void __launch_bounds__(kThreads, kNT == 1 && kD <= 128 ? 4 : 0) kv4_a
                             const uint32_t x2 = x >> (8 * h), y2 = y >> (8 * h);
                             const uint32_t f[4] = {kv4_low_codes(x2, vz[0]), kv4_high_codes(x2, vz[0]), kv4_low_codes(y2, vz[1]), kv4_high_codes(y2, vz[1])};
 #pragma unroll
-                            for (int nt = 0; nt < kNT; ++nt) mma_16816<false>(o[4 * w + 2 * half + h][nt], f, pf[nt][0], pf[nt][1]);
+                            for (int nt = 0; nt < kNT; ++nt) {
+                                mma_16816<false>(o[4 * w + 2 * half + h][nt], f, pf[nt][0], pf[nt][1]);
+                                if constexpr (kParts > 1) mma_16816<false>(o[4 * w + 2 * half + h][nt], f, rest[nt][0], rest[nt][1]);
+                            }
                         }
                     }
             }

@@ -331,3 +331,27 @@ def test_errors_as_a_root_mean_square(spread, new, ctx, D, dtype):
             lse = torch.logsumexp(x, 1)
             assert float((s["lse"][:new, i].double() - lse).square().mean().sqrt()) <= 2.0 ** -18 * high + 2.0 ** -22 * float(lse.abs().max())
     assert math.sqrt(total / count) <= 1.0
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (8, 2), (16, 1)])
+@pytest.mark.parametrize("new,ctx,window", [(1, 1, 0), (1, 2, 0), (1, 900, 1), (3, 3, 0), (1, 777, 0), (1, 5000, 0), (6, 300, 40)])
+def test_fp16_outputs_of_few_rows_are_rounded_once(new, ctx, window, Hq, H, D):
+    """A weight is off by 2^-22 of itself beside the output's own rounding, u |out|: scores below 2^5, exponentials and sums add less than 2^-17 of
+    sum p |v|.  Of one token the output is its values."""
+    s = make([new], [ctx], Hq, H, D, 16, b.F16, window, seed=D + ctx)
+    call(s)
+    u, G = 2.0 ** -11, Hq // H
+    pages = s["table"][0, :-(-ctx // 16)].long()
+    tok, pos = torch.arange(ctx, device="cuda"), torch.arange(ctx - new, ctx, device="cuda")[:, None]
+    hidden = (tok > pos) | ((tok <= pos - window) if window else torch.zeros_like(tok > pos))
+    for h in range(H):
+        k, v = (values(s[a][pages, h], s[a + "p"][pages, h]).reshape(-1, D)[:ctx] for a in "kv")
+        for i in range(G * h, G * h + G):
+            x = (s["q"][:, i * D:(i + 1) * D].double() @ k.t() * s["scale"]).masked_fill(hidden, -math.inf)
+            assert float(x.masked_fill(hidden, 0.0).abs().max()) < 2 ** 5 * math.log(2.0)
+            p = torch.softmax(x, 1)
+            want, got = p @ v, s["out"][:new, i * D:(i + 1) * D].double()
+            assert bool(((got - want).abs() <= u * want.abs() + (1 + u) * 2.0 ** -17 * (p @ v.abs()) + 2.0 ** -25).all())
+            if ctx == 1 or window == 1:
+                assert torch.equal(got, v[-1:].half().double())
