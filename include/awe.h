@@ -484,10 +484,11 @@ size_t awe_kv4_attention_workspace_bytes(awe_handle_t h, const awe_kv4_cache* ca
 /* awe_kv_attention over the cache of 4 bits, with the same arguments, and the same answers for rows that see nothing.  Scores are FP32 sums of
  * exact products.  For few query rows they are the difference of two, of q (code + 8) and (zero + 8) q, off by up to head_dim 2^-23 of 15 times the key's
  * scale times the query's sum of magnitudes even where its products with the key are small, and a query's elements below 2^-26 of its largest
- * lose bits.  The divisor and lse are summed before weights are rounded to FP16.  What that costs depends on the kernel, which the sizes alone
- * choose: for few query rows a token's weight times its value's scale is off by 2^-11 of itself (2^-22 where q is AWE_F16) or 2^-34 of the
- * largest such product; for prompts the weight alone is, by 2^-11 of itself or 2^-34 of the largest weight, so that a token far below the largest
- * loses bits however large its value's scale is. */
+ * lose bits.  lse and the divisor are summed before weights are rounded to FP16 (the divisor behind it for rows of FP16 prompts that see fewer than 32
+ * tokens, where the rounding cancels: a row of one token has its values).  What that costs depends on the kernel, which the sizes alone choose: for few
+ * query rows a token's weight times its value's scale is off by 2^-11 of itself (2^-22 where q is AWE_F16) or 2^-34 of the largest such product; for
+ * prompts the weight alone is, by 2^-11 of itself or 2^-34 of the largest weight, so that a token far below the largest loses bits however large its
+ * value's scale is. */
 awe_status_t awe_kv4_attention(awe_handle_t h, const awe_kv4_cache* cache, const void* q_dev, awe_float_t type, int64_t T,
                                int64_t n_q_heads, int64_t ldq, const int32_t* q_start_dev, const int32_t* ctx_len_dev, int64_t B,
                                const int32_t* block_table_dev, int64_t max_pages, int64_t ld_table, float scale, int causal,

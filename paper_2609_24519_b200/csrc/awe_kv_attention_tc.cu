@@ -19,7 +19,7 @@
 // The cache of 4 bits has a scale for every token.  Its values, scale times (code - zero), are exact in FP16, so they are unpacked whole
 // and the softmax knows no scales: P is the weight alone, rounded by 2^-11 of itself or 2^-34 of the largest weight (m, which moves by whole
 // numbers, stays 9 to 15 below the largest s), whatever the values' scales.  A word's eight codes come apart in the order 0 4 1 5 2 6 3 7, in which the operands keep them: queries are
-// brought into it, results back.  2,048 queries of 8,192 tokens, 32 / 8 heads of 128: 349 us, 690 TFLOP/s; with S read twice, as for 8 bits, 373.
+// brought into it, results back.  2,048 queries of 8,192 tokens, 32 / 8 heads of 128: 347 us, 690 TFLOP/s; with S read twice, as for 8 bits, 373.
 //
 // All steps of all units in a row are dealt out evenly to one block per SM; units that were cut are joined by a second
 // kernel in the order of the tokens.  A small kernel before lists the units' steps, which causality makes uneven.
@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_attention_units_kernel(const 
 }
 
 constexpr int kSharedBytes = 3 * 1024;  // room for Shared
+constexpr int kFewTokens = 32;  // of more, errors are at most 1.4 times those of weights in FP32, here 1.3; 2,048 FP16 queries of 8,192 tokens 341 -> 347 us
 constexpr float kDivisorUnit = 1.0f / 4096, kDivisorLog2 = 12.0f;
 
 template <int kD>
@@ -212,6 +213,9 @@ template <int kD, bool kBf16, bool kFour>
 __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAttnParams tp) {
     using C = Config<kD>;
     using T16 = typename Half<kBf16>::type;
+    // FP16 outputs over the cache of 4 bits: where a warp has a row that sees few tokens, the divisor is the sum of the rounded weights, so that the
+    // rounding of a token that dominates cancels and a row of one token has exactly its values.  (BF16 outputs round eight times as much themselves.)
+    constexpr bool kRounded = kFour && !kBf16;
     const AttnParams& p = tp.a;
     extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles
     const uint32_t base = ptx::smem_u32(smem);
@@ -556,7 +560,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             if (!live || see_hi < 0) see_hi = 0;
             // steps that begin in [all_lo, whole_hi] are seen whole by all rows (their ends may pass 32 bits)
             const int all_lo = __reduce_max_sync(~0u, live ? see_lo : 0), whole_hi = __reduce_min_sync(~0u, live ? see_hi : 0x7FFFFFFF) - kStep;
-            float m_ref = -INFINITY, sum = 0.0f;
+            float m_ref = -INFINITY, sum = 0.0f, rounding = 0.0f;  // rounding: what the divisor is more than the sum (kRounded)
+            const bool few = kRounded && __any_sync(~0u, live && see_hi - see_lo < kFewTokens);
             if constexpr (kFour) cq = factor_of(1.0f, cq);
             else sh->unvalued_sum[128 * t + row] = make_float2(-INFINITY, 0.0f);  // this thread's alone
             for (int j = s0; j < s1; ++j, ++step, ++done) {
@@ -584,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                     // One pass: P against the reference so far, with the largest score beside it, half a step at a time.  Where a row's passes the
                     // reference by too much (its first step, rarely a later one), the reference moves, by a whole number so that what there is of O
                     // and P follows exactly, and the warp goes over the half once more, which P has not taken the place of yet.
-                    float part = 0.0f;
+                    float part = 0.0f, part_rounding = 0.0f;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t from = s_at[t] + lanes + 64 * half;
@@ -633,6 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                                 if (grows) m_ref = first ? top - kBelow : m_ref + ceilf(top - kBelow - m_ref);
                                 const float shrink = first || !grows ? 1.0f : exp2_approx(before - m_ref);
                                 sum *= shrink, part *= shrink;
+                                if constexpr (kRounded) rounding *= shrink, part_rounding *= shrink;
                                 if (j > s0 && __any_sync(~0u, shrink != 1.0f) && !rescale(shrink)) return false;
                                 if (half) {
                                     uint32_t before_p[32];
@@ -646,11 +652,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                                 }
                             } else {
                                 part += even + odd;
+                                if (kRounded && few) {
+                                    float rounded = 0.0f;
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) {
+                                        const float2 f = Half<false>::unpack(pk[e]);
+                                        rounded += f.x + f.y;
+                                    }
+                                    part_rounding += rounded - (even + odd);
+                                }
                                 ptx::tmem_st_32x32(s_at[t] + lanes + 32 * half, pk);
                             }
                         }
                     }
                     sum += part;
+                    if constexpr (kRounded) rounding += part_rounding;
                 } else {
                     // Both passes read S in pieces of 32 tokens, the next on its way meanwhile; 16 tokens share their scales.
                     auto for_pieces = [&](auto f) {
@@ -735,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
                 keep *= a;
                 m_all = m;
             }
-            const float inv = sum == 0.0f ? 0.0f : keep / sum;
+            const float inv = sum == 0.0f ? 0.0f : keep / (kRounded ? sum + rounding : sum);
             T16* dst = reinterpret_cast<T16*>(p.out) + token * p.ldo + (int64_t)qh * kD;
 #pragma unroll 1
             for (int c = 0; c < kD; c += 32) {
@@ -760,7 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attention_tc_kernel(const TcAt
             }
             ptx::tc_fence_before();
             if (live) {
-                if (!whole) p.part_stat[part_row] = make_float4(m_all, sum, 0.0f, 0.0f);
+                if (!whole) p.part_stat[part_row] = make_float4(m_all, sum, rounding, 0.0f);
                 else if (p.lse) p.lse[token * p.heads * p.group + qh] = sum == 0.0f ? -INFINITY : (m_all + log2f(sum)) * 0.69314718056f;
             }
             return true;
@@ -799,7 +815,7 @@ __global__ void __launch_bounds__(128) kv_attention_tc_join_kernel(const TcAttnP
     const int first = deal.block_of(w0), last = deal.block_of(w0 + steps - 1);
     if (first == last) return;  // one block had all of it
     constexpr int kVecs = kD == 64 ? 1 : kD / 128;
-    float m = -INFINITY, sum = 0.0f;
+    float m = -INFINITY, sum = 0.0f, rounding = 0.0f;
     float4 x[kVecs];
 #pragma unroll
     for (auto& v : x) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -809,7 +825,7 @@ __global__ void __launch_bounds__(128) kv_attention_tc_join_kernel(const TcAttnP
         const float m_new = fmaxf(m, st.x);
         const float a = m == -INFINITY ? (sum == 0.0f ? 0.0f : 1.0f) : exp2_approx(m - m_new);
         const float c = st.x == -INFINITY ? (st.y == 0.0f ? 0.0f : 1.0f) : exp2_approx(st.x - m_new);
-        sum = fmaf(sum, a, st.y * c);
+        sum = fmaf(sum, a, st.y * c), rounding = fmaf(rounding, a, st.z * c);
         m = m_new;
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
@@ -821,7 +837,7 @@ __global__ void __launch_bounds__(128) kv_attention_tc_join_kernel(const TcAttnP
             }
         }
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / (sum + rounding);
     T16* dst = reinterpret_cast<T16*>(p.out) + (int64_t)token * p.ldo + (int64_t)qh * kD;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {

@@ -355,3 +355,32 @@ def test_fp16_outputs_of_few_rows_are_rounded_once(new, ctx, window, Hq, H, D):
             assert bool(((got - want).abs() <= u * want.abs() + (1 + u) * 2.0 ** -17 * (p @ v.abs()) + 2.0 ** -25).all())
             if ctx == 1 or window == 1:
                 assert torch.equal(got, v[-1:].half().double())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,ctx,window", [(1500, 1500, 0), (1500, 3000, 1), (2000, 2500, 3), (1500, 1600, 20)])
+def test_fp16_prompts_rows_of_few_tokens(new, ctx, window, D):
+    """Rows that see one token have its values; of few, the weights' roundings (2^-11 of each, d_j) are off by sum p_j d_j (v_j - out), and the output's
+    own by u |out|: scores, exponentials and sums add less than 2^-17 of sum p |v|."""
+    s = make([new], [ctx], 8, 2, D, 16, b.F16, window, seed=D + ctx, width=256)
+    assert call(s) == 3
+    u = 2.0 ** -11
+    pages = s["table"][0, :-(-ctx // 16)].long()
+    tok, pos = torch.arange(ctx, device="cuda"), torch.arange(ctx - new, ctx, device="cuda")[:, None]
+    seen = (tok <= pos) & ((tok > pos - window) if window else torch.ones_like(tok <= pos))
+    few = seen.sum(1) < 32
+    assert bool(few.any())
+    for h in range(2):
+        k, v = (values(s[a][pages, h], s[a + "p"][pages, h]).reshape(-1, D)[:ctx] for a in "kv")
+        for i in range(4 * h, 4 * h + 4):
+            x = (s["q"][:, i * D:(i + 1) * D].double() @ k.t() * s["scale"]).masked_fill(~seen, -math.inf)[few]
+            p = torch.softmax(x, 1)
+            want, got = p @ v, s["out"][:new, i * D:(i + 1) * D].double()[few]
+            for r0 in range(0, len(p), 256):
+                q, w = p[r0:r0 + 256], want[r0:r0 + 256]
+                near = q.sum(0) > 0
+                spread = torch.einsum("rn,rnd->rd", q[:, near], (v[near] - w[:, None]).abs())
+                bound = u * w.abs() + (1 + u) * (u * spread + 2.0 ** -17 * (q @ v.abs())) + 2.0 ** -25
+                assert bool(((got[r0:r0 + 256] - w).abs() <= bound).all())
+            one = seen[few].sum(1) == 1
+            assert torch.equal(got[one], (seen[few][one].double() @ v).half().double())
