@@ -9,8 +9,8 @@
 // needs four cosines and four sines, which it keeps for its rows (heads) of a token; each row is read once and written once.  A block has
 // one token's keys, its values or a part of its queries: mixed rows in one block took a quarter of the instructions to tell them apart.
 //
-// 19.6 k tokens of 32 query and 8 cache heads of 128: 98 us for 403 MB = 4.1 TB/s, with 62 % of the issue slots used (a first form of one
-// kind of block, a division for each value: 138 us); 64 tokens 3.6 us with the read-back behind it.  The read-back of 19.6 k: 27 us for 121 MB.
+// 19,707 tokens of 32 query and 8 cache heads of 128: 98 us for 430 MB = 4.4 TB/s, with 62 % of the issue slots used (a first form of one
+// kind of block, a division for each value: 138 us); 64 tokens 3.6 us with the read-back behind it.  Their read-back: 27 us for 102 MB = 3.8 TB/s.
 #include <algorithm>
 #include <type_traits>
 
